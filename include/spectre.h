@@ -426,6 +426,110 @@ int spectre_prefix_step(spectre_prefix_cache *cache /*host*/, const void *v_t, c
                         const spectre_gate_params *P /*host*/, void *out, spectre_dtype io,
                         void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Attention layers beside the spectral ones.  A model that replaces only some of its attention heads keeps the keys and
+ * values of the others in pages; these calls write them, attend over them and manage the pages.
+ *
+ *   H query heads share Hkv key/value heads in groups of G = H / Hkv (head h reads key head h / G).  d = 64 or 128.
+ *   Rows are [T, heads, d] of dtype io with heads adjacent and tokens `stride` elements apart (a multiple of 16 bytes, at
+ *   least heads * d), base addresses 16-byte aligned.  A batch's new tokens stand one sequence after the other:
+ *   sequence b has tokens start[b] .. start[b+1] - 1 (device int32 [B + 1], ascending, start[0] = 0, start[B] <= T; rows behind it are
+ *   left as they are).
+ *
+ * A pool of pages, caller-owned device memory described by a host struct.  A page holds `page` tokens of every key/value head:
+ *   k  [layers, pages, Hkv, d / E, page, E]      v  [layers, pages, Hkv, page / E, d, E]       E = 16 bytes of elements
+ *   book  int32: 8 words of status, lens [seqs], users of each page [pages], page numbers [seqs, max_pages] (-1: none)
+ * Sequence s of lens[s] tokens has them in the first ceil(lens[s] / page) pages of its row.  All of it is device state, so reserving pages
+ * and decoding can be captured into a graph together.  A page number outside 0 .. pages - 1 is never followed: nothing is written
+ * there, and attention treats its tokens as absent.  A pool is worked on by one stream at a time.
+ */
+typedef struct {
+    int layers, pages;         /* pages: of each layer                                       */
+    int Hkv, d;
+    int page;                  /* tokens a page: 16, 32, 64, 128 or 256                      */
+    int seqs, max_pages;       /* rows of the table, page numbers a row                      */
+    spectre_dtype dtype;
+    void *k, *v;               /* device, 16-byte aligned                                    */
+    int *book;                 /* device                                                     */
+} spectre_kv;
+
+enum { SPECTRE_KV_MAX_SEQS = 65536, SPECTRE_KV_MAX_TABLE = 1 << 20 };      /* limits of seqs and max_pages */
+enum { SPECTRE_KV_K = 0, SPECTRE_KV_V = 1, SPECTRE_KV_BOOK = 2 };
+
+/* Words of the status (book[0 .. 7]): [0] bits of what calls found wrong, kept until the caller clears them; [1] pages that the last
+ * spectre_kv_fork or _compact copied; [2] pages in use after the last _compact. */
+enum { SPECTRE_KV_NO_PAGES = 1, SPECTRE_KV_TOO_LONG = 2, SPECTRE_KV_BAD_ARGUMENT = 4, SPECTRE_KV_NOT_EMPTY = 8 };
+
+/* Bytes of the pool's arrays (which: SPECTRE_KV_K, _V, _BOOK); 0 for a pool that is not supported.  Only sizes and dtype are read. */
+size_t spectre_kv_bytes(const spectre_kv *kv /*host*/, int which);
+
+/* Set-up, once per device before any call below is captured into a graph: loads their kernels. */
+int spectre_kv_prepare(void);
+
+/* Empty bookkeeping: no sequence has a token, no page a user.  Page contents are left as they are. */
+int spectre_kv_init(const spectre_kv *kv /*host*/, void *stream);
+
+/*
+ * Page management; seqs, src, dst, add are device int32 [n], n = 0 is a call that does nothing.  Pages are taken lowest number first, in the
+ * order of the list.  A call that cannot be carried out as a whole sets bits of the status and changes nothing else
+ * (spectre_kv_free and _copy: leave out what is out of range).
+ *   reserve  sequence seqs[i] grows by add[i] >= 0 tokens, whose contents are whatever the pages hold.  No sequence twice.
+ *   fork     dst[i], empty, becomes what src[i] is: full pages are shared, the tokens of a last page that is not full are copied (in
+ *            whole 16-byte groups of V) into a page of its own, in every layer.  No dst twice, none that is a src.
+ *   free     the sequences' pages lose a user each; the sequences are empty.
+ *   compact  pages in use move so that their numbers are 0 .. in use - 1: the i-th page in use above goes to the i-th free one below.
+ *   copy     the contents of page src[i] of every layer to page dst[i]; no dst twice, none that is a src.
+ */
+size_t spectre_kv_workspace_bytes(const spectre_kv *kv /*host*/, int n);   /* of reserve, fork and compact (n = 0) */
+int spectre_kv_reserve(const spectre_kv *kv /*host*/, const int *seqs, const int *add, int n, void *ws, size_t ws_bytes, void *stream);
+int spectre_kv_fork(const spectre_kv *kv /*host*/, const int *src, const int *dst, int n, void *ws, size_t ws_bytes, void *stream);
+int spectre_kv_free(const spectre_kv *kv /*host*/, const int *seqs, int n, void *stream);
+int spectre_kv_compact(const spectre_kv *kv /*host*/, void *ws, size_t ws_bytes, void *stream);
+int spectre_kv_copy(const spectre_kv *kv /*host*/, const int *src, const int *dst, int n, void *stream);
+
+/*
+ * Norm and rotation of query and key heads.  Per row x: y = w * x / sqrt(mean x^2 + eps), then each pair of the first `rot` channels is turned by
+ * the angle position * inv_freq[i], formed in fp64: (a, b) -> (a cos - b sin, b cos + a sin); pair i is channels (i, i + rot/2), or (2i, 2i + 1)
+ * when interleaved.  wq, wk device fp32 [d], both NULL: no norm.  rot = 0: no rotation; else a multiple of 16 up to d, inv_freq device fp64 [rot / 2].
+ */
+typedef struct {
+    int d, rot, interleaved;
+    float eps;
+    const double *inv_freq;
+    const float *wq, *wk;
+} spectre_heads;
+
+/* q [T, H, d], k [T, Hkv, d] -> q_out, k_out of the same shapes, dense.  positions: device int32 [T], NULL: 0 .. T - 1. */
+int spectre_heads_forward(const spectre_heads *P /*host*/, const void *q, long long q_stride, const void *k, long long k_stride, const int *positions,
+                          int T, int H, int Hkv, spectre_dtype io, void *q_out, void *k_out, void *stream);
+
+/* Its gradients: from dq, dk (of q_out and k_out; strides of their own) and the inputs, gq [T, H, d], gk [T, Hkv, d] (dense) and, with a norm,
+ * gwq, gwk fp32 [d].  The sums over tokens and heads are formed in fp64 in a fixed order. */
+size_t spectre_heads_backward_workspace_bytes(int T, int d);
+int spectre_heads_backward(const spectre_heads *P /*host*/, const void *dq, long long dq_stride, const void *dk, long long dk_stride, const void *q,
+                           long long q_stride, const void *k, long long k_stride, const int *positions, int T, int H, int Hkv, spectre_dtype io,
+                           void *gq, void *gk, float *gwq, float *gwk, void *ws, size_t ws_bytes, void *stream);
+
+/* Serving: the new tokens are the last ones of their sequences (spectre_kv_reserve has made room): token i of the n of sequence seqs[b] (NULL: b) has
+ * position lens - n + i.  Queries go to q_out [T, H, d], keys, with norm and rotation, and values into the pages of `layer`.  A sequence of
+ * fewer than n tokens, or a row outside the table, is left out.  No sequence twice. */
+int spectre_kv_append(const spectre_kv *kv /*host*/, int layer, const spectre_heads *P /*host*/, const void *q, long long q_stride, const void *k,
+                      long long k_stride, const void *v, long long v_stride, const int *start, const int *seqs, int B, int T, int H,
+                      void *q_out, void *stream);
+
+/*
+ * spectre_kv_attend - attention of new tokens over the pages: query i of a sequence's n stands at p = lens - n + i and sees the keys j <= p, with
+ * window > 0 only j > p - window.  out [T, H, d] = softmax(scale q.k) v of dtype, lse fp32 [T, H] (NULL: not wanted) the logarithm of its
+ * denominator.  A row that sees no key gets out = 0 and lse = -inf; keys that a row does not see, and what lies behind a sequence's
+ * last token, take no part even if they are infinite or NaN.
+ *   max_new, max_len   bounds of the sequences' new tokens and lengths, which the launch is sized by: a sequence with more new tokens than
+ *                      max_new has the rest left out; a length above max_len costs time only
+ *   scale              above zero
+ */
+size_t spectre_kv_attend_workspace_bytes(const spectre_kv *kv /*host*/, int B, int T, int H, int max_new, int max_len, int window);
+int spectre_kv_attend(const spectre_kv *kv /*host*/, int layer, const void *q, long long q_stride, const int *start, const int *seqs, int B, int T,
+                      int H, int max_new, int max_len, float scale, int window, void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

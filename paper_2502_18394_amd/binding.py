@@ -50,6 +50,17 @@ class PrefixCacheC(ctypes.Structure):
                 ("pending_slot", ctypes.c_int * 32)]
 
 
+class KvC(ctypes.Structure):
+    _fields_ = [("layers", ctypes.c_int), ("pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("d", ctypes.c_int), ("page", ctypes.c_int),
+                ("seqs", ctypes.c_int), ("max_pages", ctypes.c_int), ("dtype", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("book", ctypes.c_void_p)]
+
+
+class HeadsC(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_int), ("rot", ctypes.c_int), ("interleaved", ctypes.c_int), ("eps", ctypes.c_float),
+                ("inv_freq", ctypes.c_void_p), ("wq", ctypes.c_void_p), ("wk", ctypes.c_void_p)]
+
+
 def lib():
     """The loaded C library; raises if it is missing (never falls back to another path)."""
     global _lib
@@ -63,12 +74,13 @@ def lib():
                      "spectre_wrm_apply_workspace_bytes",
                      "spectre_prefix_update_workspace_bytes", "spectre_prefix_readout_workspace_bytes",
                      "spectre_prefix_step_workspace_bytes", "spectre_prefix_set_memory_workspace_bytes",
-                     "spectre_mix_static_bytes", "spectre_layer_workspace_bytes"):
+                     "spectre_mix_static_bytes", "spectre_layer_workspace_bytes", "spectre_kv_bytes", "spectre_kv_workspace_bytes",
+                     "spectre_kv_attend_workspace_bytes", "spectre_heads_backward_workspace_bytes"):
             getattr(L, name).restype = ctypes.c_size_t
         L.spectre_get_option.restype = ctypes.c_long
         # with the types declared, ctypes converts plain integers itself: a wrapper object per argument costs a few
         # microseconds a call, as much as the kernels of the smallest ones take
-        p, i, n, f = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_double
+        p, i, n, f, ll = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_double, ctypes.c_longlong
         for name, types in {
                 "spectre_mix_workspace_bytes": (i, i, i, i, i),
                 "spectre_mix_forward_ex": (p, p, p, i, i, i, i, i, ctypes.c_uint, p, n, p),
@@ -82,7 +94,16 @@ def lib():
                 "spectre_prefix_readout_workspace_bytes": (p, i, i),
                 "spectre_prefix_readout": (p, p, i, p, i, p, n, p),
                 "spectre_prefix_step_workspace_bytes": (p, p),
-                "spectre_prefix_step": (p, p, p, p, p, i, p, n, p)}.items():
+                "spectre_prefix_step": (p, p, p, p, p, i, p, n, p),
+                "spectre_kv_bytes": (p, i), "spectre_kv_workspace_bytes": (p, i), "spectre_kv_prepare": (), "spectre_kv_init": (p, p),
+                "spectre_kv_reserve": (p, p, p, i, p, n, p), "spectre_kv_fork": (p, p, p, i, p, n, p), "spectre_kv_free": (p, p, i, p),
+                "spectre_kv_compact": (p, p, n, p), "spectre_kv_copy": (p, p, p, i, p),
+                "spectre_heads_forward": (p, p, ll, p, ll, p, i, i, i, i, p, p, p),
+                "spectre_heads_backward_workspace_bytes": (i, i),
+                "spectre_heads_backward": (p, p, ll, p, ll, p, ll, p, ll, p, i, i, i, i, p, p, p, p, p, n, p),
+                "spectre_kv_append": (p, i, p, p, ll, p, ll, p, ll, p, p, i, i, i, p, p),
+                "spectre_kv_attend_workspace_bytes": (p, i, i, i, i, i, i),
+                "spectre_kv_attend": (p, i, p, ll, p, p, i, i, i, i, i, ctypes.c_float, i, p, p, p, n, p)}.items():
             getattr(L, name).argtypes = types
         _lib = L
     return _lib
@@ -478,3 +499,273 @@ class PrefixCache:
         _check(lib().spectre_prefix_step(ctypes.byref(self.c), _ptr(v_t, "v_t"), _ptr(q_t, "q_t"), ctypes.byref(P.c),
                                          _ptr(out, "out"), io, wsp, wsn, _stream(stream)))
         return out
+
+
+def _rows(t, name, dtype, T=None, heads=None):
+    """(address, elements from token to token) of rows [T, heads, d]: heads adjacent, tokens any distance apart."""
+    if not t.is_cuda or t.dim() != 3:
+        raise ValueError(f"{name} must be a device tensor [T, heads, d]")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, not {dtype}")
+    n, h, d = t.shape
+    if (T is not None and n != T) or (heads is not None and h != heads):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not [{T}, {heads}, d]")
+    st, sh, sc = t.stride()
+    if (sc != 1 and d > 1) or (sh != d and h > 1):
+        raise ValueError(f"{name} must have its heads' channels adjacent")
+    return t.data_ptr(), st if n > 1 else h * d
+
+
+def _ints(t, name, n=None):
+    if t.dtype != torch.int32:
+        raise TypeError(f"{name} must be int32")
+    if t.dim() != 1 or (n is not None and t.numel() != n):
+        raise ValueError(f"{name} must be one-dimensional" + ("" if n is None else f" of {n} entries"))
+    return _ptr(t, name)
+
+
+def _new(shape, dtype, device, stream):
+    """A tensor that work on `stream` (None: the current one) writes: its memory comes from that stream's blocks."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+_kv_prepared = set()
+
+
+def _kv_prepare():
+    dev = torch.cuda.current_device()
+    if dev not in _kv_prepared:
+        _check(lib().spectre_kv_prepare())
+        _kv_prepared.add(dev)
+
+
+class Rope:
+    """Angles by which a head's channels are turned: position * inv_freq[i] for pair i.  inv_freq: float64 [rot / 2] (any rule a model has for
+    it), or use Rope.of for theta^(-2 i / rot)."""
+
+    def __init__(self, inv_freq, interleaved=False, device="cuda"):
+        self.inv_freq = torch.as_tensor(inv_freq, dtype=torch.float64).to(device).contiguous()
+        if self.inv_freq.dim() != 1:
+            raise ValueError("inv_freq must be one-dimensional")
+        self.rot, self.interleaved = 2 * self.inv_freq.numel(), bool(interleaved)
+
+    @classmethod
+    def of(cls, rot, theta=10000.0, interleaved=False, device="cuda"):
+        return cls(theta ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot), interleaved, device)
+
+
+def _heads(d, rope, wq, wk, eps):
+    """The C parameters; rope None: no rotation, wq and wk None: no norm."""
+    for w, name in ((wq, "wq"), (wk, "wk")):
+        if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,)):
+            raise ValueError(f"{name} must be float32 [{d}]")
+    return HeadsC(d, rope.rot if rope else 0, int(rope.interleaved) if rope else 0, eps, rope.inv_freq.data_ptr() if rope else None,
+                  None if wq is None else _ptr(wq, "wq"), None if wk is None else _ptr(wk, "wk"))
+
+
+def qk_norm_rotate(q, k, positions=None, rope=None, wq=None, wk=None, eps=1e-6, q_out=None, k_out=None, stream=None):
+    """Norm of each query and key head and rotation by position in one pass (spectre_heads_forward).  q [T,H,d], k [T,Hkv,d] f32/bf16, tokens any
+    16-byte multiple apart; positions int32 [T] (None: 0 .. T-1); wq, wk float32 [d], both None: no norm.  Returns (q_out, k_out)."""
+    T, H, d = q.shape
+    Hkv = k.shape[1]
+    io = _dtype_code(q)
+    qa, qs = _rows(q, "q", q.dtype)
+    ka, ks = _rows(k, "k", q.dtype, T)
+    if k.shape[2] != d:
+        raise ValueError("q and k differ in d")
+    P = _heads(d, rope, wq, wk, eps)
+    if q_out is None:
+        q_out = _new((T, H, d), q.dtype, q.device, stream)
+    if k_out is None:
+        k_out = _new((T, Hkv, d), q.dtype, q.device, stream)
+    _same(q_out, q, "q_out")
+    _same(k_out, k, "k_out")
+    _check(lib().spectre_heads_forward(ctypes.byref(P), qa, qs, ka, ks, None if positions is None else _ints(positions, "positions", T), T, H, Hkv, io,
+                                       _ptr(q_out, "q_out"), _ptr(k_out, "k_out"), _raw_stream(stream)))
+    return q_out, k_out
+
+
+def _same(t, like, name):
+    if t.shape != like.shape or t.dtype != like.dtype:
+        raise ValueError(f"{name} must be {like.dtype} {tuple(like.shape)}")
+
+
+def qk_norm_rotate_backward(dq, dk, q, k, positions=None, rope=None, wq=None, wk=None, eps=1e-6, ws=None, stream=None):
+    """Gradients of qk_norm_rotate (spectre_heads_backward) from those of its outputs and its inputs.
+    Returns (gq, gk, gwq, gwk), the last two None without a norm."""
+    T, H, d = q.shape
+    Hkv = k.shape[1]
+    io = _dtype_code(q)
+    if tuple(k.shape) != (T, Hkv, d) or dq.shape != q.shape or dk.shape != k.shape:
+        raise ValueError("dq and dk must have the shapes of q [T,H,d] and k [T,Hkv,d]")
+    P = _heads(d, rope, wq, wk, eps)
+    rows = [_rows(t, name, q.dtype) for t, name in ((dq, "dq"), (dk, "dk"), (q, "q"), (k, "k"))]
+    gq, gk = _new((T, H, d), q.dtype, q.device, stream), _new((T, Hkv, d), q.dtype, q.device, stream)
+    gw, wsp, wsn = (None, None), None, 0
+    if wq is not None:
+        gw = _new((2, d), torch.float32, q.device, stream).unbind(0)
+        if ws is None:
+            ws = _new((lib().spectre_heads_backward_workspace_bytes(T, d) + 256,), torch.uint8, q.device, stream)
+        wsp, wsn = _given(ws)
+    _check(lib().spectre_heads_backward(ctypes.byref(P), *rows[0], *rows[1], *rows[2], *rows[3],
+                                        None if positions is None else _ints(positions, "positions", T), T, H, Hkv, io, gq.data_ptr(), gk.data_ptr(),
+                                        None if gw[0] is None else gw[0].data_ptr(), None if gw[1] is None else gw[1].data_ptr(), wsp, wsn,
+                                        _raw_stream(stream)))
+    return gq, gk, gw[0], gw[1]
+
+
+class KvPages:
+    """Keys and values of attention layers in pages, with their bookkeeping on the device (spectre_kv; layout and rules in spectre.h).
+
+    KvPages.empty(...) allocates an empty pool; the constructor takes tensors that exist:
+    k_pages [layers, pages, Hkv, d/E, page, E], v_pages [layers, pages, Hkv, page/E, d, E] (E = 8 bf16 or 4 f32 elements),
+    book int32 [8 + seqs + pages + seqs * max_pages]."""
+
+    NO_PAGES, TOO_LONG, BAD_ARGUMENT, NOT_EMPTY = 1, 2, 4, 8          # bits of the status
+
+    def __init__(self, k_pages, v_pages, book, seqs, max_pages):
+        io = _dtype_code(k_pages)
+        E = 8 if io == BF16 else 4
+        if k_pages.dim() != 6 or k_pages.shape[5] != E:
+            raise ValueError(f"k_pages must be [layers, pages, Hkv, d/{E}, page, {E}]")
+        layers, pages, Hkv, groups, page, _ = k_pages.shape
+        d = groups * E
+        if tuple(v_pages.shape) != (layers, pages, Hkv, page // E, d, E) or v_pages.dtype != k_pages.dtype:
+            raise ValueError(f"v_pages must be {k_pages.dtype} [layers, pages, Hkv, page/{E}, d, {E}]")
+        if book.numel() != 8 + seqs + pages + seqs * max_pages:
+            raise ValueError("book must have 8 + seqs + pages + seqs * max_pages entries")
+        self.layers, self.pages, self.Hkv, self.d, self.page, self.seqs, self.max_pages = layers, pages, Hkv, d, page, seqs, max_pages
+        self.dtype, self.k_pages, self.v_pages, self.book = k_pages.dtype, k_pages, v_pages, book
+        self.c = KvC(layers, pages, Hkv, d, page, seqs, max_pages, io, _ptr(k_pages, "k_pages"), _ptr(v_pages, "v_pages"), _ints(book, "book"))
+        self._ref = ctypes.byref(self.c)
+        if lib().spectre_kv_bytes(self._ref, 0) == 0:
+            raise SpectreError(EUNSUPPORTED, lib().spectre_last_error().decode())
+        _kv_prepare()
+        self._ws = {}
+
+    @classmethod
+    def empty(cls, layers, pages, Hkv, d, page, seqs, max_pages, dtype=torch.bfloat16, device="cuda"):
+        c = KvC(layers, pages, Hkv, d, page, seqs, max_pages, BF16 if dtype == torch.bfloat16 else F32, None, None, None)
+        n = lib().spectre_kv_bytes(ctypes.byref(c), 0)
+        if n == 0:
+            raise SpectreError(EUNSUPPORTED, lib().spectre_last_error().decode())
+        E = 8 if dtype == torch.bfloat16 else 4
+        k = torch.zeros((layers, pages, Hkv, d // E, page, E), dtype=dtype, device=device)
+        v = torch.zeros((layers, pages, Hkv, page // E, d, E), dtype=dtype, device=device)
+        book = torch.empty(8 + seqs + pages + seqs * max_pages, dtype=torch.int32, device=device)
+        pool = cls(k, v, book, seqs, max_pages)
+        pool.reset()
+        return pool
+
+    def reset(self, stream=None):
+        """No sequence has a token, no page a user."""
+        _check(lib().spectre_kv_init(self._ref, _raw_stream(stream)))
+
+    # views of the bookkeeping, on the device
+    @property
+    def status(self):
+        return self.book[:8]
+
+    @property
+    def lens(self):
+        return self.book[8:8 + self.seqs]
+
+    @property
+    def refs(self):
+        return self.book[8 + self.seqs:8 + self.seqs + self.pages]
+
+    @property
+    def table(self):
+        return self.book[8 + self.seqs + self.pages:].view(self.seqs, self.max_pages)
+
+    def _scratch(self, need, kind, ws, stream):
+        """The caller's workspace or the pool's own, kept between calls (one for the attention, one for the pages: a pool works on one stream at a time)."""
+        if ws is not None:
+            return _given(ws)
+        own, at = self._ws.get(kind, (None, None))
+        raw = _raw_stream(stream)
+        if own is None or own.numel() < need + 256:
+            own, at = _new((need + 256,), torch.uint8, self.book.device, stream), raw
+            self._ws[kind] = own, at
+        elif raw != at:                    # the allocator must not give its memory away while another stream works with it
+            own.record_stream(torch.cuda.current_stream() if stream is None else stream)
+        return _given(own)
+
+    def _pages_ws(self, n, ws, stream):
+        return self._scratch(lib().spectre_kv_workspace_bytes(self._ref, n), "pages", ws, stream)
+
+    def reserve(self, seqs, add, ws=None, stream=None):
+        """Sequence seqs[i] grows by add[i] tokens (int32 on the device); room that is missing is reported in `status`, and then nothing changes."""
+        n = seqs.numel()
+        _check(lib().spectre_kv_reserve(self._ref, _ints(seqs, "seqs"), _ints(add, "add", n), n, *self._pages_ws(n, ws, stream), _raw_stream(stream)))
+
+    def fork(self, src, dst, ws=None, stream=None):
+        """The empty sequences dst[i] become what src[i] are: full pages shared, the last one copied."""
+        n = src.numel()
+        _check(lib().spectre_kv_fork(self._ref, _ints(src, "src"), _ints(dst, "dst", n), n, *self._pages_ws(n, ws, stream), _raw_stream(stream)))
+
+    def free(self, seqs, stream=None):
+        """The sequences end; pages that nobody else uses are free."""
+        _check(lib().spectre_kv_free(self._ref, _ints(seqs, "seqs"), seqs.numel(), _raw_stream(stream)))
+
+    def compact(self, ws=None, stream=None):
+        """Pages in use move to the front of the pool; status[2] = how many there are."""
+        _check(lib().spectre_kv_compact(self._ref, *self._pages_ws(0, ws, stream), _raw_stream(stream)))
+
+    def copy(self, src, dst, stream=None):
+        """Contents of page src[i] of every layer to page dst[i]."""
+        n = src.numel()
+        _check(lib().spectre_kv_copy(self._ref, _ints(src, "src"), _ints(dst, "dst", n), n, _raw_stream(stream)))
+
+    def append(self, layer, q, k, v, start, seqs=None, rope=None, wq=None, wk=None, eps=1e-6, q_out=None, stream=None):
+        """Norm and rotation of the new tokens' heads; keys and values go into the pages of `layer`, queries are returned.  q [T,H,d], k, v [T,Hkv,d] of the
+        pool's dtype; start int32 [B+1]: first token of each sequence; seqs int32 [B]: their rows of the table (None: 0 .. B-1).  The new tokens are
+        the last ones of their sequences: reserve() comes first, once for all layers."""
+        T, H, d = q.shape
+        B = start.numel() - 1
+        qa, qs = _rows(q, "q", self.dtype)
+        ka, ks = _rows(k, "k", self.dtype, T, self.Hkv)
+        va, vs = _rows(v, "v", self.dtype, T, self.Hkv)
+        if d != self.d or k.shape[2] != d or v.shape[2] != d:
+            raise ValueError(f"q, k and v must have d = {self.d}")
+        P = _heads(d, rope, wq, wk, eps)
+        if q_out is None:
+            q_out = _new((T, H, d), q.dtype, q.device, stream)
+        _same(q_out, q, "q_out")
+        _check(lib().spectre_kv_append(self._ref, layer, ctypes.byref(P), qa, qs, ka, ks, va, vs, _ints(start, "start"),
+                                       None if seqs is None else _ints(seqs, "seqs", B), B, T, H, _ptr(q_out, "q_out"), _raw_stream(stream)))
+        return q_out
+
+    def attend_workspace_bytes(self, B, T, H, max_new, max_len=None, window=0):
+        return int(lib().spectre_kv_attend_workspace_bytes(self._ref, B, T, H, max_new, max_len or self.max_pages * self.page, window))
+
+    def attend(self, layer, q, start, seqs=None, max_new=None, max_len=None, scale=None, window=0, out=None, lse=None, want_lse=False, ws=None,
+               stream=None):
+        """Attention of the new tokens (append has written their keys and values) over their sequences' pages (spectre_kv_attend).
+        max_new, max_len: bounds of the sequences' new tokens and lengths (None: T, and the table's width); scale None: d^-1/2; window > 0: each
+        query sees that many keys, its own the last.  Returns out [T,H,d], with want_lse or a tensor `lse` also lse float32 [T,H]."""
+        T, H, d = q.shape
+        B = start.numel() - 1
+        qa, qs = _rows(q, "q", self.dtype)
+        if d != self.d:
+            raise ValueError(f"q must have d = {self.d}")
+        if max_new is None:
+            max_new = max(T, 1)
+        if max_len is None:
+            max_len = self.max_pages * self.page
+        if out is None:
+            out = _new((T, H, d), q.dtype, q.device, stream)
+        _same(out, q, "out")
+        if lse is None and want_lse:
+            lse = _new((T, H), torch.float32, q.device, stream)
+        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (T, H)):
+            raise ValueError("lse must be float32 [T, H]")
+        need = 0 if ws is not None else lib().spectre_kv_attend_workspace_bytes(self._ref, B, T, H, max_new, max_len, window)
+        at, have = self._scratch(need, "attend", ws, stream)
+        _check(lib().spectre_kv_attend(self._ref, layer, qa, qs, _ints(start, "start"), None if seqs is None else _ints(seqs, "seqs", B), B, T, H, max_new,
+                                       max_len, 1.0 / d ** 0.5 if scale is None else scale, window, _ptr(out, "out"),
+                                       None if lse is None else _ptr(lse, "lse"), at, have, _raw_stream(stream)))
+        return (out, lse) if lse is not None else out

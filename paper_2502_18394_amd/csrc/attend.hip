@@ -1,0 +1,692 @@
+// Attention of each sequence's new tokens over its pages.
+//
+// Query i of n new ones, in a sequence of m tokens with them, stands at p = m - n + i and sees the keys j <= p (with a window: j > p - window):
+// o = sum_j e^(s_j - M) v_j / sum_j e^(s_j - M), s_j = scale q . k_j, lse = M + log sum.  One pass over the keys with a running maximum and sum,
+// both in fp32, as are scores and outputs until they are stored.
+//
+// The heads that share a key head and the new tokens are one list of rows, (token, head of the group): they read the same keys.  All products are
+// formed transposed, S^T = K Q^T and O^T = V^T P^T, so that a row of scores lies in one lane (and its mate 32 or 16 lanes on): the softmax needs almost no
+// exchange, and what a lane holds of P^T after S^T is what the second product wants of it, without a move.  For that the keys of a bf16 tile are
+// given to the matrix instruction in an order in which each lane ends up with runs of 8.
+// Probabilities go to the matrix cores in the type of the rows: bf16 rounds each to half a step of 2^-8, errors of independent signs that average
+// out like the values they weigh, so outputs are as far off as by their own rounding; the sum in the denominator is of the unrounded ones.
+// Keys that nobody of the row's may see take no part whatever lies there: their scores are replaced, not shifted, and values that are infinite or NaN are
+// taken out of the tiles where rows see different keys and added for the rows that do see them.
+#include <math.h>
+
+#include <algorithm>
+
+#include "common.h"
+#include "paged.h"
+
+namespace spectre {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+
+constexpr float kLog2E = 1.4426950408889634f;
+constexpr int kTileRows = 128;                     // rows a workgroup, 32 a wave
+// The maximum follows only when a score is this far above it, in powers of two: until then probabilities grow to 2^8, which costs neither fp32 nor bf16
+// any digit, and the outputs need not be rescaled.
+constexpr float kLag = 8.f;
+
+struct AttendK {
+    KvView kv;
+    AttendArgs a;
+    int G, few_rows, splits, tiles, slots;         // slots: parts that a row has room for
+    float c;                                       // scale * log2(e)
+    float *part;                                   // [T * H][slots][d]
+    float2 *stat;                                  // [T * H][slots]: maximum in powers of two, sum
+};
+
+struct Seq {
+    int from, n, m, row;                           // first new token, new tokens, tokens, row of the table
+};
+__device__ __forceinline__ Seq sequence(const AttendK &k, int b) {
+    Seq s;
+    s.from = k.a.start[b];
+    const int to = min(k.a.start[b + 1], k.a.T);
+    s.n = s.from >= 0 ? max(to - s.from, 0) : 0;
+    s.row = k.a.seqs ? k.a.seqs[b] : b;
+    s.m = 0;
+    if ((unsigned)s.row < (unsigned)k.kv.S) s.m = min(max(k.kv.lens[s.row], 0), k.kv.M << k.kv.page_log);
+    else s.row = 0;
+    return s;
+}
+
+struct Bf16Mma {
+    static constexpr int E = 8, kBytes = 2;
+    static constexpr int kTileKeys = 64, kStepKeys = 32;
+    typedef uint16_t elem_t;
+    // 32 rows of A (keys, channels) x 32 columns: one group of 8 of the contraction a lane
+    __device__ static __forceinline__ void mma32(f32x16_t &acc, uint4 a, uint4 b) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+    }
+    __device__ static __forceinline__ void mma16(f32x4_t &acc, uint4 a, uint4 b) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+    }
+    // key of row r of a 32-row tile, and of accumulator r in half h of the wave: runs of 8 a lane
+    __device__ static __forceinline__ int key_of_row(int r) { return 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3); }
+    __device__ static __forceinline__ constexpr int key_of_acc(int r) { return 16 * (r >> 3) + (r & 7); }   // + 8 h
+    static constexpr int kHalf = 8;
+    static constexpr int kChunks = 2;                                          // groups of P a lane holds of 32 keys
+    __device__ static __forceinline__ uint4 pack(const float *p) {
+        return make_uint4(IoBf16::pack(make_float2(p[0], p[1])), IoBf16::pack(make_float2(p[2], p[3])), IoBf16::pack(make_float2(p[4], p[5])),
+                          IoBf16::pack(make_float2(p[6], p[7])));
+    }
+    __device__ static __forceinline__ bool finite(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (w & 0x7f800000u) != 0x7f800000u; }
+    __device__ static __forceinline__ uint32_t finite_only(uint32_t w) {
+        return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
+    }
+    __device__ static __forceinline__ float value(elem_t e) { return __uint_as_float((uint32_t)e << 16); }
+    // the first `n` elements of a group, zeros behind
+    __device__ static __forceinline__ uint32_t keep(uint32_t w, int i, int n) { return 2 * i + 1 < n ? w : 2 * i < n ? w & 0xffffu : 0u; }
+};
+struct F32Mma {
+    static constexpr int E = 4, kBytes = 4;
+    static constexpr int kTileKeys = 32, kStepKeys = 16;
+    typedef uint32_t elem_t;
+    __device__ static __forceinline__ void mma32(f32x16_t &acc, uint4 a, uint4 b) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+    }
+    __device__ static __forceinline__ void mma16(f32x4_t &acc, uint4 a, uint4 b) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+    }
+    __device__ static __forceinline__ int key_of_row(int r) { return r; }
+    __device__ static __forceinline__ constexpr int key_of_acc(int r) { return 8 * (r >> 2) + (r & 3); }    // + 4 h
+    static constexpr int kHalf = 4;
+    static constexpr int kChunks = 4;
+    __device__ static __forceinline__ uint4 pack(const float *p) {
+        return make_uint4(__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3]));
+    }
+    __device__ static __forceinline__ bool finite(uint32_t w) { return (w & 0x7f800000u) != 0x7f800000u; }
+    __device__ static __forceinline__ uint32_t finite_only(uint32_t w) { return finite(w) ? w : 0u; }
+    __device__ static __forceinline__ float value(elem_t e) { return __uint_as_float(e); }
+    __device__ static __forceinline__ uint32_t keep(uint32_t w, int i, int n) { return i < n ? w : 0u; }
+};
+
+template <typename IO>
+__device__ __forceinline__ uint4 keep_first(uint4 g, int n) {
+    return make_uint4(IO::keep(g.x, 0, n), IO::keep(g.y, 1, n), IO::keep(g.z, 2, n), IO::keep(g.w, 3, n));
+}
+template <typename IO>
+__device__ __forceinline__ bool all_finite(uint4 g) { return IO::finite(g.x) && IO::finite(g.y) && IO::finite(g.z) && IO::finite(g.w); }
+template <typename IO>
+__device__ __forceinline__ uint4 finite_only(uint4 g) {
+    return make_uint4(IO::finite_only(g.x), IO::finite_only(g.y), IO::finite_only(g.z), IO::finite_only(g.w));
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// One row's statistics after scores whose largest is mx: true in any lane asks for a rescale by the factor that follow() returns.
+__device__ __forceinline__ bool lags(float mx, float top, float lag) { return mx > top + lag; }
+__device__ __forceinline__ float follow(float mx, float c, float *top) {
+    const float next = fmaxf(*top, mx), f = next == *top ? 1.f : exp2_fast((*top - next) * c);
+    *top = next;
+    return f;
+}
+// -top * c, 0 while nothing has been seen (then every score is -inf, and 2^(-inf) = 0)
+__device__ __forceinline__ float shift_of(float top, float c) { return top == -INFINITY ? 0.f : -top * c; }
+
+// Values that are not finite, of keys base .. base + count - 1 of head h, for a row at `pos` whose lane holds channels channel(r), r < N.  The rows' finite
+// parts have been added; a weight is above zero for every key a row sees, so what is added is the value itself.
+template <typename IO, int D, int N, typename Channel, typename Add>
+__device__ __forceinline__ void add_not_finite(const KvView &kv, const Seq &s, int h, int base, int count, int pos, int from, Channel channel, Add add) {
+    typedef typename IO::elem_t elem_t;
+    const int *table = kv.table + (long long)s.row * kv.M;
+#pragma unroll 1
+    for (int key = base; key < base + count && key < s.m; ++key) {
+        const int page = table[key >> kv.page_log], slot = key & ((1 << kv.page_log) - 1);
+        if ((unsigned)page >= (unsigned)kv.P || key > pos || key <= from) continue;
+        const elem_t *v = reinterpret_cast<const elem_t *>(kv.v) + ((((long long)page * kv.Hkv + h) << kv.page_log) + slot / IO::E * IO::E) * D + slot % IO::E;
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+            const float x = IO::value(v[channel(r) * IO::E]);
+            if (!isfinite(x)) add(r, x);
+        }
+    }
+}
+
+template <typename IO>
+__device__ __forceinline__ void store4(void *out, long long at, float4 x) {
+    if constexpr (IO::kBytes == 2) {
+        uint2 w;
+        w.x = IoBf16::pack(make_float2(x.x, x.y));
+        w.y = IoBf16::pack(make_float2(x.z, x.w));
+        *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(out) + at) = w;
+    } else {
+        *reinterpret_cast<float4 *>(reinterpret_cast<float *>(out) + at) = x;
+    }
+}
+
+__device__ __forceinline__ float lse_of(float top2, float sum) { return sum == 0.f ? -INFINITY : (top2 + log2f(sum)) * 0.69314718055994531f; }
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+
+// ---------------------------------------------------------------- many rows: 128 of a key head a workgroup, tiles of keys through LDS
+template <typename IO, int D>
+__global__ __launch_bounds__(256, 2) void k_attend_tile(AttendK k) {
+    constexpr int E = IO::E, KT = IO::kTileKeys, NK = KT / 32, GROUPS = KT * D / E, PER = GROUPS / 256, QG = D / (2 * E), DT = D / 32;
+    __shared__ uint4 sk[2][GROUPS], sv[2][GROUPS];
+    __shared__ int odd[2];                          // the last tile whose values were not all finite
+    const KvView &kv = k.kv;
+    const int pairs = kv.Hkv * k.a.B, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+    const int h = pair % kv.Hkv, split = rest % k.splits, tile = k.tiles - 1 - rest / k.splits;   // long rows first
+    const Seq s = sequence(k, pair / kv.Hkv);
+    const int rows = s.n * k.G, r0 = tile * kTileRows;
+    if (rows <= k.few_rows || r0 >= rows) return;
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int r = min(r0 + 32 * wave + (lane & 31), rows - 1), token = r / k.G, head = h * k.G + (r - token * k.G);
+    const bool mine = r0 + 32 * wave + (lane & 31) < rows, busy = r0 + 32 * wave < rows;
+    const int p0 = s.m - s.n, pos = p0 + token;
+    const int from = k.a.window ? pos - k.a.window : -1;                      // keys above it
+    // what all rows of the workgroup, and of the wave, see
+    const int first_pos = p0 + r0 / k.G, last_pos = p0 + min(r0 + kTileRows - 1, rows - 1) / k.G;
+    const int wave_first = p0 + min(r0 + 32 * wave, rows - 1) / k.G, wave_last = p0 + min(r0 + 32 * wave + 31, rows - 1) / k.G;
+    int t_lo = k.a.window ? max(0, first_pos - k.a.window + 1) / KT : 0, t_hi = last_pos >= 0 ? last_pos / KT + 1 : 0;
+    if (k.splits > 1) {
+        const int per = (max(t_hi - t_lo, 0) + k.splits - 1) / k.splits;
+        t_lo += split * per;
+        t_hi = min(t_hi, t_lo + per);
+    }
+
+    uint4 q[QG];
+    {
+        const char *base = reinterpret_cast<const char *>(k.a.q) + ((s.from + token) * k.a.q_stride + head * D) * IO::kBytes;
+#pragma unroll
+        for (int i = 0; i < QG; ++i) q[i] = reinterpret_cast<const uint4 *>(base)[2 * i + half];
+    }
+    f32x16_t o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    float top = -INFINITY, sum = 0.f;
+    const float lag = kLag / k.c;
+
+    const int mask = (1 << kv.page_log) - 1;
+    const int *table = kv.table + (long long)s.row * kv.M;
+    // page of this lane's key of tile t (every wave has all keys of a tile), -1 where there is none
+    auto page_of = [&](int t) {
+        const int key = t * KT + (lane & (KT - 1));
+        int p = -1;
+        if (t < t_hi && key < s.m) p = table[key >> kv.page_log];
+        return (unsigned)p < (unsigned)kv.P ? p : -1;
+    };
+    uint4 kr[PER], vr[PER];
+    auto request = [&](int t, int page) {
+        const int slot = (t * KT + (lane & (KT - 1))) & mask;
+        const uint4 *K = reinterpret_cast<const uint4 *>(kv.k), *V = reinterpret_cast<const uint4 *>(kv.v);
+        const long long block = ((long long)page * kv.Hkv + h) * (D / E);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            kr[i] = make_uint4(0, 0, 0, 0);
+            if (page >= 0) kr[i] = K[((block + (threadIdx.x + 256 * i) / KT) << kv.page_log) + slot];
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int kg = (64 * wave + 256 * i) / D, vp = __builtin_amdgcn_readlane(page, kg * E);
+            vr[i] = make_uint4(0, 0, 0, 0);
+            if (vp >= 0) vr[i] = V[(((long long)vp * kv.Hkv + h) * (D / E) << kv.page_log) + (((t * KT + kg * E) & mask) / E) * D + (threadIdx.x + 256 * i) % D];
+        }
+    };
+    if (threadIdx.x < 2) odd[threadIdx.x] = -1;
+    __syncthreads();
+    int page = page_of(t_lo), next = page_of(t_lo + 1);
+    if (t_lo < t_hi) request(t_lo, page);
+    const int krow = IO::key_of_row(lane & 31);
+
+    for (int t = t_lo, buf = 0; t < t_hi; ++t, buf ^= 1) {
+        const unsigned long long there = __ballot(page >= 0);      // bit = key of the tile (fp32: twice 32 keys)
+        const bool edge = there != ~0ull || t * KT + KT - 1 > first_pos || t * KT <= last_pos - (k.a.window ? k.a.window : last_pos + 1);
+        if (edge) {                                                 // values of no one's keys, and those that are not finite
+            bool fine = true;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int have = s.m - (t * KT + (64 * wave + 256 * i) / D * E);
+                if (have < E) vr[i] = keep_first<IO>(vr[i], have);
+                if (!all_finite<IO>(vr[i])) {
+                    fine = false;
+                    vr[i] = finite_only<IO>(vr[i]);
+                }
+            }
+            if (!fine) odd[buf] = t;
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            sk[buf][threadIdx.x + 256 * i] = kr[i];
+            sv[buf][threadIdx.x + 256 * i] = vr[i];
+        }
+        page = next;
+        if (t + 1 < t_hi) {
+            request(t + 1, page);
+            next = page_of(t + 2);
+        }
+        __syncthreads();
+        if (!busy || t * KT > wave_last) continue;
+
+        f32x16_t sc[NK];
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[n][i] = 0.f;
+#pragma unroll
+            for (int i = 0; i < QG; ++i) IO::mma32(sc[n], sk[buf][(2 * i + half) * KT + 32 * n + krow], q[i]);
+        }
+        const bool some = there != ~0ull || t * KT + KT - 1 > wave_first || t * KT <= wave_last - (k.a.window ? k.a.window : wave_last + 1);
+        if (some) {
+            const unsigned long long mates = there >> (IO::kHalf * half);
+#pragma unroll
+            for (int n = 0; n < NK; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int at = 32 * n + IO::key_of_acc(i), key = t * KT + at + IO::kHalf * half;
+                    if (!((mates >> at) & 1) || key > pos || key <= from) sc[n][i] = -INFINITY;
+                }
+        }
+        float mx = sc[0][0];
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[n][i]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        if (__ballot(lags(mx, top, lag))) {
+            const float f = follow(mx, k.c, &top);
+            sum *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        }
+        const float shift = shift_of(top, k.c);
+        float p[NK * 16];
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                p[16 * n + i] = exp2_fast(fmaf(sc[n][i], k.c, shift));
+                sum += p[16 * n + i];
+            }
+#pragma unroll
+        for (int g = 0; g < NK * IO::kChunks; ++g) {
+            const uint4 pg = IO::pack(p + g * E);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) IO::mma32(o[d], sv[buf][(2 * g + half) * D + 32 * d + (lane & 31)], pg);
+        }
+        if (odd[buf] == t) {
+            add_not_finite<IO, D, 16 * DT>(kv, s, h, t * KT, KT, pos, from, [half](int i) { return 32 * (i / 16) + 8 * ((i % 16) / 4) + 4 * half + i % 4; },
+                                           [&](int i, float x) { o[i / 16][i % 16] += x; });
+        }
+    }
+    if (!mine) return;
+    sum += __shfl_xor(sum, 32, 64);
+    const long long at = (long long)(s.from + token) * k.a.H + head;
+    const float top2 = top * k.c;
+    if (k.splits > 1) {
+        if (half == 0) k.stat[at * k.slots + split] = make_float2(top2, sum);
+        if (sum == 0.f) return;
+        float *to = k.part + (at * k.slots + split) * D;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<float4 *>(to + 32 * d + 8 * i + 4 * half) = make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
+        return;
+    }
+    const float inv = inverse(sum);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            store4<IO>(k.a.out, at * D + 32 * d + 8 * i + 4 * half, make_float4(o[d][4 * i] * inv, o[d][4 * i + 1] * inv, o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv));
+    if (k.a.lse && half == 0) k.a.lse[at] = lse_of(top2, sum);
+}
+
+// ---------------------------------------------------------------- few rows: up to 16 R of a key head, keys split over waves and workgroups
+constexpr int kSection = 1024;                     // page numbers in LDS at a time
+
+template <typename IO, int D, int R>
+__global__ __launch_bounds__(256, R * D == 64 ? 3 : R * D == 128 ? 2 : 1) void k_attend_few(AttendK k) {
+    constexpr int E = IO::E, SK = IO::kStepKeys, KTILES = SK / 16, QG = D / (4 * E), DT = D / 16, SD = (R == 2 && D == 128) ? 64 : D, PAD = SD + 4;
+    __shared__ int pages[kSection + 2];
+    __shared__ float tops[4][16 * R], sums[4][16 * R];
+    __shared__ float so[4][16 * R][PAD];
+    const KvView &kv = k.kv;
+    const int pairs = kv.Hkv * k.a.B, pair = blockIdx.x % pairs, split = blockIdx.x / pairs, h = pair % kv.Hkv;
+    const Seq s = sequence(k, pair / kv.Hkv);
+    const int rows = s.n * k.G;
+    if (rows == 0 || rows > k.few_rows) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
+    const int p0 = s.m - s.n, mask = (1 << kv.page_log) - 1;
+    int pos[R], from[R];
+    uint4 q[R][QG];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int r = min(16 * i + col, rows - 1), token = r / k.G, head = h * k.G + (r - token * k.G);
+        pos[i] = p0 + token;
+        from[i] = k.a.window ? pos[i] - k.a.window : -1;
+        const char *base = reinterpret_cast<const char *>(k.a.q) + ((s.from + token) * k.a.q_stride + head * D) * IO::kBytes;
+#pragma unroll
+        for (int j = 0; j < QG; ++j) q[i][j] = reinterpret_cast<const uint4 *>(base)[4 * j + quarter];
+    }
+    // this workgroup's keys: whole steps of all waves
+    const int lo = k.a.window ? max(0, p0 - k.a.window + 1) & ~63 : 0, hi = s.m;
+    const int chunk = ((max(hi - lo, 0) + k.splits - 1) / k.splits + 4 * SK - 1) / (4 * SK) * (4 * SK);
+    const int begin = min(lo + (long long)split * chunk, (long long)hi), end = min(hi, begin + chunk);
+    const int all_from = k.a.window ? p0 + s.n - 1 - k.a.window : -1;         // every row sees the keys above it ...
+    const int all_pos = p0;                                                   // ... up to this one
+
+    f32x4_t o[R][DT];
+    float top[R], sum[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        top[i] = -INFINITY;
+        sum[i] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    const float lag = kLag / k.c;
+    const uint4 *K = reinterpret_cast<const uint4 *>(kv.k), *V = reinterpret_cast<const uint4 *>(kv.v);
+    const int koff = E == 8 ? 8 * (col >> 2) + (col & 3) : col;               // this lane's key of a step (bf16: and the one 4 on)
+
+    struct Step {
+        uint4 k[KTILES * QG], v[DT];
+        int kpage, vpage;
+    };
+    // sections of keys whose page numbers fit LDS
+    const int keys_a_section = kSection << kv.page_log;
+    for (int sec = begin; sec < end; sec += keys_a_section) {
+        const int sec_end = min(end, sec + keys_a_section), first = sec >> kv.page_log, count = ((sec_end - 1) >> kv.page_log) - first + 1;
+        __syncthreads();
+        for (int i = threadIdx.x; i < count; i += 256) pages[i] = kv.table[(long long)s.row * kv.M + first + i];
+        __syncthreads();
+        auto page_at = [&](int key) {
+            const int p = key < sec_end ? pages[(key >> kv.page_log) - first] : -1;
+            return (unsigned)p < (unsigned)kv.P ? p : -1;
+        };
+        auto request = [&](Step &x, int base) {
+            const int key = base + koff, vkey = base + E * quarter;
+            x.kpage = page_at(base + (E == 8 ? 8 * (col >> 2) : col));        // keys at and behind the end lie in its page, or in none
+            x.vpage = page_at(vkey);
+            const long long kb = ((long long)x.kpage * kv.Hkv + h) * (D / E);
+            const uint4 *vb = V + (((long long)x.vpage * kv.Hkv + h) * (D / E) << kv.page_log) + ((vkey & mask) / E) * D + col;
+#pragma unroll
+            for (int t = 0; t < KTILES; ++t)
+#pragma unroll
+                for (int j = 0; j < QG; ++j) {
+                    x.k[t * QG + j] = make_uint4(0, 0, 0, 0);
+                    if (x.kpage >= 0) x.k[t * QG + j] = K[((kb + 4 * j + quarter) << kv.page_log) + ((key + 4 * t) & mask)];
+                }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                x.v[d] = make_uint4(0, 0, 0, 0);
+                if (x.vpage >= 0) x.v[d] = vb[16 * d];
+            }
+        };
+        auto work = [&](Step &x, int base) {
+            const bool gone = __ballot(x.vpage < 0) != 0;                     // lanes' value pages are all pages of the step
+            const bool edge = gone || base + SK - 1 > all_pos || base <= all_from;
+            bool odd = false;
+            if (edge) {
+                const int have = s.m - (base + E * quarter);
+                bool fine = true;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    if (have < E) x.v[d] = keep_first<IO>(x.v[d], have);
+                    if (!all_finite<IO>(x.v[d])) {
+                        fine = false;
+                        x.v[d] = finite_only<IO>(x.v[d]);
+                    }
+                }
+                odd = __ballot(!fine) != 0;
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                f32x4_t sc[KTILES];
+#pragma unroll
+                for (int t = 0; t < KTILES; ++t) {
+                    sc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < QG; ++j) IO::mma16(sc[t], x.k[t * QG + j], q[i][j]);
+                }
+                // lane: keys base + E * quarter + 4 t + e, all of one page (x.vpage)
+                if (edge) {
+#pragma unroll
+                    for (int t = 0; t < KTILES; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int key = base + E * quarter + 4 * t + e;
+                            if (x.vpage < 0 || key > pos[i] || key <= from[i]) sc[t][e] = -INFINITY;
+                        }
+                }
+                float mx = sc[0][0];
+#pragma unroll
+                for (int t = 0; t < KTILES; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[t][e]);
+                mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                if (__ballot(lags(mx, top[i], lag))) {
+                    const float f = follow(mx, k.c, &top[i]);
+                    sum[i] *= f;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[i][d] *= f;
+                }
+                const float shift = shift_of(top[i], k.c);
+                float p[4 * KTILES];
+#pragma unroll
+                for (int t = 0; t < KTILES; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[4 * t + e] = exp2_fast(fmaf(sc[t][e], k.c, shift));
+                        sum[i] += p[4 * t + e];
+                    }
+                const uint4 pg = IO::pack(p);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) IO::mma16(o[i][d], x.v[d], pg);
+                if (odd) {
+                    add_not_finite<IO, D, 4 * DT>(kv, s, h, base, SK, pos[i], from[i], [quarter](int n) { return 16 * (n / 4) + 4 * quarter + n % 4; },
+                                                  [&](int n, float y) { o[i][n / 4][n % 4] += y; });
+                }
+            }
+        };
+        // two steps' registers in turn: one on its way from memory while the other is worked on
+        Step a, b;
+        int base = sec + SK * wave;
+        if (base < sec_end) request(a, base);
+        for (; base < sec_end; base += 8 * SK) {
+            const bool second = base + 4 * SK < sec_end;
+            if (second) request(b, base + 4 * SK);
+            work(a, base);
+            if (base + 8 * SK < sec_end) request(a, base + 8 * SK);
+            if (second) work(b, base + 4 * SK);
+        }
+    }
+
+    // the waves' results, joined in a fixed order
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        sum[i] += __shfl_xor(sum[i], 16, 64);
+        sum[i] += __shfl_xor(sum[i], 32, 64);
+        if (quarter == 0) {
+            tops[wave][16 * i + col] = top[i];
+            sums[wave][16 * i + col] = sum[i];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        float best = tops[0][16 * i + col];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) best = fmaxf(best, tops[w][16 * i + col]);
+        const float f = top[i] == best ? 1.f : exp2_fast((top[i] - best) * k.c);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[i][d] *= f;
+    }
+    for (int d0 = 0; d0 < D; d0 += SD) {
+        if (d0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+                if (16 * d >= d0 && 16 * d < d0 + SD) *reinterpret_cast<f32x4_t *>(&so[wave][16 * i + col][16 * d - d0 + 4 * quarter]) = o[i][d];
+        __syncthreads();
+        for (int x = threadIdx.x; x < rows * (SD / 4); x += 256) {
+            const int r = x / (SD / 4), c = 4 * (x % (SD / 4));
+            float best = -INFINITY, total = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) best = fmaxf(best, tops[w][r]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) total += sums[w][r] * (tops[w][r] == best ? 1.f : exp2_fast((tops[w][r] - best) * k.c));
+            f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) y += *reinterpret_cast<const f32x4_t *>(&so[w][r][c]);
+            const int token = r / k.G, head = h * k.G + (r - token * k.G);
+            const long long at = (long long)(s.from + token) * k.a.H + head;
+            if (k.splits > 1) {
+                *reinterpret_cast<f32x4_t *>(k.part + (at * k.slots + split) * D + d0 + c) = y;
+                if (d0 + c == 0) k.stat[at * k.slots + split] = make_float2(best * k.c, total);
+            } else {
+                const float inv = inverse(total);
+                store4<IO>(k.a.out, at * D + d0 + c, make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv));
+                if (k.a.lse && d0 + c == 0) k.a.lse[at] = lse_of(best * k.c, total);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- splits joined: a wave a row
+template <typename IO, int D>
+__global__ __launch_bounds__(256) void k_attend_join(AttendK k, int few_splits, int tile_splits) {
+    constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (row >= (long long)k.a.T * k.a.H) return;
+    const int t = (int)(row / k.a.H);
+    int lo = 0, hi = k.a.B;                        // the sequence with start <= t < the next one's
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (k.a.start[mid] <= t) lo = mid;
+        else hi = mid;
+    }
+    if (t < k.a.start[lo] || t >= k.a.start[lo + 1]) return;
+    const int n = k.a.start[lo + 1] - k.a.start[lo], splits = (long long)n * k.G <= k.few_rows ? few_splits : tile_splits;
+    if (splits <= 1) return;
+    const float2 *stat = k.stat + row * k.slots;
+    float best = -INFINITY;
+    for (int s = lane; s < splits; s += 64) best = fmaxf(best, stat[s].y == 0.f ? -INFINITY : stat[s].x);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) best = fmaxf(best, __shfl_xor(best, m, 64));
+    const int g = lane / LANES, c = lane % LANES;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+    float total = 0.f;
+    const float *part = k.part + row * k.slots * D + 4 * c;
+#pragma unroll 4
+    for (int s = g; s < splits; s += AT_ONCE) {
+        const float2 x = stat[s];
+        if (x.y == 0.f) continue;                  // nothing seen, nothing written
+        const float f = x.x == best ? 1.f : exp2_fast(x.x - best);
+        total += f * x.y;
+        o += f * *reinterpret_cast<const f32x4_t *>(part + (long long)s * D);
+    }
+#pragma unroll
+    for (int m = LANES; m < 64; m <<= 1) {
+        total += __shfl_xor(total, m, 64);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m, 64);
+    }
+    if (g) return;
+    const float inv = inverse(total);
+    store4<IO>(k.a.out, row * D + 4 * c, make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv));
+    if (k.a.lse && c == 0) k.a.lse[row] = lse_of(best, total);
+}
+
+}  // namespace
+
+hipError_t load_kernels_attend() {
+    hipFuncAttributes a;
+    return hipFuncGetAttributes(&a, reinterpret_cast<const void *>(k_attend_join<Bf16Mma, 64>));
+}
+
+AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new, int max_len, int window) {
+    AttendPlan p{};
+    const int G = H / Hkv;
+    const long long rows = (long long)max_new * G;
+    const bool even = T == (long long)B * max_new;                 // every sequence has max_new tokens
+    const long long len = window ? std::min<long long>(max_len, (long long)window + max_new) : max_len;
+    p.few = rows <= 32 || (!even && G <= 16);
+    p.tile = rows > 32;
+    p.few_rows = !p.few ? 0 : p.tile ? 16 : (int)rows;
+    p.tiles = (int)((rows + kTileRows - 1) / kTileRows);
+    p.few_splits = p.tile_splits = 1;
+    const long long pairs = (long long)B * Hkv;
+    if (p.few) {
+        long long s = std::max((1024 + pairs - 1) / pairs, (len + 2047) / 2048);
+        s = std::min(s, (len + 127) / 128);
+        p.few_splits = (int)std::max(1ll, std::min(s, 256ll));
+    }
+    if (p.tile) {
+        const long long groups = Hkv * (even ? (long long)B * p.tiles : std::min<long long>((long long)B * p.tiles, ((long long)T * G + kTileRows - 1) / kTileRows));
+        long long s = std::min(512 / groups, len / 256);
+        p.tile_splits = (int)std::max(1ll, std::min(s, 64ll));
+    }
+    const int most = std::max(p.few_splits, p.tile_splits);
+    if (most > 1) p.partial_bytes = (size_t)T * H * most * ((size_t)d * 4 + 8);
+    return p;
+}
+
+hipError_t launch_attend(const KvView &kv, int d, int io, const AttendArgs &a, const AttendPlan &p, void *ws, hipStream_t st) {
+    AttendK k;
+    k.kv = kv;
+    k.a = a;
+    k.G = a.H / kv.Hkv;
+    k.few_rows = p.few_rows;
+    k.tiles = p.tiles;
+    k.c = a.scale * kLog2E;
+    const size_t most = std::max(p.few_splits, p.tile_splits);
+    k.slots = (int)most;
+    k.part = (float *)ws;
+    k.stat = (float2 *)((char *)ws + (size_t)a.T * a.H * most * d * 4);
+    const int pairs = a.B * kv.Hkv;
+#define SPECTRE_ATTEND_DISPATCH(CALL)                                 \
+    if (io == SPECTRE_BF16 && d == 64) { CALL(Bf16Mma, 64); }         \
+    else if (io == SPECTRE_BF16) { CALL(Bf16Mma, 128); }              \
+    else if (d == 64) { CALL(F32Mma, 64); }                           \
+    else { CALL(F32Mma, 128); }
+    if (p.few) {
+        k.splits = p.few_splits;
+        const int blocks = pairs * p.few_splits;
+#define CALL(IO, D)                                                                        \
+    if (p.few_rows <= 16) k_attend_few<IO, D, 1><<<blocks, 256, 0, st>>>(k);               \
+    else k_attend_few<IO, D, 2><<<blocks, 256, 0, st>>>(k)
+        SPECTRE_ATTEND_DISPATCH(CALL)
+#undef CALL
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (p.tile) {
+        k.splits = p.tile_splits;
+        const int blocks = pairs * p.tile_splits * p.tiles;
+#define CALL(IO, D) k_attend_tile<IO, D><<<blocks, 256, 0, st>>>(k)
+        SPECTRE_ATTEND_DISPATCH(CALL)
+#undef CALL
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (p.few_splits > 1 || p.tile_splits > 1) {
+        const long long rows = (long long)a.T * a.H;
+#define CALL(IO, D) k_attend_join<IO, D><<<(int)((rows + 3) / 4), 256, 0, st>>>(k, p.few_splits, p.tile_splits)
+        SPECTRE_ATTEND_DISPATCH(CALL)
+#undef CALL
+    }
+    return hipGetLastError();
+}
+
+}  // namespace spectre

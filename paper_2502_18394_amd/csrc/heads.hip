@@ -1,0 +1,448 @@
+// Norms of query and key heads with the rotation by their position, in one pass: training forms (forward, backward) and the serving form
+// that writes keys and values into their pages.
+//
+// Per row x of d channels: r = (mean x^2 + eps)^-1/2, y = w r x, and each pair (a, b) of y turned by the angle pos * f_i:
+// (a cos - b sin, b cos + a sin).  Backward with g = the output's gradient turned back: g_w = sum g r x over rows, h = g w,
+// g_x = r (h - r x mean(h r x)).  Rows are read and written once; memory bounds the long calls, the launch the short ones.
+#include <math.h>
+
+#include "common.h"
+#include "paged.h"
+
+namespace spectre {
+namespace {
+
+constexpr int kThreads = 256, kTokens = 8;      // tokens a workgroup: one 16-byte group of V pages, two in fp32
+constexpr int kMostHalf = 64;                   // pairs of a row of 128 channels
+
+struct Bf16Group {
+    static constexpr int E = 8;
+    typedef uint16_t elem_t;
+    __device__ static __forceinline__ void unpack(uint4 g, float (&x)[8]) {
+        const uint32_t w[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    __device__ static __forceinline__ uint4 pack(const float (&x)[8]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = IoBf16::pack(make_float2(x[2 * i], x[2 * i + 1]));
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+struct F32Group {
+    static constexpr int E = 4;
+    typedef uint32_t elem_t;
+    __device__ static __forceinline__ void unpack(uint4 g, float (&x)[4]) {
+        x[0] = __uint_as_float(g.x); x[1] = __uint_as_float(g.y); x[2] = __uint_as_float(g.z); x[3] = __uint_as_float(g.w);
+    }
+    __device__ static __forceinline__ uint4 pack(const float (&x)[4]) {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    }
+};
+
+struct HeadParams {
+    const double *freq;
+    const float *wq, *wk;
+    float eps;
+    int half;                       // pairs a row, 0: no rotation
+    int interleaved;
+};
+
+// cos and sin of the angles of a workgroup's tokens, one pair a thread.  The turns pos * f / 2 pi are formed and reduced in 64 bits: a position of
+// 131072 leaves 32 bits with an angle that is wrong in the third digit.
+__device__ __forceinline__ void fill_turns(const HeadParams &P, const int *pos, int count, float2 (*turns)[kMostHalf]) {
+    for (int i = threadIdx.x; i < count * P.half; i += kThreads) {
+        const int t = i / P.half, f = i - t * P.half;
+        double rev = (double)pos[t] * P.freq[f] * 0.15915494309189533577;
+        rev -= rint(rev);
+        float s, c;
+        sincospif((float)(2.0 * rev), &s, &c);
+        turns[t][f] = make_float2(c, s);
+    }
+}
+
+// What a lane needs of its E channels, the same for every row it visits: its pairs' cos and sin (sin negated in the first half of split pairs)
+// and the lane that holds the partners.
+template <typename IO, int D>
+struct Lane {
+    static constexpr int E = IO::E, kLanes = D / E;
+    int lane, partner;              // within a row; the partner's lane in the wave
+    bool turned;
+    float c[E], s[E];
+
+    __device__ __forceinline__ void set(const HeadParams &P, const float2 *turns, float sign) {
+        lane = threadIdx.x % kLanes;
+        const int groups = 2 * P.half / E;             // lanes of a row that hold rotated channels
+        turned = lane < groups;
+        int at = lane;
+        if (!P.interleaved && turned) at = lane < groups / 2 ? lane + groups / 2 : lane - groups / 2;
+        partner = (threadIdx.x & 63) - lane + at;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            c[e] = 1.f; s[e] = 0.f;
+            if (turned) {
+                const int ch = lane * E + e;
+                const int f = P.interleaved ? ch >> 1 : (ch < P.half ? ch : ch - P.half);
+                const float2 t = turns[f];
+                const bool first = P.interleaved ? !(ch & 1) : ch < P.half;
+                c[e] = t.x;
+                s[e] = first ? -sign * t.y : sign * t.y;
+            }
+        }
+    }
+    // y of this lane's channels, z of their partners'
+    __device__ __forceinline__ void turn(const HeadParams &P, const float (&y)[E], const float (&z)[E], float (&o)[E]) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = y[e] * c[e] + (P.interleaved ? y[e ^ 1] : z[e]) * s[e];
+    }
+};
+
+template <int LANES>
+__device__ __forceinline__ float row_sum(float x) {
+#pragma unroll
+    for (int m = 1; m < LANES; m <<= 1) x += __shfl_xor(x, m, 64);
+    return x;
+}
+
+__device__ __forceinline__ uint4 shuffle(uint4 g, int lane) {
+    return make_uint4(__shfl((int)g.x, lane, 64), __shfl((int)g.y, lane, 64), __shfl((int)g.z, lane, 64), __shfl((int)g.w, lane, 64));
+}
+
+// One row's norm and rotation.
+template <typename IO, int D>
+__device__ __forceinline__ uint4 head_row(const HeadParams &P, const Lane<IO, D> &L, const float *w, uint4 raw) {
+    constexpr int E = IO::E;
+    float x[E], z[E], o[E];
+    IO::unpack(raw, x);
+    const uint4 other = (P.half && !P.interleaved) ? shuffle(raw, L.partner) : raw;
+    IO::unpack(other, z);
+    if (w) {
+        float sq = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) sq += x[e] * x[e];
+        const float r = rsqrtf(row_sum<D / E>(sq) * (1.f / D) + P.eps);
+        const int base = L.lane * E, mate = (L.lane + (L.partner - (int)(threadIdx.x & 63))) * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            x[e] = x[e] * r * w[base + e];
+            z[e] = z[e] * r * w[mate + e];
+        }
+    }
+    if (P.half) L.turn(P, x, z, o);
+    else
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = x[e];
+    return IO::pack(o);
+}
+
+// Place of a workgroup's tokens.  Training: kTokens tokens from kTokens * block on.  Serving: the tokens of one sequence that fall into one
+// kTokens-aligned run of cache indexes, so that runs inside a chunk fill whole groups of the V pages.  Sequence b's runs are numbered from
+// start[b] / kTokens + 2 b on: n tokens touch at most n / kTokens + 2 runs, so no two sequences' numbers meet.
+struct Run {
+    int first, count;               // tokens
+    int index;                      // cache index of the first one
+    int seq;                        // its row of the table
+};
+
+__device__ __forceinline__ bool find_run(const KvView &kv, const int *start, const int *seqs, int B, int T, int block, Run *r) {
+    int lo = 0, hi = B;             // the last b with start[b] / kTokens + 2 b <= block
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] / kTokens + 2 * mid <= block) lo = mid;
+        else hi = mid;
+    }
+    const int from = start[lo], to = min(start[lo + 1], T), n = to - from;
+    const int row = seqs ? seqs[lo] : lo;
+    if (from < 0 || n <= 0 || (unsigned)row >= (unsigned)kv.S) return false;
+    const int had = kv.lens[row] - n;          // tokens before the new ones
+    if (had < 0) return false;
+    const int run = block - (from / kTokens + 2 * lo);
+    const int a = max((had / kTokens + run) * kTokens, had), b = min((had / kTokens + run + 1) * kTokens, had + n);
+    if (run < 0 || a >= b) return false;
+    r->first = from + (a - had);
+    r->count = b - a;
+    r->index = a;
+    r->seq = row;
+    return true;
+}
+
+template <typename IO, int D, bool SERVE>
+__global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, const int *positions, uint4 *q_out, uint4 *k_out, KvView kv, const int *start, const int *seqs,
+                                                    int B) {
+    constexpr int E = IO::E, LANES = D / E, ROWS = kThreads / LANES;
+    __shared__ float2 turns[kTokens][kMostHalf];
+    __shared__ int pos[kTokens];
+    __shared__ float weights[2][D];
+    Run run{(int)blockIdx.x * kTokens, min(kTokens, X.T - (int)blockIdx.x * kTokens), 0, 0};
+    if (SERVE && !find_run(kv, start, seqs, B, X.T, blockIdx.x, &run)) return;
+    if (threadIdx.x < run.count) pos[threadIdx.x] = SERVE ? run.index + threadIdx.x : (positions ? positions[run.first + threadIdx.x] : run.first + (int)threadIdx.x);
+    for (int i = threadIdx.x; i < D; i += kThreads) {
+        weights[0][i] = P.wq ? P.wq[i] : 1.f;
+        weights[1][i] = P.wk ? P.wk[i] : 1.f;
+    }
+    __syncthreads();
+    fill_turns(P, pos, run.count, turns);
+    __syncthreads();
+
+    int page = 0, slot = 0;
+    if (SERVE) {                                   // kTokens divides a page: one page a workgroup
+        const int p = run.index >> kv.page_log;
+        page = p < kv.M ? kv.table[(long long)run.seq * kv.M + p] : -1;
+        slot = run.index & ((1 << kv.page_log) - 1);
+    }
+    const bool in_pool = SERVE && (unsigned)page < (unsigned)kv.P;
+
+    // rows in the order (head, token), tokens padded to a power of two, so that a thread stays with one token and one group of channels
+    int tl = 0;
+    while ((1 << tl) < run.count) ++tl;
+    const int token = (threadIdx.x / LANES) & ((1 << tl) - 1);
+    const bool there = token < run.count;
+    Lane<IO, D> L;
+    L.set(P, turns[there ? token : 0], 1.f);
+    const long long t = run.first + token;
+    const int heads = X.H + X.Hkv, step = ROWS >> tl;          // ROWS >= kTokens
+    const uint4 *q = reinterpret_cast<const uint4 *>(X.q), *k = reinterpret_cast<const uint4 *>(X.k);
+    const int first = (threadIdx.x / LANES) >> tl;
+    constexpr int AHEAD = 4;                                   // rows on their way at once
+    for (int h0 = first; h0 - first < heads; h0 += AHEAD * step) {
+        uint4 raw[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int h = h0 + i * step;
+            raw[i] = make_uint4(0, 0, 0, 0);
+            if (there && h < heads) raw[i] = h < X.H ? q[(t * X.q_stride + h * D) / E + L.lane] : k[(t * X.k_stride + (h - X.H) * D) / E + L.lane];
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int h = h0 + i * step;
+            const bool key = h >= X.H;
+            const uint4 o = head_row<IO, D>(P, L, P.wq ? weights[key] : nullptr, raw[i]);
+            if (!there || h >= heads) continue;
+            if (!key) q_out[(t * X.H + h) * LANES + L.lane] = o;
+            else if (!SERVE) k_out[(t * X.Hkv + h - X.H) * LANES + L.lane] = o;
+            else if (in_pool) {
+                const long long block = ((long long)page * X.Hkv + h - X.H) * LANES + L.lane;
+                reinterpret_cast<uint4 *>(kv.k)[(block << kv.page_log) + slot + token] = o;
+            }
+        }
+    }
+    if (!in_pool) return;
+    // values: a lane holds one channel of every token of the run and writes whole groups where the run has them
+    typedef typename IO::elem_t elem_t;
+    const elem_t *v = reinterpret_cast<const elem_t *>(X.v);
+    for (int i = threadIdx.x; i < X.Hkv * D; i += kThreads) {
+        const int h = i / D, c = i % D;
+        elem_t x[kTokens];
+        const int off = slot & (kTokens - 1);      // runs of more than one token in front of an aligned index start inside a group
+#pragma unroll
+        for (int j = 0; j < kTokens; ++j) x[j] = (j >= off && j - off < run.count) ? v[(run.first + j - off) * X.v_stride + i] : 0;
+        elem_t *to = reinterpret_cast<elem_t *>(kv.v) + ((((long long)page * X.Hkv + h) << kv.page_log) * D);
+#pragma unroll
+        for (int g = 0; g < kTokens / E; ++g) {
+            elem_t *at = to + ((long long)((slot - off) / E + g) * D + c) * E;
+            const int a = max(off - g * E, 0), b = min(off + run.count - g * E, E);
+            if (a == 0 && b == E) {
+                uint32_t w[4];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    if constexpr (E == 8) w[m] = (uint32_t)x[g * E + 2 * m] | ((uint32_t)x[g * E + 2 * m + 1] << 16);
+                    else w[m] = x[g * E + m];
+                }
+                *reinterpret_cast<uint4 *>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (e >= a && e < b) at[e] = x[g * E + e];
+            }
+        }
+    }
+}
+
+// Backward.  Weight gradients: a thread sums its rows of one run of tokens in fp32 (at most a few hundred terms go into a channel there) and the
+// runs in fp64; workgroups write their sums and k_heads_weights adds them in a fixed order, so results do not change from run to run.
+template <typename IO, int D>
+__global__ __launch_bounds__(kThreads) void k_heads_backward(HeadParams P, HeadRows X, HeadRows Y, const int *positions, uint4 *gq, uint4 *gk, double *partial) {
+    constexpr int E = IO::E, LANES = D / E, ROWS = kThreads / LANES;
+    __shared__ float2 turns[kTokens][kMostHalf];
+    __shared__ int pos[kTokens];
+    __shared__ float weights[2][D];
+    __shared__ double sums[kThreads / 64][2][D];
+    for (int i = threadIdx.x; i < D; i += kThreads) {
+        weights[0][i] = P.wq ? P.wq[i] : 1.f;
+        weights[1][i] = P.wk ? P.wk[i] : 1.f;
+    }
+    double acc[2][E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[0][e] = acc[1][e] = 0.0;
+    const uint4 *xq = reinterpret_cast<const uint4 *>(X.q), *xk = reinterpret_cast<const uint4 *>(X.k);
+    const uint4 *yq = reinterpret_cast<const uint4 *>(Y.q), *yk = reinterpret_cast<const uint4 *>(Y.k);
+    const int heads = X.H + X.Hkv, token = (threadIdx.x / LANES) & (kTokens - 1);
+    constexpr int step = ROWS / kTokens;
+    for (int t0 = blockIdx.x * kTokens; t0 < X.T; t0 += gridDim.x * kTokens) {
+        const int count = min(kTokens, X.T - t0);
+        __syncthreads();                            // the run before has read `turns`
+        if (threadIdx.x < count) pos[threadIdx.x] = positions ? positions[t0 + threadIdx.x] : t0 + (int)threadIdx.x;
+        __syncthreads();
+        fill_turns(P, pos, count, turns);
+        __syncthreads();
+        const bool there = token < count;
+        Lane<IO, D> L;
+        L.set(P, turns[there ? token : 0], -1.f);
+        const long long t = t0 + token;
+        float part[2][E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) part[0][e] = part[1][e] = 0.f;
+        const int first = (threadIdx.x / LANES) / kTokens;
+        constexpr int AHEAD = 2;
+        for (int h0 = first; h0 - first < heads; h0 += AHEAD * step) {
+            uint4 rx[AHEAD], ry[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int h = h0 + i * step;
+                rx[i] = ry[i] = make_uint4(0, 0, 0, 0);
+                if (there && h < heads) {
+                    rx[i] = h < X.H ? xq[(t * X.q_stride + h * D) / E + L.lane] : xk[(t * X.k_stride + (h - X.H) * D) / E + L.lane];
+                    ry[i] = h < X.H ? yq[(t * Y.q_stride + h * D) / E + L.lane] : yk[(t * Y.k_stride + (h - X.H) * D) / E + L.lane];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int h = h0 + i * step;
+                const bool key = h >= X.H;
+                float y[E], z[E], g[E], x[E];
+                IO::unpack(ry[i], y);
+                if (P.half) {
+                    const uint4 other = P.interleaved ? ry[i] : shuffle(ry[i], L.partner);
+                    IO::unpack(other, z);
+                    L.turn(P, y, z, g);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) g[e] = y[e];
+                }
+                if (P.wq) {
+                    IO::unpack(rx[i], x);
+                    const float *w = weights[key] + L.lane * E;
+                    float sq = 0.f, dot = 0.f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        sq += x[e] * x[e];
+                        dot += g[e] * w[e] * x[e];
+                    }
+                    const float r = rsqrtf(row_sum<LANES>(sq) * (1.f / D) + P.eps);
+                    const float m = row_sum<LANES>(dot) * r * (1.f / D);          // mean(h r x)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const float xh = x[e] * r, gx = g[e] * xh;
+                        if (key) part[1][e] += gx;
+                        else part[0][e] += gx;
+                        g[e] = r * (g[e] * w[e] - xh * m);
+                    }
+                }
+                if (!there || h >= heads) continue;
+                if (!key) gq[(t * X.H + h) * LANES + L.lane] = IO::pack(g);
+                else gk[(t * X.Hkv + h - X.H) * LANES + L.lane] = IO::pack(g);
+            }
+        }
+        if (P.wq)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                acc[0][e] += part[0][e];
+                acc[1][e] += part[1][e];
+            }
+    }
+    if (!P.wq) return;
+    // lanes of a wave that hold the same channels, then the waves
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int m = LANES; m < 64; m <<= 1) acc[n][e] += __shfl_xor(acc[n][e], m, 64);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (lane < LANES)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            sums[wave][0][lane * E + e] = acc[0][e];
+            sums[wave][1][lane * E + e] = acc[1][e];
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
+        double s = 0.0;
+#pragma unroll
+        for (int w = 0; w < kThreads / 64; ++w) s += (&sums[w][0][0])[i];
+        partial[(long long)blockIdx.x * 2 * D + i] = s;
+    }
+}
+
+// 32 channels a workgroup, eight threads each.
+template <int D>
+__global__ __launch_bounds__(256) void k_heads_weights(const double *partial, int blocks, float *gwq, float *gwk) {
+    __shared__ double sums[8][32];
+    const int c = threadIdx.x & 31, part = threadIdx.x >> 5, i = blockIdx.x * 32 + c;
+    double s = 0.0;
+    for (int b = part; b < blocks; b += 8) s += partial[(long long)b * 2 * D + i];
+    sums[part][c] = s;
+    __syncthreads();
+    if (part) return;
+#pragma unroll
+    for (int p = 1; p < 8; ++p) s += sums[p][c];
+    if (i < D) gwq[i] = (float)s;
+    else gwk[i - D] = (float)s;
+}
+
+HeadParams params(const spectre_heads &P) {
+    HeadParams p;
+    p.freq = P.inv_freq; p.wq = P.wq; p.wk = P.wk; p.eps = P.eps; p.half = P.rot / 2; p.interleaved = P.interleaved;
+    return p;
+}
+
+}  // namespace
+
+hipError_t load_kernels_heads() {
+    hipFuncAttributes a;
+    return hipFuncGetAttributes(&a, reinterpret_cast<const void *>(k_heads_weights<64>));
+}
+
+#define SPECTRE_HEADS_DISPATCH(CALL)                                  \
+    if (io == SPECTRE_BF16 && P.d == 64) { CALL(Bf16Group, 64); }     \
+    else if (io == SPECTRE_BF16) { CALL(Bf16Group, 128); }            \
+    else if (P.d == 64) { CALL(F32Group, 64); }                       \
+    else { CALL(F32Group, 128); }
+
+hipError_t launch_heads_forward(const spectre_heads &P, int io, const HeadRows &x, const int *positions, void *q_out, void *k_out, hipStream_t st) {
+    const int blocks = (x.T + kTokens - 1) / kTokens;
+#define CALL(IO, D) k_heads<IO, D, false><<<blocks, kThreads, 0, st>>>(params(P), x, positions, (uint4 *)q_out, (uint4 *)k_out, KvView{}, nullptr, nullptr, 0)
+    SPECTRE_HEADS_DISPATCH(CALL)
+#undef CALL
+    return hipGetLastError();
+}
+
+hipError_t launch_heads_append(const spectre_heads &P, int io, const HeadRows &x, const KvView &kv, const int *start, const int *seqs, int B, void *q_out, hipStream_t st) {
+    const int blocks = x.T / kTokens + 2 * B;
+#define CALL(IO, D) k_heads<IO, D, true><<<blocks, kThreads, 0, st>>>(params(P), x, nullptr, (uint4 *)q_out, nullptr, kv, start, seqs, B)
+    SPECTRE_HEADS_DISPATCH(CALL)
+#undef CALL
+    return hipGetLastError();
+}
+
+int heads_backward_blocks(int T) {
+    const int runs = (T + kTokens - 1) / kTokens;
+    return runs < 1024 ? runs : 1024;               // four workgroups a compute unit, each adds its runs in registers
+}
+
+hipError_t launch_heads_backward(const spectre_heads &P, int io, const HeadRows &x, const HeadRows &dy, const int *positions, void *gq, void *gk, float *gwq, float *gwk,
+                                 double *partial, hipStream_t st) {
+    const int blocks = heads_backward_blocks(x.T);
+#define CALL(IO, D)                                                                                                              \
+    if (blocks) k_heads_backward<IO, D><<<blocks, kThreads, 0, st>>>(params(P), x, dy, positions, (uint4 *)gq, (uint4 *)gk, partial);        \
+    if (P.wq) k_heads_weights<D><<<2 * D / 32, 256, 0, st>>>(partial, blocks, gwq, gwk)
+    SPECTRE_HEADS_DISPATCH(CALL)
+#undef CALL
+    return hipGetLastError();
+}
+
+}  // namespace spectre
