@@ -26,10 +26,14 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2E = 1.4426950408889634f;
-constexpr int kTileRows = 128;                     // rows a workgroup, 32 a wave
 // The maximum follows only when a score is this far above it, in powers of two: until then probabilities grow to 2^8, which costs neither fp32 nor bf16
 // any digit, and the outputs need not be rescaled.
 constexpr float kLag = 8.f;
+
+// 16 bytes a lane from its address into LDS, lane after lane from `to` on (the same in every lane of the wave).
+__device__ __forceinline__ void to_lds(const void *from, uint4 *to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
 
 struct AttendK {
     KvView kv;
@@ -166,14 +170,34 @@ __device__ __forceinline__ void store4(void *out, long long at, float4 x) {
     }
 }
 
+// The larger, NaN if one is: gfx950 has it as one instruction of three operands, without the quieting that fmaxf asks for.
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
+// The larger of a lane's number and that of the lane 32 on.
+typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float max_halves(float x) {
+    const u32x2_t y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return larger(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+
 __device__ __forceinline__ float lse_of(float top2, float sum) { return sum == 0.f ? -INFINITY : (top2 + log2f(sum)) * 0.69314718055994531f; }
 __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
-// ---------------------------------------------------------------- many rows: 128 of a key head a workgroup, tiles of keys through LDS
-template <typename IO, int D>
-__global__ __launch_bounds__(256, 2) void k_attend_tile(AttendK k) {
-    constexpr int E = IO::E, KT = IO::kTileKeys, NK = KT / 32, GROUPS = KT * D / E, PER = GROUPS / 256, QG = D / (2 * E), DT = D / 32;
-    __shared__ uint4 sk[2][GROUPS], sv[2][GROUPS];
+// ---------------------------------------------------------------- many rows: tiles of 64 keys (fp32: 32) through LDS
+// 32 rows a wave; a workgroup's waves share each tile, which goes from memory into LDS without registers (one tile ahead, two buffers, a barrier a tile).
+// The layout of the pages is that of the operands, so LDS reads are runs of 16 bytes without conflicts.
+//
+// What bounds it at d = 64: per 64 keys and 32 rows a wave issues 16 products (32 clocks each on the matrix cores) and about 130 vector instructions
+// that cannot be saved (32 each of scale-and-shift, 2^x, sum; 16 each of maximum and packing), 2^x taking two slots.  Measured on their own in that proportion with their
+// LDS reads, products and vector work overlap only in part: 26.5 ns a product, against 17.5 for products alone and 15.7 for the rest alone.  The kernel takes 35.
+// An 8192-token prompt, 32 heads: 315 us, 872 TFLOP/s (all-zero inputs, which draw less power, 289); 2048 tokens over 28672 558 us, 892 TFLOP/s.
+// Measured and not taken: two sets of 32 rows a wave (half the LDS reads, two waves a SIMD: 4 % slower), scores of the next tile formed between the steps of this tile's
+// softmax within a wave (17 % slower), two tiles a barrier (3 % slower), raised priority around the products (no difference), tiles through registers (4 % slower).
+template <typename IO, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k_attend_tile(AttendK k) {
+    constexpr int THREADS = 64 * WAVES, kTileRows = 32 * WAVES;
+    constexpr int E = IO::E, KT = IO::kTileKeys, NK = KT / 32, GROUPS = KT * D / E, PER = GROUPS / THREADS, QG = D / (2 * E), DT = D / 32;
+    __shared__ uint4 sk0[GROUPS], sv0[GROUPS], sk1[GROUPS], sv1[GROUPS];      // of their own each: the compiler sees which loads a read need not wait for
     __shared__ int odd[2];                          // the last tile whose values were not all finite
     const KvView &kv = k.kv;
     const int pairs = kv.Hkv * k.a.B, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
@@ -186,7 +210,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_tile(AttendK k) {
     const int r = min(r0 + 32 * wave + (lane & 31), rows - 1), token = r / k.G, head = h * k.G + (r - token * k.G);
     const bool mine = r0 + 32 * wave + (lane & 31) < rows, busy = r0 + 32 * wave < rows;
     const int p0 = s.m - s.n, pos = p0 + token;
-    const int from = k.a.window ? pos - k.a.window : -1;                      // keys above it
+    const int lowest = k.a.window ? pos - k.a.window + 1 : 0;                  // the row sees the `span` keys from here on
+    const unsigned span = (unsigned)max(pos - lowest + 1, 0);
     // what all rows of the workgroup, and of the wave, see
     const int first_pos = p0 + r0 / k.G, last_pos = p0 + min(r0 + kTileRows - 1, rows - 1) / k.G;
     const int wave_first = p0 + min(r0 + 32 * wave, rows - 1) / k.G, wave_last = p0 + min(r0 + 32 * wave + 31, rows - 1) / k.G;
@@ -213,90 +238,103 @@ __global__ __launch_bounds__(256, 2) void k_attend_tile(AttendK k) {
 
     const int mask = (1 << kv.page_log) - 1;
     const int *table = kv.table + (long long)s.row * kv.M;
-    // page of this lane's key of tile t (every wave has all keys of a tile), -1 where there is none
+    // page of this lane's key of tile t (every wave has all keys of a tile), -1 where there is none.  It is looked at only when its tile is requested: a
+    // comparison here would wait for it, and with it for the tile requested before.
     auto page_of = [&](int t) {
         const int key = t * KT + (lane & (KT - 1));
         int p = -1;
         if (t < t_hi && key < s.m) p = table[key >> kv.page_log];
-        return (unsigned)p < (unsigned)kv.P ? p : -1;
+        return p;
     };
-    uint4 kr[PER], vr[PER];
-    auto request = [&](int t, int page) {
-        const int slot = (t * KT + (lane & (KT - 1))) & mask;
-        const uint4 *K = reinterpret_cast<const uint4 *>(kv.k), *V = reinterpret_cast<const uint4 *>(kv.v);
-        const long long block = ((long long)page * kv.Hkv + h) * (D / E);
+    const unsigned P = (unsigned)kv.P;
+    // bytes of a page, and of this head and thread inside one: a 64-bit product a lane (keys) or a wave (values), 32-bit sums for the rest
+    const unsigned page_bytes = (unsigned)kv.Hkv * (D * IO::kBytes) << kv.page_log, head_bytes = (unsigned)h * (D * IO::kBytes) << kv.page_log;
+    const unsigned k_at = head_bytes + ((threadIdx.x / KT * 16u) << kv.page_log), v_at = head_bytes + threadIdx.x % D * 16u;
+    const unsigned k_next = ((unsigned)THREADS / KT * 16u) << kv.page_log;
+    // Groups of a tile straight from memory into LDS, in the order they have there: a wave's 64 lanes write 1 KB from its first group on.  Absent keys leave
+    // what lies there.
+    auto request = [&](int t, int page, uint4 *to_k, uint4 *to_v) {
+        const char *kb = reinterpret_cast<const char *>(kv.k) + (unsigned long long)(unsigned)page * page_bytes + (k_at + ((t * KT + (lane & (KT - 1))) & mask) * 16u);
+        if ((unsigned)page < P) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            kr[i] = make_uint4(0, 0, 0, 0);
-            if (page >= 0) kr[i] = K[((block + (threadIdx.x + 256 * i) / KT) << kv.page_log) + slot];
+            for (int i = 0; i < PER; ++i) to_lds(kb + i * k_next, to_k + 64 * wave + THREADS * i);
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int kg = (64 * wave + 256 * i) / D, vp = __builtin_amdgcn_readlane(page, kg * E);
-            vr[i] = make_uint4(0, 0, 0, 0);
-            if (vp >= 0) vr[i] = V[(((long long)vp * kv.Hkv + h) * (D / E) << kv.page_log) + (((t * KT + kg * E) & mask) / E) * D + (threadIdx.x + 256 * i) % D];
+            const int kg = (64 * wave + THREADS * i) / D * E;
+            const unsigned p = (unsigned)__builtin_amdgcn_readlane(page, kg);
+            const char *vb = reinterpret_cast<const char *>(kv.v) + (unsigned long long)p * page_bytes + (((t * KT + kg) & mask) / E) * (D * 16u);
+            if (p < P) to_lds(vb + v_at, to_v + 64 * wave + THREADS * i);
         }
     };
     if (threadIdx.x < 2) odd[threadIdx.x] = -1;
-    __syncthreads();
     int page = page_of(t_lo), next = page_of(t_lo + 1);
-    if (t_lo < t_hi) request(t_lo, page);
+    if (t_lo < t_hi) request(t_lo, page, sk0, sv0);
     const int krow = IO::key_of_row(lane & 31);
 
-    for (int t = t_lo, buf = 0; t < t_hi; ++t, buf ^= 1) {
-        const unsigned long long there = __ballot(page >= 0);      // bit = key of the tile (fp32: twice 32 keys)
+    auto tile_step = [&](int t, uint4 *sk, uint4 *sv, uint4 *next_k, uint4 *next_v, int *flag) {
+        const unsigned long long there = __ballot((unsigned)page < P);      // bit = key of the tile (fp32: twice 32 keys)
         const bool edge = there != ~0ull || t * KT + KT - 1 > first_pos || t * KT <= last_pos - (k.a.window ? k.a.window : last_pos + 1);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                     // this wave's part of the tile has arrived ...
+        __syncthreads();                                                    // ... and everybody's, and nobody reads the other buffer any more
+        page = next;
+        if (t + 1 < t_hi) {
+            request(t + 1, page, next_k, next_v);
+            next = page_of(t + 2);
+        }
         if (edge) {                                                 // values of no one's keys, and those that are not finite
             bool fine = true;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int have = s.m - (t * KT + (64 * wave + 256 * i) / D * E);
-                if (have < E) vr[i] = keep_first<IO>(vr[i], have);
-                if (!all_finite<IO>(vr[i])) {
+                const int kg = (64 * wave + THREADS * i) / D * E;
+                uint4 x = sv[threadIdx.x + THREADS * i];
+                x = keep_first<IO>(x, ((there >> kg) & 1) ? s.m - (t * KT + kg) : 0);
+                if (!all_finite<IO>(x)) {
                     fine = false;
-                    vr[i] = finite_only<IO>(vr[i]);
+                    x = finite_only<IO>(x);
                 }
+                sv[threadIdx.x + THREADS * i] = x;
             }
-            if (!fine) odd[buf] = t;
+            if (!fine) *flag = t;
+            __syncthreads();
         }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            sk[buf][threadIdx.x + 256 * i] = kr[i];
-            sv[buf][threadIdx.x + 256 * i] = vr[i];
-        }
-        page = next;
-        if (t + 1 < t_hi) {
-            request(t + 1, page);
-            next = page_of(t + 2);
-        }
-        __syncthreads();
-        if (!busy || t * KT > wave_last) continue;
+        if (!busy || t * KT > wave_last) return;
 
         f32x16_t sc[NK];
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[n][i] = 0.f;
+            uint4 a[QG];
 #pragma unroll
-            for (int i = 0; i < QG; ++i) IO::mma32(sc[n], sk[buf][(2 * i + half) * KT + 32 * n + krow], q[i]);
+            for (int i = 0; i < QG; ++i) a[i] = sk[(2 * i + half) * KT + 32 * n + krow];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < QG; ++i) IO::mma32(sc[n], a[i], q[i]);
         }
         const bool some = there != ~0ull || t * KT + KT - 1 > wave_first || t * KT <= wave_last - (k.a.window ? k.a.window : wave_last + 1);
         if (some) {
-            const unsigned long long mates = there >> (IO::kHalf * half);
+            const unsigned at0 = (unsigned)(t * KT + IO::kHalf * half - lowest);
 #pragma unroll
             for (int n = 0; n < NK; ++n)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int at = 32 * n + IO::key_of_acc(i), key = t * KT + at + IO::kHalf * half;
-                    if (!((mates >> at) & 1) || key > pos || key <= from) sc[n][i] = -INFINITY;
-                }
+                for (int i = 0; i < 16; ++i)
+                    if (at0 + (32 * n + IO::key_of_acc(i)) >= span) sc[n][i] = -INFINITY;
+            if (there != ~0ull) {                                   // pages that are not there
+                const unsigned long long mates = there >> (IO::kHalf * half);
+#pragma unroll
+                for (int n = 0; n < NK; ++n)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (!((mates >> (32 * n + IO::key_of_acc(i))) & 1)) sc[n][i] = -INFINITY;
+            }
         }
         float mx = sc[0][0];
 #pragma unroll
         for (int n = 0; n < NK; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[n][i]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            for (int i = 0; i < 16; ++i) mx = larger(mx, sc[n][i]);
+        mx = max_halves(mx);
         if (__ballot(lags(mx, top, lag))) {
             const float f = follow(mx, k.c, &top);
             sum *= f;
@@ -318,12 +356,16 @@ __global__ __launch_bounds__(256, 2) void k_attend_tile(AttendK k) {
         for (int g = 0; g < NK * IO::kChunks; ++g) {
             const uint4 pg = IO::pack(p + g * E);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) IO::mma32(o[d], sv[buf][(2 * g + half) * D + 32 * d + (lane & 31)], pg);
+            for (int d = 0; d < DT; ++d) IO::mma32(o[d], sv[(2 * g + half) * D + 32 * d + (lane & 31)], pg);
         }
-        if (odd[buf] == t) {
-            add_not_finite<IO, D, 16 * DT>(kv, s, h, t * KT, KT, pos, from, [half](int i) { return 32 * (i / 16) + 8 * ((i % 16) / 4) + 4 * half + i % 4; },
+        if (*flag == t) {
+            add_not_finite<IO, D, 16 * DT>(kv, s, h, t * KT, KT, pos, lowest - 1, [half](int i) { return 32 * (i / 16) + 8 * ((i % 16) / 4) + 4 * half + i % 4; },
                                            [&](int i, float x) { o[i / 16][i % 16] += x; });
         }
+    };
+    for (int t = t_lo; t < t_hi; t += 2) {
+        tile_step(t, sk0, sv0, sk1, sv1, &odd[0]);
+        if (t + 1 < t_hi) tile_step(t + 1, sk1, sv1, sk0, sv0, &odd[1]);
     }
     if (!mine) return;
     sum += __shfl_xor(sum, 32, 64);
@@ -562,47 +604,67 @@ __global__ __launch_bounds__(256, R * D == 64 ? 3 : R * D == 128 ? 2 : 1) void k
     }
 }
 
-// ---------------------------------------------------------------- splits joined: a wave a row
-template <typename IO, int D>
+// ---------------------------------------------------------------- splits joined
+// D / 4 lanes hold a row's channels; GROUPS such groups of a workgroup share the splits of one row.  Many rows have a group each; few rows (and then many
+// splits) a workgroup each, where what counts is that all loads are on their way at once.
+template <typename IO, int D, int GROUPS>
 __global__ __launch_bounds__(256) void k_attend_join(AttendK k, int few_splits, int tile_splits) {
-    constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;
-    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (row >= (long long)k.a.T * k.a.H) return;
-    const int t = (int)(row / k.a.H);
-    int lo = 0, hi = k.a.B;                        // the sequence with start <= t < the next one's
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (k.a.start[mid] <= t) lo = mid;
-        else hi = mid;
+    constexpr int LANES = D / 4, ROWS = 256 / (LANES * GROUPS);
+    __shared__ f32x4_t so[GROUPS > 1 ? GROUPS : 1][LANES];
+    __shared__ float2 st[GROUPS > 1 ? GROUPS : 1];
+    const int c = threadIdx.x % LANES, g = threadIdx.x / LANES % GROUPS;
+    const long long row = (long long)blockIdx.x * ROWS + threadIdx.x / (LANES * GROUPS), rows = (long long)k.a.T * k.a.H;
+    int splits = 0;
+    if (row < rows) {
+        const int t = (int)(row / k.a.H);
+        if (few_splits && tile_splits) {           // which kernel had the row depends on its sequence, the last one with start <= t
+            int lo = 0, hi = k.a.B;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (k.a.start[mid] <= t) lo = mid;
+                else hi = mid;
+            }
+            const int n = k.a.start[lo + 1] - k.a.start[lo];
+            splits = (long long)n * k.G <= k.few_rows ? few_splits : tile_splits;
+        } else splits = few_splits + tile_splits;
+        if (t >= k.a.start[k.a.B] || splits == 1) splits = 0;
     }
-    if (t < k.a.start[lo] || t >= k.a.start[lo + 1]) return;
-    const int n = k.a.start[lo + 1] - k.a.start[lo], splits = (long long)n * k.G <= k.few_rows ? few_splits : tile_splits;
-    if (splits <= 1) return;
     const float2 *stat = k.stat + row * k.slots;
-    float best = -INFINITY;
-    for (int s = lane; s < splits; s += 64) best = fmaxf(best, stat[s].y == 0.f ? -INFINITY : stat[s].x);
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) best = fmaxf(best, __shfl_xor(best, m, 64));
-    const int g = lane / LANES, c = lane % LANES;
-    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
     const float *part = k.part + row * k.slots * D + 4 * c;
+    float best = -INFINITY, total = 0.f;
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int s = g; s < splits; s += AT_ONCE) {
+    for (int s = g; s < splits; s += GROUPS) {
         const float2 x = stat[s];
-        if (x.y == 0.f) continue;                  // nothing seen, nothing written
+        if (x.y != 0.f) best = fmaxf(best, x.x);   // a part whose sum is zero saw nothing and wrote nothing
+    }
+#pragma unroll 4
+    for (int s = g; s < splits; s += GROUPS) {
+        const float2 x = stat[s];
+        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(part + (long long)s * D);
         const float f = x.x == best ? 1.f : exp2_fast(x.x - best);
-        total += f * x.y;
-        o += f * *reinterpret_cast<const f32x4_t *>(part + (long long)s * D);
+        if (x.y != 0.f) {
+            total += f * x.y;
+            o += f * y;
+        }
     }
-#pragma unroll
-    for (int m = LANES; m < 64; m <<= 1) {
-        total += __shfl_xor(total, m, 64);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], m, 64);
+    if constexpr (GROUPS > 1) {
+        so[g][c] = o;
+        if (c == 0) st[g] = make_float2(best, total);
+        __syncthreads();
+        if (g) return;
+        for (int i = 1; i < GROUPS; ++i) best = fmaxf(best, st[i].x);
+        total = 0.f;
+        o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < GROUPS; ++i) {
+            const float2 x = st[i];
+            if (x.y == 0.f) continue;
+            const float f = x.x == best ? 1.f : exp2_fast(x.x - best);
+            total += f * x.y;
+            o += f * so[i][c];
+        }
     }
-    if (g) return;
+    if (!splits) return;
     const float inv = inverse(total);
     store4<IO>(k.a.out, row * D + 4 * c, make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv));
     if (k.a.lse && c == 0) k.a.lse[row] = lse_of(best, total);
@@ -612,8 +674,15 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendK k, int few_splits, 
 
 hipError_t load_kernels_attend() {
     hipFuncAttributes a;
-    return hipFuncGetAttributes(&a, reinterpret_cast<const void *>(k_attend_join<Bf16Mma, 64>));
+    return hipFuncGetAttributes(&a, reinterpret_cast<const void *>(k_attend_join<Bf16Mma, 64, 1>));
 }
+
+// Up to this many rows a joining workgroup has one row, beyond it a row for each D / 4 lanes: 32 rows of 64 parts 4.5 instead of 8 us, 131072 of two 27 instead of 64
+// (the first form gave every row a wave).
+constexpr long long kWideRows = 4096;
+// Where the sequences differ, the longest must not be one workgroup's work for as long as the others take together; every part costs its rows once through
+// memory: 32 sequences of up to 512 new and 8500 tokens in all take 315 us with parts of 4096 keys, 334 with 2048, 394 with 1024, 401 undivided.
+constexpr long long kRaggedKeys = 4096;
 
 AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new, int max_len, int window) {
     AttendPlan p{};
@@ -624,7 +693,6 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
     p.few = rows <= 32 || (!even && G <= 16);
     p.tile = rows > 32;
     p.few_rows = !p.few ? 0 : p.tile ? 16 : (int)rows;
-    p.tiles = (int)((rows + kTileRows - 1) / kTileRows);
     p.few_splits = p.tile_splits = 1;
     const long long pairs = (long long)B * Hkv;
     if (p.few) {
@@ -633,9 +701,19 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
         p.few_splits = (int)std::max(1ll, std::min(s, 256ll));
     }
     if (p.tile) {
-        const long long groups = Hkv * (even ? (long long)B * p.tiles : std::min<long long>((long long)B * p.tiles, ((long long)T * G + kTileRows - 1) / kTileRows));
-        long long s = std::min(512 / groups, len / 256);
-        p.tile_splits = (int)std::max(1ll, std::min(s, 64ll));
+        auto groups = [&](int waves) {
+            const long long tiles = (rows + 32 * waves - 1) / (32 * waves), filled = ((long long)T * G + 32 * waves - 1) / (32 * waves);
+            return Hkv * (even ? B * tiles : std::max(1ll, std::min(B * tiles, filled)));
+        };
+        // 256 rows a workgroup halve the keys' way through LDS (8192-token prompt 315 instead of 322 us, d = 128 120 instead of 130); with fewer than a workgroup
+        // a compute unit 128 fill the card better (512 tokens over 16000, d = 128: 97 instead of 109 us; a ragged fp32 batch 155 instead of 167).
+        p.tile_waves = groups(8) >= 256 ? 8 : 4;
+        p.tiles = (int)((rows + 32 * p.tile_waves - 1) / (32 * p.tile_waves));
+        // workgroups that run at once, by their registers and LDS; keys are split where rows leave some of them free
+        const long long slots = p.tile_waves == 8 || d == 128 ? 512 : io == SPECTRE_BF16 ? 1024 : 768;
+        long long s = slots / groups(p.tile_waves);
+        if (!even) s = std::max(s, (len + kRaggedKeys - 1) / kRaggedKeys);
+        p.tile_splits = (int)std::max(1ll, std::min({s, len / 256, 64ll}));
     }
     const int most = std::max(p.few_splits, p.tile_splits);
     if (most > 1) p.partial_bytes = (size_t)T * H * most * ((size_t)d * 4 + 8);
@@ -674,7 +752,9 @@ hipError_t launch_attend(const KvView &kv, int d, int io, const AttendArgs &a, c
     if (p.tile) {
         k.splits = p.tile_splits;
         const int blocks = pairs * p.tile_splits * p.tiles;
-#define CALL(IO, D) k_attend_tile<IO, D><<<blocks, 256, 0, st>>>(k)
+#define CALL(IO, D)                                                                        \
+    if (p.tile_waves == 8) k_attend_tile<IO, D, 8><<<blocks, 512, 0, st>>>(k);             \
+    else k_attend_tile<IO, D, 4><<<blocks, 256, 0, st>>>(k)
         SPECTRE_ATTEND_DISPATCH(CALL)
 #undef CALL
         hipError_t e = hipGetLastError();
@@ -682,7 +762,10 @@ hipError_t launch_attend(const KvView &kv, int d, int io, const AttendArgs &a, c
     }
     if (p.few_splits > 1 || p.tile_splits > 1) {
         const long long rows = (long long)a.T * a.H;
-#define CALL(IO, D) k_attend_join<IO, D><<<(int)((rows + 3) / 4), 256, 0, st>>>(k, p.few_splits, p.tile_splits)
+        const int few = p.few ? p.few_splits : 0, tile = p.tile ? p.tile_splits : 0;
+#define CALL(IO, D)                                                                                                             \
+    if (rows <= kWideRows) k_attend_join<IO, D, 1024 / D><<<(int)rows, 256, 0, st>>>(k, few, tile);                             \
+    else k_attend_join<IO, D, 1><<<(int)((rows + 1024 / D - 1) / (1024 / D)), 256, 0, st>>>(k, few, tile)
         SPECTRE_ATTEND_DISPATCH(CALL)
 #undef CALL
     }

@@ -62,7 +62,7 @@ hipError_t launch_kv_copy(const KvView &kv, int layers, const int *src, const in
 struct AttendPlan {
     int few, tile;                   // whether each kernel is launched
     int few_rows;                    // rows (new tokens x heads of a key head) that the kernel of few rows takes, 0 if it is not launched
-    int few_splits, tile_splits, tiles;
+    int few_splits, tile_splits, tiles, tile_waves;
     size_t partial_bytes;            // of all rows' split results
 };
 struct AttendArgs {
