@@ -3,7 +3,9 @@
 //
 // Per row x of d channels: r = (mean x^2 + eps)^-1/2, y = w r x, and each pair (a, b) of y turned by the angle pos * f_i:
 // (a cos - b sin, b cos + a sin).  Backward with g = the output's gradient turned back: g_w = sum g r x over rows, h = g w,
-// g_x = r (h - r x mean(h r x)).  Rows are read and written once; memory bounds the long calls, the launch the short ones.
+// g_x = r (h - r x mean(h r x)).  Rows are read and written once; memory bounds the long calls, the launch the short ones.  32768 tokens of 32 + 8 bf16 heads, d = 64:
+// forward 68 us (336 MB, 4.9 TB/s), backward 108 (503 MB, 4.7 TB/s, the sums of the weights' gradients in it), against 5.2 TB/s of a large copy; 8192 tokens into
+// pages 22 us (4.6 TB/s); one token 5.
 #include <math.h>
 
 #include "common.h"
@@ -101,11 +103,32 @@ struct Lane {
     }
 };
 
+// Sum over the 8, 16 or 32 lanes of a row, in all of them: moves inside the vector unit, not through LDS.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+    return __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
 template <int LANES>
 __device__ __forceinline__ float row_sum(float x) {
-#pragma unroll
-    for (int m = 1; m < LANES; m <<= 1) x += __shfl_xor(x, m, 64);
+    static_assert(LANES == 8 || LANES == 16 || LANES == 32, "lanes of a row");
+    x += dpp<0xB1>(x);                              // lane ^ 1
+    x += dpp<0x4E>(x);                              // lane ^ 2
+    x += dpp<0x141>(x);                             // the other four of eight
+    if constexpr (LANES >= 16) x += dpp<0x140>(x);  // the other eight of sixteen
+    if constexpr (LANES == 32) {
+        typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+        const u32x2_t y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+    }
     return x;
+}
+
+// Rows of gradients and of training's outputs: through plain stores while the L2s hold them together for whoever comes next, streaming beyond that, which
+// leaves the memory-side cache to what is read again (32768 tokens of 40 bf16 heads, forward and backward: 163 instead of 181 us; 8000 fp32 tokens 91 instead of 93).
+__device__ __forceinline__ void put(uint4 *p, uint4 v, bool stream) {
+    const float4 w = __builtin_bit_cast(float4, v);
+    if (stream) stream_store(reinterpret_cast<float4 *>(p), w);
+    else *reinterpret_cast<float4 *>(p) = w;
 }
 
 __device__ __forceinline__ uint4 shuffle(uint4 g, int lane) {
@@ -172,7 +195,7 @@ __device__ __forceinline__ bool find_run(const KvView &kv, const int *start, con
 
 template <typename IO, int D, bool SERVE>
 __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, const int *positions, uint4 *q_out, uint4 *k_out, KvView kv, const int *start, const int *seqs,
-                                                    int B) {
+                                                    int B, bool stream) {
     constexpr int E = IO::E, LANES = D / E, ROWS = kThreads / LANES;
     __shared__ float2 turns[kTokens][kMostHalf];
     __shared__ int pos[kTokens];
@@ -208,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
     const uint4 *q = reinterpret_cast<const uint4 *>(X.q), *k = reinterpret_cast<const uint4 *>(X.k);
     const int first = (threadIdx.x / LANES) >> tl;
     constexpr int AHEAD = 4;                                   // rows on their way at once
-    for (int h0 = first; h0 - first < heads; h0 += AHEAD * step) {
+    for (int h0 = first + (int)blockIdx.y * AHEAD * step; h0 - first < heads; h0 += AHEAD * step * (int)gridDim.y) {
         uint4 raw[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
@@ -222,8 +245,8 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
             const bool key = h >= X.H;
             const uint4 o = head_row<IO, D>(P, L, P.wq ? weights[key] : nullptr, raw[i]);
             if (!there || h >= heads) continue;
-            if (!key) q_out[(t * X.H + h) * LANES + L.lane] = o;
-            else if (!SERVE) k_out[(t * X.Hkv + h - X.H) * LANES + L.lane] = o;
+            if (!key) put(&q_out[(t * X.H + h) * LANES + L.lane], o, stream);
+            else if (!SERVE) put(&k_out[(t * X.Hkv + h - X.H) * LANES + L.lane], o, stream);
             else if (in_pool) {
                 const long long block = ((long long)page * X.Hkv + h - X.H) * LANES + L.lane;
                 reinterpret_cast<uint4 *>(kv.k)[(block << kv.page_log) + slot + token] = o;
@@ -234,7 +257,7 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
     // values: a lane holds one channel of every token of the run and writes whole groups where the run has them
     typedef typename IO::elem_t elem_t;
     const elem_t *v = reinterpret_cast<const elem_t *>(X.v);
-    for (int i = threadIdx.x; i < X.Hkv * D; i += kThreads) {
+    for (int i = threadIdx.x + kThreads * blockIdx.y; i < X.Hkv * D; i += kThreads * gridDim.y) {
         const int h = i / D, c = i % D;
         elem_t x[kTokens];
         const int off = slot & (kTokens - 1);      // runs of more than one token in front of an aligned index start inside a group
@@ -262,10 +285,12 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
     }
 }
 
-// Backward.  Weight gradients: a thread sums its rows of one run of tokens in fp32 (at most a few hundred terms go into a channel there) and the
-// runs in fp64; workgroups write their sums and k_heads_weights adds them in a fixed order, so results do not change from run to run.
+// Backward.  Weight gradients: a thread sums its rows in fp32 (of at most kRunsEach runs of tokens, a few dozen terms a channel); the lanes' and the workgroups'
+// sums are added in fp64 in a fixed order, so results do not change from run to run.
+constexpr int kRunsEach = 4;
+
 template <typename IO, int D>
-__global__ __launch_bounds__(kThreads) void k_heads_backward(HeadParams P, HeadRows X, HeadRows Y, const int *positions, uint4 *gq, uint4 *gk, double *partial) {
+__global__ __launch_bounds__(kThreads) void k_heads_backward(HeadParams P, HeadRows X, HeadRows Y, const int *positions, uint4 *gq, uint4 *gk, double *partial, bool stream) {
     constexpr int E = IO::E, LANES = D / E, ROWS = kThreads / LANES;
     __shared__ float2 turns[kTokens][kMostHalf];
     __shared__ int pos[kTokens];
@@ -275,99 +300,83 @@ __global__ __launch_bounds__(kThreads) void k_heads_backward(HeadParams P, HeadR
         weights[0][i] = P.wq ? P.wq[i] : 1.f;
         weights[1][i] = P.wk ? P.wk[i] : 1.f;
     }
-    double acc[2][E];
+    float part[2][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[0][e] = acc[1][e] = 0.0;
+    for (int e = 0; e < E; ++e) part[0][e] = part[1][e] = 0.f;
     const uint4 *xq = reinterpret_cast<const uint4 *>(X.q), *xk = reinterpret_cast<const uint4 *>(X.k);
     const uint4 *yq = reinterpret_cast<const uint4 *>(Y.q), *yk = reinterpret_cast<const uint4 *>(Y.k);
-    const int heads = X.H + X.Hkv, token = (threadIdx.x / LANES) & (kTokens - 1);
+    const int heads = X.H + X.Hkv, token = (threadIdx.x / LANES) & (kTokens - 1), lane = threadIdx.x % LANES;
     constexpr int step = ROWS / kTokens;
+    const int first = (threadIdx.x / LANES) / kTokens;
     for (int t0 = blockIdx.x * kTokens; t0 < X.T; t0 += gridDim.x * kTokens) {
         const int count = min(kTokens, X.T - t0);
+        const bool there = token < count;
+        const long long t = t0 + token;
+        uint4 rx, ry, nx, ny;                       // this row, and the next one on its way; two at a time cost registers, and with them waves: 122 instead of 108 us
+        auto request = [&](int h, uint4 &x, uint4 &y) {
+            x = y = make_uint4(0, 0, 0, 0);
+            if (there && h < heads) {
+                x = h < X.H ? xq[(t * X.q_stride + h * D) / E + lane] : xk[(t * X.k_stride + (h - X.H) * D) / E + lane];
+                y = h < X.H ? yq[(t * Y.q_stride + h * D) / E + lane] : yk[(t * Y.k_stride + (h - X.H) * D) / E + lane];
+            }
+        };
+        request(first, rx, ry);                     // on their way while the angles are formed
         __syncthreads();                            // the run before has read `turns`
         if (threadIdx.x < count) pos[threadIdx.x] = positions ? positions[t0 + threadIdx.x] : t0 + (int)threadIdx.x;
         __syncthreads();
         fill_turns(P, pos, count, turns);
         __syncthreads();
-        const bool there = token < count;
         Lane<IO, D> L;
         L.set(P, turns[there ? token : 0], -1.f);
-        const long long t = t0 + token;
-        float part[2][E];
+        for (int h = first; h - first < heads; h += step) {
+            request(h + step, nx, ny);
+            const bool key = h >= X.H;
+            float y[E], z[E], g[E], x[E];
+            IO::unpack(ry, y);
+            if (P.half) {
+                const uint4 other = P.interleaved ? ry : shuffle(ry, L.partner);
+                IO::unpack(other, z);
+                L.turn(P, y, z, g);
+            } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) part[0][e] = part[1][e] = 0.f;
-        const int first = (threadIdx.x / LANES) / kTokens;
-        constexpr int AHEAD = 2;
-        for (int h0 = first; h0 - first < heads; h0 += AHEAD * step) {
-            uint4 rx[AHEAD], ry[AHEAD];
+                for (int e = 0; e < E; ++e) g[e] = y[e];
+            }
+            if (P.wq) {
+                IO::unpack(rx, x);
+                const float *w = weights[key] + lane * E;
+                float sq = 0.f, dot = 0.f;
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                const int h = h0 + i * step;
-                rx[i] = ry[i] = make_uint4(0, 0, 0, 0);
-                if (there && h < heads) {
-                    rx[i] = h < X.H ? xq[(t * X.q_stride + h * D) / E + L.lane] : xk[(t * X.k_stride + (h - X.H) * D) / E + L.lane];
-                    ry[i] = h < X.H ? yq[(t * Y.q_stride + h * D) / E + L.lane] : yk[(t * Y.k_stride + (h - X.H) * D) / E + L.lane];
+                for (int e = 0; e < E; ++e) {
+                    sq += x[e] * x[e];
+                    dot += g[e] * w[e] * x[e];
+                }
+                const float r = rsqrtf(row_sum<LANES>(sq) * (1.f / D) + P.eps);
+                const float m = row_sum<LANES>(dot) * r * (1.f / D);          // mean(h r x)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float xh = x[e] * r, gx = g[e] * xh;
+                    if (key) part[1][e] += gx;
+                    else part[0][e] += gx;
+                    g[e] = r * (g[e] * w[e] - xh * m);
                 }
             }
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                const int h = h0 + i * step;
-                const bool key = h >= X.H;
-                float y[E], z[E], g[E], x[E];
-                IO::unpack(ry[i], y);
-                if (P.half) {
-                    const uint4 other = P.interleaved ? ry[i] : shuffle(ry[i], L.partner);
-                    IO::unpack(other, z);
-                    L.turn(P, y, z, g);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) g[e] = y[e];
-                }
-                if (P.wq) {
-                    IO::unpack(rx[i], x);
-                    const float *w = weights[key] + L.lane * E;
-                    float sq = 0.f, dot = 0.f;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        sq += x[e] * x[e];
-                        dot += g[e] * w[e] * x[e];
-                    }
-                    const float r = rsqrtf(row_sum<LANES>(sq) * (1.f / D) + P.eps);
-                    const float m = row_sum<LANES>(dot) * r * (1.f / D);          // mean(h r x)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const float xh = x[e] * r, gx = g[e] * xh;
-                        if (key) part[1][e] += gx;
-                        else part[0][e] += gx;
-                        g[e] = r * (g[e] * w[e] - xh * m);
-                    }
-                }
-                if (!there || h >= heads) continue;
-                if (!key) gq[(t * X.H + h) * LANES + L.lane] = IO::pack(g);
-                else gk[(t * X.Hkv + h - X.H) * LANES + L.lane] = IO::pack(g);
-            }
+            if (there && !key) put(&gq[(t * X.H + h) * LANES + lane], IO::pack(g), stream);
+            else if (there && h < heads) put(&gk[(t * X.Hkv + h - X.H) * LANES + lane], IO::pack(g), stream);
+            rx = nx;
+            ry = ny;
         }
-        if (P.wq)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                acc[0][e] += part[0][e];
-                acc[1][e] += part[1][e];
-            }
     }
     if (!P.wq) return;
     // lanes of a wave that hold the same channels, then the waves
+    const int wave = threadIdx.x >> 6;
 #pragma unroll
     for (int e = 0; e < E; ++e)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < 2; ++n) {
+            double s = part[n][e];
 #pragma unroll
-            for (int m = LANES; m < 64; m <<= 1) acc[n][e] += __shfl_xor(acc[n][e], m, 64);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if (lane < LANES)
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            sums[wave][0][lane * E + e] = acc[0][e];
-            sums[wave][1][lane * E + e] = acc[1][e];
+            for (int m = LANES; m < 64; m <<= 1) s += __shfl_xor(s, m, 64);
+            if ((threadIdx.x & 63) < LANES) sums[wave][n][lane * E + e] = s;
         }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
@@ -378,21 +387,30 @@ __global__ __launch_bounds__(kThreads) void k_heads_backward(HeadParams P, HeadR
     }
 }
 
-// 32 channels a workgroup, eight threads each.
+// Eight channels a workgroup, 32 threads each.
 template <int D>
 __global__ __launch_bounds__(256) void k_heads_weights(const double *partial, int blocks, float *gwq, float *gwk) {
-    __shared__ double sums[8][32];
-    const int c = threadIdx.x & 31, part = threadIdx.x >> 5, i = blockIdx.x * 32 + c;
+    __shared__ double sums[32][8];
+    const int c = threadIdx.x & 7, part = threadIdx.x >> 3, i = blockIdx.x * 8 + c;
     double s = 0.0;
-    for (int b = part; b < blocks; b += 8) s += partial[(long long)b * 2 * D + i];
+#pragma unroll 8
+    for (int b = part; b < blocks; b += 32) s += partial[(long long)b * 2 * D + i];
     sums[part][c] = s;
     __syncthreads();
     if (part) return;
 #pragma unroll
-    for (int p = 1; p < 8; ++p) s += sums[p][c];
+    for (int p = 1; p < 32; ++p) s += sums[p][c];
     if (i < D) gwq[i] = (float)s;
     else gwk[i - D] = (float)s;
 }
+
+// A run's heads are divided among workgroups while there are few of those: 3700 fp32 tokens of 16 heads, d = 128, 19.6 instead of 23.4 us.
+int head_parts(int blocks) {
+    const int parts = 2048 / (blocks > 0 ? blocks : 1);
+    return parts < 1 ? 1 : parts > 4 ? 4 : parts;
+}
+
+bool streams(const HeadRows &x, int d, int io) { return (size_t)x.T * (x.H + x.Hkv) * d * (io == SPECTRE_BF16 ? 2 : 4) > kL2Bytes; }
 
 HeadParams params(const spectre_heads &P) {
     HeadParams p;
@@ -415,7 +433,7 @@ hipError_t load_kernels_heads() {
 
 hipError_t launch_heads_forward(const spectre_heads &P, int io, const HeadRows &x, const int *positions, void *q_out, void *k_out, hipStream_t st) {
     const int blocks = (x.T + kTokens - 1) / kTokens;
-#define CALL(IO, D) k_heads<IO, D, false><<<blocks, kThreads, 0, st>>>(params(P), x, positions, (uint4 *)q_out, (uint4 *)k_out, KvView{}, nullptr, nullptr, 0)
+#define CALL(IO, D) k_heads<IO, D, false><<<dim3(blocks, head_parts(blocks)), kThreads, 0, st>>>(params(P), x, positions, (uint4 *)q_out, (uint4 *)k_out, KvView{}, nullptr, nullptr, 0, streams(x, P.d, io))
     SPECTRE_HEADS_DISPATCH(CALL)
 #undef CALL
     return hipGetLastError();
@@ -423,23 +441,24 @@ hipError_t launch_heads_forward(const spectre_heads &P, int io, const HeadRows &
 
 hipError_t launch_heads_append(const spectre_heads &P, int io, const HeadRows &x, const KvView &kv, const int *start, const int *seqs, int B, void *q_out, hipStream_t st) {
     const int blocks = x.T / kTokens + 2 * B;
-#define CALL(IO, D) k_heads<IO, D, true><<<blocks, kThreads, 0, st>>>(params(P), x, nullptr, (uint4 *)q_out, nullptr, kv, start, seqs, B)
+#define CALL(IO, D) k_heads<IO, D, true><<<dim3(blocks, head_parts(blocks)), kThreads, 0, st>>>(params(P), x, nullptr, (uint4 *)q_out, nullptr, kv, start, seqs, B, false)
     SPECTRE_HEADS_DISPATCH(CALL)
 #undef CALL
     return hipGetLastError();
 }
 
+// One run a workgroup up to four workgroups a compute unit, then up to kRunsEach.
 int heads_backward_blocks(int T) {
-    const int runs = (T + kTokens - 1) / kTokens;
-    return runs < 1024 ? runs : 1024;               // four workgroups a compute unit, each adds its runs in registers
+    const int runs = (T + kTokens - 1) / kTokens, most = (runs + kRunsEach - 1) / kRunsEach;
+    return runs < 1024 ? runs : most > 1024 ? most : 1024;
 }
 
 hipError_t launch_heads_backward(const spectre_heads &P, int io, const HeadRows &x, const HeadRows &dy, const int *positions, void *gq, void *gk, float *gwq, float *gwk,
                                  double *partial, hipStream_t st) {
     const int blocks = heads_backward_blocks(x.T);
 #define CALL(IO, D)                                                                                                              \
-    if (blocks) k_heads_backward<IO, D><<<blocks, kThreads, 0, st>>>(params(P), x, dy, positions, (uint4 *)gq, (uint4 *)gk, partial);        \
-    if (P.wq) k_heads_weights<D><<<2 * D / 32, 256, 0, st>>>(partial, blocks, gwq, gwk)
+    if (blocks) k_heads_backward<IO, D><<<blocks, kThreads, 0, st>>>(params(P), x, dy, positions, (uint4 *)gq, (uint4 *)gk, partial, streams(x, P.d, io)); \
+    if (P.wq) k_heads_weights<D><<<2 * D / 8, 256, 0, st>>>(partial, blocks, gwq, gwk)
     SPECTRE_HEADS_DISPATCH(CALL)
 #undef CALL
     return hipGetLastError();
