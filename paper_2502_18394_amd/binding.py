@@ -532,6 +532,11 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _now(stream):
+    """Raw handle of `stream` or the current one, for the calls that take tensors (so that the device is there): a serving step makes several."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
+
+
 _kv_prepared = set()
 
 
@@ -584,7 +589,7 @@ def qk_norm_rotate(q, k, positions=None, rope=None, wq=None, wk=None, eps=1e-6, 
     _same(q_out, q, "q_out")
     _same(k_out, k, "k_out")
     _check(lib().spectre_heads_forward(ctypes.byref(P), qa, qs, ka, ks, None if positions is None else _ints(positions, "positions", T), T, H, Hkv, io,
-                                       _ptr(q_out, "q_out"), _ptr(k_out, "k_out"), _raw_stream(stream)))
+                                       _ptr(q_out, "q_out"), _ptr(k_out, "k_out"), _now(stream)))
     return q_out, k_out
 
 
@@ -613,7 +618,7 @@ def qk_norm_rotate_backward(dq, dk, q, k, positions=None, rope=None, wq=None, wk
     _check(lib().spectre_heads_backward(ctypes.byref(P), *rows[0], *rows[1], *rows[2], *rows[3],
                                         None if positions is None else _ints(positions, "positions", T), T, H, Hkv, io, gq.data_ptr(), gk.data_ptr(),
                                         None if gw[0] is None else gw[0].data_ptr(), None if gw[1] is None else gw[1].data_ptr(), wsp, wsn,
-                                        _raw_stream(stream)))
+                                        _now(stream)))
     return gq, gk, gw[0], gw[1]
 
 
@@ -662,7 +667,7 @@ class KvPages:
 
     def reset(self, stream=None):
         """No sequence has a token, no page a user."""
-        _check(lib().spectre_kv_init(self._ref, _raw_stream(stream)))
+        _check(lib().spectre_kv_init(self._ref, _now(stream)))
 
     # views of the bookkeeping, on the device
     @property
@@ -681,44 +686,43 @@ class KvPages:
     def table(self):
         return self.book[8 + self.seqs + self.pages:].view(self.seqs, self.max_pages)
 
-    def _scratch(self, need, kind, ws, stream):
-        """The caller's workspace or the pool's own, kept between calls (one for the attention, one for the pages: a pool works on one stream at a time)."""
-        if ws is not None:
-            return _given(ws)
-        own, at = self._ws.get(kind, (None, None))
-        raw = _raw_stream(stream)
-        if own is None or own.numel() < need + 256:
-            own, at = _new((need + 256,), torch.uint8, self.book.device, stream), raw
-            self._ws[kind] = own, at
-        elif raw != at:                    # the allocator must not give its memory away while another stream works with it
+    def _scratch(self, kind, stream, need=0):
+        """(address, bytes) of the pool's workspace, kept between calls (one for the attention, one for the pages: a pool works on one stream at a time)."""
+        own, raw, at, have = self._ws.get(kind, (None, 0, None, 0))
+        now = _now(stream)
+        if have < need:
+            own = _new((need + 256,), torch.uint8, self.book.device, stream)
+            at, have = _given(own)
+            self._ws[kind] = own, now, at, have
+        elif now != raw and own is not None:   # the allocator must not give its memory away while another stream works with it
             own.record_stream(torch.cuda.current_stream() if stream is None else stream)
-        return _given(own)
+        return at, have
 
     def _pages_ws(self, n, ws, stream):
-        return self._scratch(lib().spectre_kv_workspace_bytes(self._ref, n), "pages", ws, stream)
+        return _given(ws) if ws is not None else self._scratch("pages", stream, lib().spectre_kv_workspace_bytes(self._ref, n))
 
     def reserve(self, seqs, add, ws=None, stream=None):
         """Sequence seqs[i] grows by add[i] tokens (int32 on the device); room that is missing is reported in `status`, and then nothing changes."""
         n = seqs.numel()
-        _check(lib().spectre_kv_reserve(self._ref, _ints(seqs, "seqs"), _ints(add, "add", n), n, *self._pages_ws(n, ws, stream), _raw_stream(stream)))
+        _check(lib().spectre_kv_reserve(self._ref, _ints(seqs, "seqs"), _ints(add, "add", n), n, *self._pages_ws(n, ws, stream), _now(stream)))
 
     def fork(self, src, dst, ws=None, stream=None):
         """The empty sequences dst[i] become what src[i] are: full pages shared, the last one copied."""
         n = src.numel()
-        _check(lib().spectre_kv_fork(self._ref, _ints(src, "src"), _ints(dst, "dst", n), n, *self._pages_ws(n, ws, stream), _raw_stream(stream)))
+        _check(lib().spectre_kv_fork(self._ref, _ints(src, "src"), _ints(dst, "dst", n), n, *self._pages_ws(n, ws, stream), _now(stream)))
 
     def free(self, seqs, stream=None):
         """The sequences end; pages that nobody else uses are free."""
-        _check(lib().spectre_kv_free(self._ref, _ints(seqs, "seqs"), seqs.numel(), _raw_stream(stream)))
+        _check(lib().spectre_kv_free(self._ref, _ints(seqs, "seqs"), seqs.numel(), _now(stream)))
 
     def compact(self, ws=None, stream=None):
         """Pages in use move to the front of the pool; status[2] = how many there are."""
-        _check(lib().spectre_kv_compact(self._ref, *self._pages_ws(0, ws, stream), _raw_stream(stream)))
+        _check(lib().spectre_kv_compact(self._ref, *self._pages_ws(0, ws, stream), _now(stream)))
 
     def copy(self, src, dst, stream=None):
         """Contents of page src[i] of every layer to page dst[i]."""
         n = src.numel()
-        _check(lib().spectre_kv_copy(self._ref, _ints(src, "src"), _ints(dst, "dst", n), n, _raw_stream(stream)))
+        _check(lib().spectre_kv_copy(self._ref, _ints(src, "src"), _ints(dst, "dst", n), n, _now(stream)))
 
     def append(self, layer, q, k, v, start, seqs=None, rope=None, wq=None, wk=None, eps=1e-6, q_out=None, stream=None):
         """Norm and rotation of the new tokens' heads; keys and values go into the pages of `layer`, queries are returned.  q [T,H,d], k, v [T,Hkv,d] of the
@@ -734,9 +738,10 @@ class KvPages:
         P = _heads(d, rope, wq, wk, eps)
         if q_out is None:
             q_out = _new((T, H, d), q.dtype, q.device, stream)
-        _same(q_out, q, "q_out")
+        else:
+            _same(q_out, q, "q_out")
         _check(lib().spectre_kv_append(self._ref, layer, ctypes.byref(P), qa, qs, ka, ks, va, vs, _ints(start, "start"),
-                                       None if seqs is None else _ints(seqs, "seqs", B), B, T, H, _ptr(q_out, "q_out"), _raw_stream(stream)))
+                                       None if seqs is None else _ints(seqs, "seqs", B), B, T, H, _ptr(q_out, "q_out"), _now(stream)))
         return q_out
 
     def attend_workspace_bytes(self, B, T, H, max_new, max_len=None, window=0):
@@ -758,14 +763,19 @@ class KvPages:
             max_len = self.max_pages * self.page
         if out is None:
             out = _new((T, H, d), q.dtype, q.device, stream)
-        _same(out, q, "out")
-        if lse is None and want_lse:
-            lse = _new((T, H), torch.float32, q.device, stream)
-        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (T, H)):
+        else:
+            _same(out, q, "out")
+        if lse is None:
+            if want_lse:
+                lse = _new((T, H), torch.float32, q.device, stream)
+        elif lse.dtype != torch.float32 or tuple(lse.shape) != (T, H):
             raise ValueError("lse must be float32 [T, H]")
-        need = 0 if ws is not None else lib().spectre_kv_attend_workspace_bytes(self._ref, B, T, H, max_new, max_len, window)
-        at, have = self._scratch(need, "attend", ws, stream)
-        _check(lib().spectre_kv_attend(self._ref, layer, qa, qs, _ints(start, "start"), None if seqs is None else _ints(seqs, "seqs", B), B, T, H, max_new,
-                                       max_len, 1.0 / d ** 0.5 if scale is None else scale, window, _ptr(out, "out"),
-                                       None if lse is None else _ptr(lse, "lse"), at, have, _raw_stream(stream)))
+        args = (self._ref, layer, qa, qs, _ints(start, "start"), None if seqs is None else _ints(seqs, "seqs", B), B, T, H, max_new, max_len,
+                1.0 / d ** 0.5 if scale is None else scale, window, _ptr(out, "out"), None if lse is None else _ptr(lse, "lse"))
+        at, have = _given(ws) if ws is not None else self._scratch("attend", stream)
+        rc = lib().spectre_kv_attend(*args, at, have, _now(stream))
+        if rc == EWORKSPACE and ws is None:    # the library checks the size; asking for it first is a call of its own
+            at, have = self._scratch("attend", stream, lib().spectre_kv_attend_workspace_bytes(self._ref, B, T, H, max_new, max_len, window))
+            rc = lib().spectre_kv_attend(*args, at, have, _now(stream))
+        _check(rc)
         return (out, lse) if lse is not None else out

@@ -39,6 +39,7 @@ struct AttendK {
     KvView kv;
     AttendArgs a;
     int G, few_rows, splits, tiles, slots;         // slots: parts that a row has room for
+    int part_keys;                                 // of a part of a tile's rows, at least
     float c;                                       // scale * log2(e)
     float *part;                                   // [T * H][slots][d]
     float2 *stat;                                  // [T * H][slots]: maximum in powers of two, sum
@@ -46,6 +47,11 @@ struct AttendK {
 
 struct Seq {
     int from, n, m, row;                           // first new token, new tokens, tokens, row of the table
+    // parts that the keys of a tile's rows are divided into
+    __device__ __forceinline__ int parts(const AttendK &k) const {
+        const int keys = k.a.window ? min(m, k.a.window + n) : m;
+        return max(1, min(k.splits, (keys + k.part_keys - 1) / k.part_keys));
+    }
 };
 __device__ __forceinline__ Seq sequence(const AttendK &k, int b) {
     Seq s;
@@ -180,6 +186,12 @@ __device__ __forceinline__ float max_halves(float x) {
     return larger(__uint_as_float(y[0]), __uint_as_float(y[1]));
 }
 
+// The same for the lane 16 on (within its half).
+__device__ __forceinline__ float max_quarters(float x) {
+    const u32x2_t y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return larger(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+
 __device__ __forceinline__ float lse_of(float top2, float sum) { return sum == 0.f ? -INFINITY : (top2 + log2f(sum)) * 0.69314718055994531f; }
 __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
@@ -203,8 +215,8 @@ __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k
     const int pairs = kv.Hkv * k.a.B, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
     const int h = pair % kv.Hkv, split = rest % k.splits, tile = k.tiles - 1 - rest / k.splits;   // long rows first
     const Seq s = sequence(k, pair / kv.Hkv);
-    const int rows = s.n * k.G, r0 = tile * kTileRows;
-    if (rows <= k.few_rows || r0 >= rows) return;
+    const int rows = s.n * k.G, r0 = tile * kTileRows, parts = s.parts(k);
+    if (rows <= k.few_rows || r0 >= rows || split >= parts) return;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int r = min(r0 + 32 * wave + (lane & 31), rows - 1), token = r / k.G, head = h * k.G + (r - token * k.G);
@@ -216,8 +228,8 @@ __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k
     const int first_pos = p0 + r0 / k.G, last_pos = p0 + min(r0 + kTileRows - 1, rows - 1) / k.G;
     const int wave_first = p0 + min(r0 + 32 * wave, rows - 1) / k.G, wave_last = p0 + min(r0 + 32 * wave + 31, rows - 1) / k.G;
     int t_lo = k.a.window ? max(0, first_pos - k.a.window + 1) / KT : 0, t_hi = last_pos >= 0 ? last_pos / KT + 1 : 0;
-    if (k.splits > 1) {
-        const int per = (max(t_hi - t_lo, 0) + k.splits - 1) / k.splits;
+    if (parts > 1) {
+        const int per = (max(t_hi - t_lo, 0) + parts - 1) / parts;
         t_lo += split * per;
         t_hi = min(t_hi, t_lo + per);
     }
@@ -371,7 +383,7 @@ __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k
     sum += __shfl_xor(sum, 32, 64);
     const long long at = (long long)(s.from + token) * k.a.H + head;
     const float top2 = top * k.c;
-    if (k.splits > 1) {
+    if (parts > 1) {
         if (half == 0) k.stat[at * k.slots + split] = make_float2(top2, sum);
         if (sum == 0.f) return;
         float *to = k.part + (at * k.slots + split) * D;
@@ -391,15 +403,20 @@ __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k
     if (k.a.lse && half == 0) k.a.lse[at] = lse_of(top2, sum);
 }
 
-// ---------------------------------------------------------------- few rows: up to 16 R of a key head, keys split over waves and workgroups
+// ---------------------------------------------------------------- few rows: up to 16 of a key head, keys split over waves and workgroups
+// Every key and value is read once and multiplied with 16 columns of rows, empty ones among them: memory bounds it.  No LDS: a lane's loads are the operands (the
+// layout of the pages), one step of 32 keys (fp32: 16) in registers, of which each half is requested again as soon as it has been used, so that four waves a SIMD
+// keep up to 8 KB (d = 64) each on its way.  (Two steps in turn need twice the registers: 16 sequences of 4000 tokens, d = 128, 36 instead of 29 us.)
+// STREAM: a large pool is read past the memory-side cache, its pages come round again only when every other layer's have.  8 sequences of 32700 tokens, 537 MB:
+// 89 us, 6.0 TB/s (cached 100); 32 of up to 32768, 1.09 GB, 202 us, 5.4 TB/s; a pool of 67 MB would lose (23.1 -> 24.2 us), one of 131 MB gains (33.2 -> 31.1).
 constexpr int kSection = 1024;                     // page numbers in LDS at a time
 
-template <typename IO, int D, int R>
-__global__ __launch_bounds__(256, R * D == 64 ? 3 : R * D == 128 ? 2 : 1) void k_attend_few(AttendK k) {
-    constexpr int E = IO::E, SK = IO::kStepKeys, KTILES = SK / 16, QG = D / (4 * E), DT = D / 16, SD = (R == 2 && D == 128) ? 64 : D, PAD = SD + 4;
+template <typename IO, int D, bool STREAM>
+__global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) {
+    constexpr int E = IO::E, SK = IO::kStepKeys, KTILES = SK / 16, QG = D / (4 * E), DT = D / 16, PAD = D + 4;
     __shared__ int pages[kSection + 2];
-    __shared__ float tops[4][16 * R], sums[4][16 * R];
-    __shared__ float so[4][16 * R][PAD];
+    __shared__ float tops[4][16], sums[4][16];
+    __shared__ float so[4][16][PAD];
     const KvView &kv = k.kv;
     const int pairs = kv.Hkv * k.a.B, pair = blockIdx.x % pairs, split = blockIdx.x / pairs, h = pair % kv.Hkv;
     const Seq s = sequence(k, pair / kv.Hkv);
@@ -407,16 +424,14 @@ __global__ __launch_bounds__(256, R * D == 64 ? 3 : R * D == 128 ? 2 : 1) void k
     if (rows == 0 || rows > k.few_rows) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
     const int p0 = s.m - s.n, mask = (1 << kv.page_log) - 1;
-    int pos[R], from[R];
-    uint4 q[R][QG];
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const int r = min(16 * i + col, rows - 1), token = r / k.G, head = h * k.G + (r - token * k.G);
-        pos[i] = p0 + token;
-        from[i] = k.a.window ? pos[i] - k.a.window : -1;
+    const int token = min(col, rows - 1) / k.G, head = h * k.G + (min(col, rows - 1) - token * k.G);
+    const int pos = p0 + token, lowest = k.a.window ? pos - k.a.window + 1 : 0;              // the row sees the `span` keys from here on
+    const unsigned span = (unsigned)max(pos - lowest + 1, 0);
+    uint4 q[QG];
+    {
         const char *base = reinterpret_cast<const char *>(k.a.q) + ((s.from + token) * k.a.q_stride + head * D) * IO::kBytes;
 #pragma unroll
-        for (int j = 0; j < QG; ++j) q[i][j] = reinterpret_cast<const uint4 *>(base)[4 * j + quarter];
+        for (int j = 0; j < QG; ++j) q[j] = reinterpret_cast<const uint4 *>(base)[4 * j + quarter];
     }
     // this workgroup's keys: whole steps of all waves
     const int lo = k.a.window ? max(0, p0 - k.a.window + 1) & ~63 : 0, hi = s.m;
@@ -425,23 +440,22 @@ __global__ __launch_bounds__(256, R * D == 64 ? 3 : R * D == 128 ? 2 : 1) void k
     const int all_from = k.a.window ? p0 + s.n - 1 - k.a.window : -1;         // every row sees the keys above it ...
     const int all_pos = p0;                                                   // ... up to this one
 
-    f32x4_t o[R][DT];
-    float top[R], sum[R];
+    f32x4_t o[DT];
+    float top = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        top[i] = -INFINITY;
-        sum[i] = 0.f;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[i][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int d = 0; d < DT; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const float lag = kLag / k.c;
-    const uint4 *K = reinterpret_cast<const uint4 *>(kv.k), *V = reinterpret_cast<const uint4 *>(kv.v);
     const int koff = E == 8 ? 8 * (col >> 2) + (col & 3) : col;               // this lane's key of a step (bf16: and the one 4 on)
+    const unsigned page_bytes = (unsigned)kv.Hkv * (D * IO::kBytes) << kv.page_log, head_bytes = (unsigned)h * (D * IO::kBytes) << kv.page_log;
+    const unsigned k_at = head_bytes + ((quarter * 16u) << kv.page_log), k_next = 64u << kv.page_log, v_at = head_bytes + col * 16u;
+    const unsigned P = (unsigned)kv.P;
 
-    struct Step {
-        uint4 k[KTILES * QG], v[DT];
-        int kpage, vpage;
+    auto load = [](const char *p) {
+        if constexpr (STREAM) return __builtin_bit_cast(uint4, stream_load(reinterpret_cast<const float4 *>(p)));
+        else return *reinterpret_cast<const uint4 *>(p);
     };
+    uint4 kr[KTILES * QG], vr[DT];
+    int vpage = -1;
     // sections of keys whose page numbers fit LDS
     const int keys_a_section = kSection << kv.page_log;
     for (int sec = begin; sec < end; sec += keys_a_section) {
@@ -449,157 +463,134 @@ __global__ __launch_bounds__(256, R * D == 64 ? 3 : R * D == 128 ? 2 : 1) void k
         __syncthreads();
         for (int i = threadIdx.x; i < count; i += 256) pages[i] = kv.table[(long long)s.row * kv.M + first + i];
         __syncthreads();
-        auto page_at = [&](int key) {
-            const int p = key < sec_end ? pages[(key >> kv.page_log) - first] : -1;
-            return (unsigned)p < (unsigned)kv.P ? p : -1;
+        auto page_at = [&](int key) { return key < sec_end ? pages[(key >> kv.page_log) - first] : -1; };
+        auto request_keys = [&](int base) {
+            const int key = base + koff, page = page_at(base + (E == 8 ? 8 * (col >> 2) : col));     // keys at and behind the end lie in its page, or in none
+            const char *kb = reinterpret_cast<const char *>(kv.k) + (unsigned long long)(unsigned)page * page_bytes + k_at + (key & mask) * 16u;
+            auto all = [&]() {
+#pragma unroll
+                for (int j = 0; j < QG; ++j)
+#pragma unroll
+                    for (int t = 0; t < KTILES; ++t) kr[t * QG + j] = load(kb + j * k_next + 64 * t);
+            };
+            if (__ballot((unsigned)page < P) == ~0ull) return all();              // nothing to choose, nothing to clear
+#pragma unroll
+            for (int i = 0; i < KTILES * QG; ++i) kr[i] = make_uint4(0, 0, 0, 0);
+            if ((unsigned)page < P) all();
         };
-        auto request = [&](Step &x, int base) {
-            const int key = base + koff, vkey = base + E * quarter;
-            x.kpage = page_at(base + (E == 8 ? 8 * (col >> 2) : col));        // keys at and behind the end lie in its page, or in none
-            x.vpage = page_at(vkey);
-            const long long kb = ((long long)x.kpage * kv.Hkv + h) * (D / E);
-            const uint4 *vb = V + (((long long)x.vpage * kv.Hkv + h) * (D / E) << kv.page_log) + ((vkey & mask) / E) * D + col;
+        auto request_values = [&](int base) {
+            const int key = base + E * quarter;
+            vpage = page_at(key);
+            const char *vb = reinterpret_cast<const char *>(kv.v) + (unsigned long long)(unsigned)vpage * page_bytes + v_at + ((key & mask) / E) * (D * 16u);
+            auto all = [&]() {
 #pragma unroll
-            for (int t = 0; t < KTILES; ++t)
+                for (int d = 0; d < DT; ++d) vr[d] = load(vb + 256 * d);
+            };
+            if (__ballot((unsigned)vpage < P) == ~0ull) return all();
 #pragma unroll
-                for (int j = 0; j < QG; ++j) {
-                    x.k[t * QG + j] = make_uint4(0, 0, 0, 0);
-                    if (x.kpage >= 0) x.k[t * QG + j] = K[((kb + 4 * j + quarter) << kv.page_log) + ((key + 4 * t) & mask)];
-                }
+            for (int d = 0; d < DT; ++d) vr[d] = make_uint4(0, 0, 0, 0);
+            if ((unsigned)vpage < P) all();
+        };
+        // the next step's keys are requested as soon as the scores have used these, its values behind the product with these
+        int base = sec + SK * wave;
+        if (base < sec_end) {
+            request_keys(base);
+            request_values(base);
+        }
+        for (; base < sec_end; base += 4 * SK) {
+            const bool more = base + 4 * SK < sec_end;
+            const bool absent = (unsigned)vpage >= P;                             // this lane's run of E keys, whose scores and values it holds
+            const bool edge = __ballot(absent) != 0 || base + SK - 1 > all_pos || base <= all_from;
+            f32x4_t sc[KTILES];
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                x.v[d] = make_uint4(0, 0, 0, 0);
-                if (x.vpage >= 0) x.v[d] = vb[16 * d];
+            for (int t = 0; t < KTILES; ++t) {
+                sc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < QG; ++j) IO::mma16(sc[t], kr[t * QG + j], q[j]);
             }
-        };
-        auto work = [&](Step &x, int base) {
-            const bool gone = __ballot(x.vpage < 0) != 0;                     // lanes' value pages are all pages of the step
-            const bool edge = gone || base + SK - 1 > all_pos || base <= all_from;
+            if (more) request_keys(base + 4 * SK);
             bool odd = false;
             if (edge) {
+                const unsigned at = (unsigned)(base + E * quarter - lowest);
+#pragma unroll
+                for (int t = 0; t < KTILES; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (absent || at + (4 * t + e) >= span) sc[t][e] = -INFINITY;
                 const int have = s.m - (base + E * quarter);
                 bool fine = true;
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    if (have < E) x.v[d] = keep_first<IO>(x.v[d], have);
-                    if (!all_finite<IO>(x.v[d])) {
+                    if (have < E) vr[d] = keep_first<IO>(vr[d], have);
+                    if (!all_finite<IO>(vr[d])) {
                         fine = false;
-                        x.v[d] = finite_only<IO>(x.v[d]);
+                        vr[d] = finite_only<IO>(vr[d]);
                     }
                 }
                 odd = __ballot(!fine) != 0;
             }
+            float mx = sc[0][0];
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                f32x4_t sc[KTILES];
+            for (int t = 0; t < KTILES; ++t)
 #pragma unroll
-                for (int t = 0; t < KTILES; ++t) {
-                    sc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                for (int e = 0; e < 4; ++e) mx = larger(mx, sc[t][e]);
+            mx = max_halves(max_quarters(mx));
+            if (__ballot(lags(mx, top, lag))) {
+                const float f = follow(mx, k.c, &top);
+                sum *= f;
 #pragma unroll
-                    for (int j = 0; j < QG; ++j) IO::mma16(sc[t], x.k[t * QG + j], q[i][j]);
-                }
-                // lane: keys base + E * quarter + 4 t + e, all of one page (x.vpage)
-                if (edge) {
-#pragma unroll
-                    for (int t = 0; t < KTILES; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int key = base + E * quarter + 4 * t + e;
-                            if (x.vpage < 0 || key > pos[i] || key <= from[i]) sc[t][e] = -INFINITY;
-                        }
-                }
-                float mx = sc[0][0];
-#pragma unroll
-                for (int t = 0; t < KTILES; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[t][e]);
-                mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-                if (__ballot(lags(mx, top[i], lag))) {
-                    const float f = follow(mx, k.c, &top[i]);
-                    sum[i] *= f;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[i][d] *= f;
-                }
-                const float shift = shift_of(top[i], k.c);
-                float p[4 * KTILES];
-#pragma unroll
-                for (int t = 0; t < KTILES; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        p[4 * t + e] = exp2_fast(fmaf(sc[t][e], k.c, shift));
-                        sum[i] += p[4 * t + e];
-                    }
-                const uint4 pg = IO::pack(p);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) IO::mma16(o[i][d], x.v[d], pg);
-                if (odd) {
-                    add_not_finite<IO, D, 4 * DT>(kv, s, h, base, SK, pos[i], from[i], [quarter](int n) { return 16 * (n / 4) + 4 * quarter + n % 4; },
-                                                  [&](int n, float y) { o[i][n / 4][n % 4] += y; });
-                }
+                for (int d = 0; d < DT; ++d) o[d] *= f;
             }
-        };
-        // two steps' registers in turn: one on its way from memory while the other is worked on
-        Step a, b;
-        int base = sec + SK * wave;
-        if (base < sec_end) request(a, base);
-        for (; base < sec_end; base += 8 * SK) {
-            const bool second = base + 4 * SK < sec_end;
-            if (second) request(b, base + 4 * SK);
-            work(a, base);
-            if (base + 8 * SK < sec_end) request(a, base + 8 * SK);
-            if (second) work(b, base + 4 * SK);
+            const float shift = shift_of(top, k.c);
+            float p[4 * KTILES];
+#pragma unroll
+            for (int t = 0; t < KTILES; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[4 * t + e] = exp2_fast(fmaf(sc[t][e], k.c, shift));
+                    sum += p[4 * t + e];
+                }
+            const uint4 pg = IO::pack(p);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) IO::mma16(o[d], vr[d], pg);
+            if (more) request_values(base + 4 * SK);
+            if (odd)
+                add_not_finite<IO, D, 4 * DT>(kv, s, h, base, SK, pos, lowest - 1, [quarter](int n) { return 16 * (n / 4) + 4 * quarter + n % 4; },
+                                              [&](int n, float y) { o[n / 4][n % 4] += y; });
         }
     }
 
     // the waves' results, joined in a fixed order
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-        sum[i] += __shfl_xor(sum[i], 16, 64);
-        sum[i] += __shfl_xor(sum[i], 32, 64);
-        if (quarter == 0) {
-            tops[wave][16 * i + col] = top[i];
-            sums[wave][16 * i + col] = sum[i];
-        }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (quarter == 0) {
+        tops[wave][col] = top;
+        sums[wave][col] = sum;
     }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_t *>(&so[wave][col][16 * d + 4 * quarter]) = o[d];
     __syncthreads();
+    for (int x = threadIdx.x; x < rows * (D / 4); x += 256) {
+        const int r = x / (D / 4), c = 4 * (x % (D / 4));
+        float best = tops[0][r], total = 0.f;
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        float best = tops[0][16 * i + col];
+        for (int w = 1; w < 4; ++w) best = fmaxf(best, tops[w][r]);
+        f32x4_t y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 1; w < 4; ++w) best = fmaxf(best, tops[w][16 * i + col]);
-        const float f = top[i] == best ? 1.f : exp2_fast((top[i] - best) * k.c);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[i][d] *= f;
-    }
-    for (int d0 = 0; d0 < D; d0 += SD) {
-        if (d0) __syncthreads();
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-                if (16 * d >= d0 && 16 * d < d0 + SD) *reinterpret_cast<f32x4_t *>(&so[wave][16 * i + col][16 * d - d0 + 4 * quarter]) = o[i][d];
-        __syncthreads();
-        for (int x = threadIdx.x; x < rows * (SD / 4); x += 256) {
-            const int r = x / (SD / 4), c = 4 * (x % (SD / 4));
-            float best = -INFINITY, total = 0.f;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) best = fmaxf(best, tops[w][r]);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) total += sums[w][r] * (tops[w][r] == best ? 1.f : exp2_fast((tops[w][r] - best) * k.c));
-            f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < 4; ++w) y += *reinterpret_cast<const f32x4_t *>(&so[w][r][c]);
-            const int token = r / k.G, head = h * k.G + (r - token * k.G);
-            const long long at = (long long)(s.from + token) * k.a.H + head;
-            if (k.splits > 1) {
-                *reinterpret_cast<f32x4_t *>(k.part + (at * k.slots + split) * D + d0 + c) = y;
-                if (d0 + c == 0) k.stat[at * k.slots + split] = make_float2(best * k.c, total);
-            } else {
-                const float inv = inverse(total);
-                store4<IO>(k.a.out, at * D + d0 + c, make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv));
-                if (k.a.lse && d0 + c == 0) k.a.lse[at] = lse_of(best * k.c, total);
-            }
+        for (int w = 0; w < 4; ++w) {
+            const float f = tops[w][r] == best ? 1.f : exp2_fast((tops[w][r] - best) * k.c);
+            total += f * sums[w][r];
+            y += f * *reinterpret_cast<const f32x4_t *>(&so[w][r][c]);
+        }
+        const int token = r / k.G, head = h * k.G + (r - token * k.G);
+        const long long at = (long long)(s.from + token) * k.a.H + head;
+        if (k.splits > 1) {
+            *reinterpret_cast<f32x4_t *>(k.part + (at * k.slots + split) * D + c) = y;
+            if (c == 0) k.stat[at * k.slots + split] = make_float2(best * k.c, total);
+        } else {
+            const float inv = inverse(total);
+            store4<IO>(k.a.out, at * D + c, make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv));
+            if (k.a.lse && c == 0) k.a.lse[at] = lse_of(best * k.c, total);
         }
     }
 }
@@ -608,7 +599,7 @@ __global__ __launch_bounds__(256, R * D == 64 ? 3 : R * D == 128 ? 2 : 1) void k
 // D / 4 lanes hold a row's channels; GROUPS such groups of a workgroup share the splits of one row.  Many rows have a group each; few rows (and then many
 // splits) a workgroup each, where what counts is that all loads are on their way at once.
 template <typename IO, int D, int GROUPS>
-__global__ __launch_bounds__(256) void k_attend_join(AttendK k, int few_splits, int tile_splits) {
+__global__ __launch_bounds__(256) void k_attend_join(AttendK k, int few_splits, int tile_splits) {    // k.splits = tile_splits
     constexpr int LANES = D / 4, ROWS = 256 / (LANES * GROUPS);
     __shared__ f32x4_t so[GROUPS > 1 ? GROUPS : 1][LANES];
     __shared__ float2 st[GROUPS > 1 ? GROUPS : 1];
@@ -617,16 +608,17 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendK k, int few_splits, 
     int splits = 0;
     if (row < rows) {
         const int t = (int)(row / k.a.H);
-        if (few_splits && tile_splits) {           // which kernel had the row depends on its sequence, the last one with start <= t
+        splits = few_splits;
+        if (tile_splits) {                         // the row's sequence, the last one with start <= t, says which kernel had it, and in how many parts
             int lo = 0, hi = k.a.B;
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
                 if (k.a.start[mid] <= t) lo = mid;
                 else hi = mid;
             }
-            const int n = k.a.start[lo + 1] - k.a.start[lo];
-            splits = (long long)n * k.G <= k.few_rows ? few_splits : tile_splits;
-        } else splits = few_splits + tile_splits;
+            const Seq s = sequence(k, lo);
+            if ((long long)s.n * k.G > k.few_rows) splits = s.parts(k);
+        }
         if (t >= k.a.start[k.a.B] || splits == 1) splits = 0;
     }
     const float2 *stat = k.stat + row * k.slots;
@@ -683,6 +675,7 @@ constexpr long long kWideRows = 4096;
 // Where the sequences differ, the longest must not be one workgroup's work for as long as the others take together; every part costs its rows once through
 // memory: 32 sequences of up to 512 new and 8500 tokens in all take 315 us with parts of 4096 keys, 334 with 2048, 394 with 1024, 401 undivided.
 constexpr long long kRaggedKeys = 4096;
+constexpr long long kStreamBytes = 96ll << 20;
 
 AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new, int max_len, int window) {
     AttendPlan p{};
@@ -690,14 +683,19 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
     const long long rows = (long long)max_new * G;
     const bool even = T == (long long)B * max_new;                 // every sequence has max_new tokens
     const long long len = window ? std::min<long long>(max_len, (long long)window + max_new) : max_len;
-    p.few = rows <= 32 || (!even && G <= 16);
-    p.tile = rows > 32;
+    // Up to 16 rows need no tile.  Beyond, one tile does for the few rows of a mixed batch too (23 sequences of up to 5 tokens, 8 heads a key head: 39 instead of 73 us) until
+    // the tiles of the others make it long.
+    p.few = rows <= 16 || (!even && G <= 16 && rows > 128);
+    p.tile = rows > 16;
     p.few_rows = !p.few ? 0 : p.tile ? 16 : (int)rows;
     p.few_splits = p.tile_splits = 1;
     const long long pairs = (long long)B * Hkv;
     if (p.few) {
-        long long s = std::max((1024 + pairs - 1) / pairs, (len + 2047) / 2048);
-        s = std::min(s, (len + 127) / 128);
+        // two workgroups a compute unit of at least 256 keys each: four of 128 cost the join what they gain (one sequence of 32700 tokens 21.9 instead of
+        // 19.8 us, 64 of 2000, which need no join then, 48 instead of 43), one leaves the memory waiting (16 fp32 sequences of 4000: 52.7 instead of 47.5).
+        // No part longer than 2048 keys, for sequences of different lengths (32 of up to 32768: 202 us, with 4096 205).
+        long long s = std::max((512 + pairs - 1) / pairs, (len + 2047) / 2048);
+        s = std::min(s, (len + 255) / 256);
         p.few_splits = (int)std::max(1ll, std::min(s, 256ll));
     }
     if (p.tile) {
@@ -711,21 +709,22 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
         p.tiles = (int)((rows + 32 * p.tile_waves - 1) / (32 * p.tile_waves));
         // workgroups that run at once, by their registers and LDS; keys are split where rows leave some of them free
         const long long slots = p.tile_waves == 8 || d == 128 ? 512 : io == SPECTRE_BF16 ? 1024 : 768;
-        long long s = slots / groups(p.tile_waves);
-        if (!even) s = std::max(s, (len + kRaggedKeys - 1) / kRaggedKeys);
-        p.tile_splits = (int)std::max(1ll, std::min({s, len / 256, 64ll}));
+        const long long s = std::min(slots / groups(p.tile_waves), len / 256), ragged = even ? 1 : (len + kRaggedKeys - 1) / kRaggedKeys;
+        p.part_keys = s >= ragged ? 256 : (int)kRaggedKeys;
+        p.tile_splits = (int)std::max(1ll, std::min(std::max(s, ragged), 64ll));
     }
     const int most = std::max(p.few_splits, p.tile_splits);
     if (most > 1) p.partial_bytes = (size_t)T * H * most * ((size_t)d * 4 + 8);
     return p;
 }
 
-hipError_t launch_attend(const KvView &kv, int d, int io, const AttendArgs &a, const AttendPlan &p, void *ws, hipStream_t st) {
+hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const AttendArgs &a, const AttendPlan &p, void *ws, hipStream_t st) {
     AttendK k;
     k.kv = kv;
     k.a = a;
     k.G = a.H / kv.Hkv;
     k.few_rows = p.few_rows;
+    k.part_keys = p.part_keys;
     k.tiles = p.tiles;
     k.c = a.scale * kLog2E;
     const size_t most = std::max(p.few_splits, p.tile_splits);
@@ -741,9 +740,10 @@ hipError_t launch_attend(const KvView &kv, int d, int io, const AttendArgs &a, c
     if (p.few) {
         k.splits = p.few_splits;
         const int blocks = pairs * p.few_splits;
+        const bool stream = 2 * kv.layer_bytes * layers > kStreamBytes;
 #define CALL(IO, D)                                                                        \
-    if (p.few_rows <= 16) k_attend_few<IO, D, 1><<<blocks, 256, 0, st>>>(k);               \
-    else k_attend_few<IO, D, 2><<<blocks, 256, 0, st>>>(k)
+    if (stream) k_attend_few<IO, D, true><<<blocks, 256, 0, st>>>(k);                      \
+    else k_attend_few<IO, D, false><<<blocks, 256, 0, st>>>(k)
         SPECTRE_ATTEND_DISPATCH(CALL)
 #undef CALL
         hipError_t e = hipGetLastError();
@@ -763,6 +763,7 @@ hipError_t launch_attend(const KvView &kv, int d, int io, const AttendArgs &a, c
     if (p.few_splits > 1 || p.tile_splits > 1) {
         const long long rows = (long long)a.T * a.H;
         const int few = p.few ? p.few_splits : 0, tile = p.tile ? p.tile_splits : 0;
+        k.splits = tile;
 #define CALL(IO, D)                                                                                                             \
     if (rows <= kWideRows) k_attend_join<IO, D, 1024 / D><<<(int)rows, 256, 0, st>>>(k, few, tile);                             \
     else k_attend_join<IO, D, 1><<<(int)((rows + 1024 / D - 1) / (1024 / D)), 256, 0, st>>>(k, few, tile)

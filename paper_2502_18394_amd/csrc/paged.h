@@ -62,7 +62,7 @@ hipError_t launch_kv_copy(const KvView &kv, int layers, const int *src, const in
 struct AttendPlan {
     int few, tile;                   // whether each kernel is launched
     int few_rows;                    // rows (new tokens x heads of a key head) that the kernel of few rows takes, 0 if it is not launched
-    int few_splits, tile_splits, tiles, tile_waves;
+    int few_splits, tile_splits, tiles, tile_waves, part_keys;
     size_t partial_bytes;            // of all rows' split results
 };
 struct AttendArgs {
@@ -75,6 +75,6 @@ struct AttendArgs {
     float *lse;
 };
 AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new, int max_len, int window);
-hipError_t launch_attend(const KvView &kv, int d, int io, const AttendArgs &a, const AttendPlan &p, void *ws, hipStream_t st);
+hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const AttendArgs &a, const AttendPlan &p, void *ws, hipStream_t st);
 
 }  // namespace spectre

@@ -280,7 +280,7 @@ int spectre_kv_attend(const spectre_kv *kv, int layer, const void *q, long long 
     const AttendPlan p = attend_plan(kv->d, (int)kv->dtype, B, T, H, kv->Hkv, max_new, max_len, window);
     if (p.partial_bytes && (rc = check_ws(ws, ws_bytes, align256(p.partial_bytes + 1), who))) return rc;
     const AttendArgs a = {q, q_stride, start, seqs, B, T, H, window, scale, out, lse};
-    return done(launch_attend(kv_view(kv, layer), kv->d, (int)kv->dtype, a, p, ws, static_cast<hipStream_t>(stream)), who);
+    return done(launch_attend(kv_view(kv, layer), kv->layers, kv->d, (int)kv->dtype, a, p, ws, static_cast<hipStream_t>(stream)), who);
 }
 
 }  // extern "C"
