@@ -31,8 +31,10 @@ constexpr float kLog2E = 1.4426950408889634f;
 constexpr float kLag = 8.f;
 
 // 16 bytes a lane from its address into LDS, lane after lane from `to` on (the same in every lane of the wave).
+template <bool STREAM>
 __device__ __forceinline__ void to_lds(const void *from, uint4 *to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+    constexpr int kNonTemporal = STREAM ? 2 : 0;
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, kNonTemporal);
 }
 
 struct AttendK {
@@ -40,6 +42,7 @@ struct AttendK {
     AttendArgs a;
     int G, few_rows, splits, tiles, slots;         // slots: parts that a row has room for
     int part_keys;                                 // of a part of a tile's rows, at least
+    bool stream;                                   // tiles are read past the memory-side cache
     float c;                                       // scale * log2(e)
     float *part;                                   // [T * H][slots][d]
     float2 *stat;                                  // [T * H][slots]: maximum in powers of two, sum
@@ -269,14 +272,19 @@ __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k
         const char *kb = reinterpret_cast<const char *>(kv.k) + (unsigned long long)(unsigned)page * page_bytes + (k_at + ((t * KT + (lane & (KT - 1))) & mask) * 16u);
         if ((unsigned)page < P) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) to_lds(kb + i * k_next, to_k + 64 * wave + THREADS * i);
+            for (int i = 0; i < PER; ++i) {
+                if (k.stream) to_lds<true>(kb + i * k_next, to_k + 64 * wave + THREADS * i);
+                else to_lds<false>(kb + i * k_next, to_k + 64 * wave + THREADS * i);
+            }
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int kg = (64 * wave + THREADS * i) / D * E;
             const unsigned p = (unsigned)__builtin_amdgcn_readlane(page, kg);
             const char *vb = reinterpret_cast<const char *>(kv.v) + (unsigned long long)p * page_bytes + (((t * KT + kg) & mask) / E) * (D * 16u);
-            if (p < P) to_lds(vb + v_at, to_v + 64 * wave + THREADS * i);
+            if (p >= P) continue;
+            if (k.stream) to_lds<true>(vb + v_at, to_v + 64 * wave + THREADS * i);
+            else to_lds<false>(vb + v_at, to_v + 64 * wave + THREADS * i);
         }
     };
     if (threadIdx.x < 2) odd[threadIdx.x] = -1;
@@ -709,9 +717,13 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
         p.tiles = (int)((rows + 32 * p.tile_waves - 1) / (32 * p.tile_waves));
         // workgroups that run at once, by their registers and LDS; keys are split where rows leave some of them free
         const long long slots = p.tile_waves == 8 || d == 128 ? 512 : io == SPECTRE_BF16 ? 1024 : 768;
-        const long long s = std::min(slots / groups(p.tile_waves), len / 256), ragged = even ? 1 : (len + kRaggedKeys - 1) / kRaggedKeys;
-        p.part_keys = s >= ragged ? 256 : (int)kRaggedKeys;
-        p.tile_splits = (int)std::max(1ll, std::min(std::max(s, ragged), 64ll));
+        // Parts of the longest sequence; the others' parts are as long.  With several tiles a sequence of a ragged batch they take different times, and
+        // twice the parts even them out (fp32 batch of up to 397 new tokens 135 instead of 142 us; single tiles, bound by memory, lose: 25.0 -> 28.8).
+        long long s = std::max(1ll, (even || rows <= 128 ? 1 : 2) * slots / groups(p.tile_waves));
+        if (!even) s = std::max(s, (len + kRaggedKeys - 1) / kRaggedKeys);
+        s = std::max(1ll, std::min({s, len / 256, 64ll}));
+        p.part_keys = (int)((len + s - 1) / s);
+        p.tile_splits = (int)s;
     }
     const int most = std::max(p.few_splits, p.tile_splits);
     if (most > 1) p.partial_bytes = (size_t)T * H * most * ((size_t)d * 4 + 8);
@@ -731,6 +743,8 @@ hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const Atte
     k.slots = (int)most;
     k.part = (float *)ws;
     k.stat = (float2 *)((char *)ws + (size_t)a.T * a.H * most * d * 4);
+    const bool stream = 2 * kv.layer_bytes * layers > kStreamBytes;
+    k.stream = stream && p.tiles == 1;             // with several tiles of rows a tile of keys is read as often
     const int pairs = a.B * kv.Hkv;
 #define SPECTRE_ATTEND_DISPATCH(CALL)                                 \
     if (io == SPECTRE_BF16 && d == 64) { CALL(Bf16Mma, 64); }         \
@@ -740,7 +754,6 @@ hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const Atte
     if (p.few) {
         k.splits = p.few_splits;
         const int blocks = pairs * p.few_splits;
-        const bool stream = 2 * kv.layer_bytes * layers > kStreamBytes;
 #define CALL(IO, D)                                                                        \
     if (stream) k_attend_few<IO, D, true><<<blocks, 256, 0, st>>>(k);                      \
     else k_attend_few<IO, D, false><<<blocks, 256, 0, st>>>(k)
