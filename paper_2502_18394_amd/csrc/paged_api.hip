@@ -10,6 +10,8 @@
 namespace spectre {
 namespace {
 
+constexpr int kLongest = SPECTRE_KV_MAX_TABLE * 256;   // tokens that a sequence can have
+
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -86,7 +88,7 @@ int check_layer(const spectre_kv *kv, int layer, const char *who) {
 
 int check_batch(const spectre_kv *kv, const int *start, int B, int T, int H, const char *who) {
     if (!start) return fail(SPECTRE_EINVAL, "%s: null start", who);
-    if (B < 1 || T < 0 || H < 1) return fail(SPECTRE_EINVAL, "%s: T below 0, or B or H below 1", who);
+    if (B < (T > 0) || T < 0 || H < 1) return fail(SPECTRE_EINVAL, "%s: T below 0, or B or H below 1", who);
     if (B > kv->seqs) return fail(SPECTRE_EINVAL, "%s: %d sequences, the table has %d", who, B, kv->seqs);
     if (H % kv->Hkv) return fail(SPECTRE_EINVAL, "%s: %d heads do not divide among %d key heads", who, H, kv->Hkv);
     if (H > 65536) return fail(SPECTRE_EUNSUPPORTED, "%s: %d heads", who, H);
@@ -96,10 +98,10 @@ int check_batch(const spectre_kv *kv, const int *start, int B, int T, int H, con
 int done(hipError_t e, const char *who) { return e == hipSuccess ? SPECTRE_OK : fail_hip(e, who); }
 
 int check_attend(const spectre_kv *kv, int B, int T, int H, int max_new, int max_len, int window, const char *who) {
-    if (B < 1 || T < 0 || H < 1 || H % kv->Hkv) return fail(SPECTRE_EINVAL, "%s: B, T or H", who);
+    if (B < (T > 0) || T < 0 || H < 1 || H % kv->Hkv) return fail(SPECTRE_EINVAL, "%s: B, T or H", who);
     if (max_new < 1 || max_len < 1 || window < 0) return fail(SPECTRE_EINVAL, "%s: max_new or max_len below 1, or window below 0", who);
     const long long rows = (long long)max_new * (H / kv->Hkv), tiles = (rows + 127) / 128;
-    if (rows > INT_MAX || tiles * B * kv->Hkv > (1 << 24) || (long long)B * kv->Hkv > (1 << 22) || (long long)T * H > (1ll << 31))
+    if (rows > INT_MAX || tiles * B * kv->Hkv > (1 << 24) || (long long)B * kv->Hkv > (1 << 22) || (long long)T * H > INT_MAX)
         return fail(SPECTRE_EUNSUPPORTED, "%s: %d sequences of %d new tokens, %d heads", who, B, max_new, H);
     return SPECTRE_OK;
 }
@@ -260,6 +262,7 @@ int spectre_kv_append(const spectre_kv *kv, int layer, const spectre_heads *P, c
 
 size_t spectre_kv_attend_workspace_bytes(const spectre_kv *kv, int B, int T, int H, int max_new, int max_len, int window) {
     if (check_sizes(kv, "kv_attend") || check_attend(kv, B, T, H, max_new, max_len, window, "kv_attend")) return 0;
+    if (window >= kLongest) window = 0;
     return align256(attend_plan(kv->d, (int)kv->dtype, B, T, H, kv->Hkv, max_new, max_len, window).partial_bytes + 1);
 }
 
@@ -271,7 +274,9 @@ int spectre_kv_attend(const spectre_kv *kv, int layer, const void *q, long long 
     if ((rc = check_layer(kv, layer, who))) return rc;
     if ((rc = check_batch(kv, start, B, T, H, who))) return rc;
     if ((rc = check_attend(kv, B, T, H, max_new, max_len, window, who))) return rc;
-    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(SPECTRE_EINVAL, "%s: scale is not above zero", who);
+    // statistics are kept in powers of two: scale and its inverse have to leave them their range
+    if (!(scale >= 1e-30f && scale <= 1e30f)) return fail(SPECTRE_EINVAL, "%s: scale is not between 1e-30 and 1e30", who);
+    if (window >= kLongest) window = 0;                 // sees everything there can be
     if (T == 0) return SPECTRE_OK;
     const Span x = {q, q_stride, H, "q"};
     if ((rc = check_rows(x, kv->d, kv->dtype, who))) return rc;

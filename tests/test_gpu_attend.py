@@ -116,6 +116,37 @@ def test_keys_split_over_workgroups(io, d, n):
         check(out, lse, q, [n], rows, d ** -0.5, DT[io], window)
 
 
+@pytest.mark.parametrize("io,d,page", [("bf16", 64, 64), ("bf16", 128, 16), ("f32", 64, 32), ("f32", 128, 128), ("bf16", 64, 16)])
+@pytest.mark.parametrize("window", [0, 333])
+def test_many_rows_of_many_heads(io, d, page, window):
+    """Batches with work for every compute unit, which have wider tiles: queries picked at random and at the ends, absent pages, NaN and infinities where rows
+    do not see them."""
+    print(f"case {io} d={d} page={page} window={window}", flush=True)
+    news, lens, H, Hkv = [700, 1, 513, 0, 640, 600, 700, 255], [900, 77, 513, 40, 1000, 601, 700, 300], 32, 16
+    pool, rows = make(io, d, Hkv, page, lens, page + d)
+    for value in (float("nan"), float("inf")):                 # the last token but one of two sequences
+        s = 4 if value == value else 0
+        at = lens[s] - 2
+        number, slot, E = int(pool.table[s, at // page]), at % page, ref.per_group(DT[io])
+        pool.v_pages[0, number, :, slot // E, 7, slot % E] = value
+    pool.table[6, 2] = -1
+    there = np.ones(700, bool)
+    there[2 * page:3 * page] = False
+    q, start = queries(news, H, d, io, 3)
+    out, lse = pool.attend(0, q, start, max_new=700, max_len=1000, window=window, want_lse=True)
+    pick = np.random.default_rng(5)
+    for b, (n, m) in enumerate(zip(news, lens)):
+        last = n - 2 if b in (0, 4) else n                      # the last two rows of these see what is not finite
+        for i in sorted({0, n // 2, last - 1, *pick.integers(0, max(last, 1), 6)}) if n else []:
+            at, p = int(start[b]) + int(i), m - n + int(i)
+            alive = [there[:p + 1]] if b == 6 else None
+            check(out[at:at + 1], lse[at:at + 1], q[at:at + 1], [1], [(rows[b][0][:p + 1], rows[b][1][:p + 1])], d ** -0.5, DT[io], window, alive)
+        if b in (0, 4):
+            seen = out[int(start[b]) + n - 2:int(start[b]) + n, :, 7].float()
+            assert not torch.isfinite(seen).any()
+            assert torch.isfinite(out[int(start[b]):int(start[b]) + n - 2]).all()
+
+
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("n", [1, 6, 50])
 def test_bounds_that_are_wide_or_missing(io, n):
@@ -222,6 +253,32 @@ def test_strided_queries_other_streams_and_the_same_bits(n):
     given = torch.empty(pool.attend_workspace_bytes(2, 2 * n, 4, n, 700) + 256, dtype=torch.uint8, device="cuda")
     into = torch.full_like(out, 7.0)
     assert torch.equal(pool.attend(0, q, start, max_new=n, max_len=700, ws=given, out=into), out) and torch.equal(into, out)
+
+
+@pytest.mark.parametrize("n", [1, 70])
+def test_the_widest_window_is_none(n):
+    pool, rows = make("f32", 64, 1, 16, [300, 70], 2)
+    q, start = queries([n, n], 4, 64, "f32", 5)
+    want = pool.attend(0, q, start, max_new=n, max_len=300, want_lse=True)
+    for window in (300, 2 ** 28, 2 ** 31 - 1):
+        out, lse = pool.attend(0, q, start, max_new=n, max_len=300, window=window, want_lse=True)
+        check(out, lse, q, [n, n], rows, 0.125, torch.float32)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def test_nothing_to_do():
+    pool, _ = make("bf16", 64, 2, 16, [30, 5], 2)
+    q = torch.empty(0, 4, 64, dtype=torch.bfloat16, device="cuda")
+    none = torch.zeros(3, dtype=torch.int32, device="cuda")
+    before = pool.book.clone()
+    for start in (none, none[:1]):
+        out, lse = pool.attend(0, q, start, want_lse=True)
+        assert out.shape == (0, 4, 64) and lse.shape == (0, 4)
+        assert pool.append(0, q, q[:, :2], q[:, :2], start).shape == (0, 4, 64)
+    pool.reserve(none[:0], none[:0])
+    pool.fork(none[:0], none[:0])
+    pool.free(none[:0])
+    assert torch.equal(pool.book, before)
 
 
 def test_rows_behind_the_last_sequence_are_left_alone():

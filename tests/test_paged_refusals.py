@@ -121,7 +121,7 @@ def test_batches_that_are_refused(lib):
     for bad in (dict(layer=2), dict(layer=-1), dict(start=None), dict(B=0), dict(B=5), dict(T=-1), dict(H=3), dict(H=0), dict(q=None), dict(out=None), dict(qs=128),
                 dict(out=FAKE), dict(k=FAR + 4)):
         assert append(**bad) == 1, bad
-    assert append(T=0, q=None) == 0
+    assert append(T=0, q=None) == 0 and append(T=0, B=0, q=None) == 0
     assert lib.spectre_kv_append(c, 0, ctypes.byref(heads(d=128, rot=0)), FAKE, 256, FAR, 128, FAR, 128, FAKE, None, 1, 3, 4, OUT, None) == 1
 
     def attend(layer=0, q=FAKE, qs=256, start=FAKE, B=2, T=3, H=4, new=3, most=300, scale=0.125, window=0, out=OUT, ws=FAKE, size=big):
@@ -131,7 +131,9 @@ def test_batches_that_are_refused(lib):
                       (dict(scale=0.0), 1), (dict(scale=-1.0), 1), (dict(scale=float("nan")), 1), (dict(scale=float("inf")), 1), (dict(q=None), 1), (dict(out=None), 1),
                       (dict(out=FAKE + 16), 1), (dict(qs=250), 1), (dict(ws=None), 3), (dict(size=64), 3), (dict(new=1 << 30), 2), (dict(T=-2), 1)):
         assert attend(**bad) == code, bad
-    assert attend(T=0, q=None, out=None, ws=None) == 0
+    assert attend(T=0, q=None, out=None, ws=None) == 0 and attend(T=0, B=0, q=None, out=None, ws=None) == 0
+    assert attend(scale=1e-31) == 1 and attend(scale=1e31) == 1
+    assert attend(T=1 << 29, B=4, H=4, new=1) == 2                       # more rows than an int counts
     assert lib.spectre_kv_attend_workspace_bytes(c, 2, 3, 5, 3, 300, 0) == 0
     assert lib.spectre_kv_attend_workspace_bytes(c, 2, 3, 4, 3, 300, 0) > 3 * 4 * 64 * 4
 
