@@ -40,9 +40,11 @@ __device__ __forceinline__ void to_lds(const void *from, uint4 *to) {
 struct AttendK {
     KvView kv;
     AttendArgs a;
-    int G, few_rows, splits, tiles, slots;         // slots: parts that a row has room for
+    int G, tiles, few_rows;                        // heads of a key head; tiles of a sequence; the rows up to which a sequence is the business of `few`
+    int few_splits, tile_splits, slots;            // parts of a sequence's keys, at most; parts that a row has room for
     int part_keys;                                 // of a part of a tile's rows, at least
-    bool stream;                                   // tiles are read past the memory-side cache
+    int few_blocks, tile_blocks;                   // workgroups of each kind, where both are in one launch
+    bool few_stream, tile_stream;                  // pages are read past the memory-side cache
     float c;                                       // scale * log2(e)
     float *part;                                   // [T * H][slots][d]
     float2 *stat;                                  // [T * H][slots]: maximum in powers of two, sum
@@ -53,7 +55,7 @@ struct Seq {
     // parts that the keys of a tile's rows are divided into
     __device__ __forceinline__ int parts(const AttendK &k) const {
         const int keys = k.a.window ? min(m, k.a.window + n) : m;
-        return max(1, min(k.splits, (keys + k.part_keys - 1) / k.part_keys));
+        return max(1, min(k.tile_splits, (keys + k.part_keys - 1) / k.part_keys));
     }
 };
 __device__ __forceinline__ Seq sequence(const AttendK &k, int b) {
@@ -67,6 +69,11 @@ __device__ __forceinline__ Seq sequence(const AttendK &k, int b) {
     else s.row = 0;
     return s;
 }
+
+// Which sequence and key head a workgroup works on: all of them in turn, for each `rest` (tile, part) turned on by eight.  Eight keep a pair on one XCD, whose L2 then has its
+// keys; without the turn the workgroups of a long sequence come at a fixed distance, often a multiple of what an XCD deals out at a time, and
+// land on the same few compute units (24 ragged sequences, d = 128: 302 instead of 137 us).
+__device__ __forceinline__ int turned_pair(int block, int rest, int pairs) { return (int)((block - (long long)rest * pairs + 8ll * rest) % pairs); }
 
 struct Bf16Mma {
     static constexpr int E = 8, kBytes = 2;
@@ -208,15 +215,22 @@ __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 
 // An 8192-token prompt, 32 heads: 315 us, 872 TFLOP/s (all-zero inputs, which draw less power, 289); 2048 tokens over 28672 558 us, 892 TFLOP/s.
 // Measured and not taken: two sets of 32 rows a wave (half the LDS reads, two waves a SIMD: 4 % slower), scores of the next tile formed between the steps of this tile's
 // softmax within a wave (17 % slower), two tiles a barrier (3 % slower), raised priority around the products (no difference), tiles through registers (4 % slower).
+template <typename IO, int D>
+constexpr int kTileGroups = IO::kTileKeys * D / IO::E;
+struct TileLds {
+    uint4 *sk0, *sv0, *sk1, *sv1;                   // kTileGroups each, arrays of their own: the compiler sees which loads a read need not wait for
+    int *odd;                                       // [2] the last tile whose values were not all finite
+};
+
 template <typename IO, int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k_attend_tile(AttendK k) {
+__device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLds lds) {
     constexpr int THREADS = 64 * WAVES, kTileRows = 32 * WAVES;
-    constexpr int E = IO::E, KT = IO::kTileKeys, NK = KT / 32, GROUPS = KT * D / E, PER = GROUPS / THREADS, QG = D / (2 * E), DT = D / 32;
-    __shared__ uint4 sk0[GROUPS], sv0[GROUPS], sk1[GROUPS], sv1[GROUPS];      // of their own each: the compiler sees which loads a read need not wait for
-    __shared__ int odd[2];                          // the last tile whose values were not all finite
+    constexpr int E = IO::E, KT = IO::kTileKeys, NK = KT / 32, GROUPS = kTileGroups<IO, D>, PER = GROUPS / THREADS, QG = D / (2 * E), DT = D / 32;
+    uint4 *const sk0 = lds.sk0, *const sv0 = lds.sv0, *const sk1 = lds.sk1, *const sv1 = lds.sv1;
+    int *const odd = lds.odd;
     const KvView &kv = k.kv;
-    const int pairs = kv.Hkv * k.a.B, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-    const int h = pair % kv.Hkv, split = rest % k.splits, tile = k.tiles - 1 - rest / k.splits;   // long rows first
+    const int pairs = kv.Hkv * k.a.B, rest = block / pairs, pair = turned_pair(block, rest, pairs);
+    const int h = pair % kv.Hkv, split = rest % k.tile_splits, tile = k.tiles - 1 - rest / k.tile_splits;   // long rows first
     const Seq s = sequence(k, pair / kv.Hkv);
     const int rows = s.n * k.G, r0 = tile * kTileRows, parts = s.parts(k);
     if (rows <= k.few_rows || r0 >= rows || split >= parts) return;
@@ -273,7 +287,7 @@ __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k
         if ((unsigned)page < P) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                if (k.stream) to_lds<true>(kb + i * k_next, to_k + 64 * wave + THREADS * i);
+                if (k.tile_stream) to_lds<true>(kb + i * k_next, to_k + 64 * wave + THREADS * i);
                 else to_lds<false>(kb + i * k_next, to_k + 64 * wave + THREADS * i);
             }
         }
@@ -283,7 +297,7 @@ __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k
             const unsigned p = (unsigned)__builtin_amdgcn_readlane(page, kg);
             const char *vb = reinterpret_cast<const char *>(kv.v) + (unsigned long long)p * page_bytes + (((t * KT + kg) & mask) / E) * (D * 16u);
             if (p >= P) continue;
-            if (k.stream) to_lds<true>(vb + v_at, to_v + 64 * wave + THREADS * i);
+            if (k.tile_stream) to_lds<true>(vb + v_at, to_v + 64 * wave + THREADS * i);
             else to_lds<false>(vb + v_at, to_v + 64 * wave + THREADS * i);
         }
     };
@@ -415,18 +429,24 @@ __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k
 // Every key and value is read once and multiplied with 16 columns of rows, empty ones among them: memory bounds it.  No LDS: a lane's loads are the operands (the
 // layout of the pages), one step of 32 keys (fp32: 16) in registers, of which each half is requested again as soon as it has been used, so that four waves a SIMD
 // keep up to 8 KB (d = 64) each on its way.  (Two steps in turn need twice the registers: 16 sequences of 4000 tokens, d = 128, 36 instead of 29 us.)
-// STREAM: a large pool is read past the memory-side cache, its pages come round again only when every other layer's have.  8 sequences of 32700 tokens, 537 MB:
-// 89 us, 6.0 TB/s (cached 100); 32 of up to 32768, 1.09 GB, 202 us, 5.4 TB/s; a pool of 67 MB would lose (23.1 -> 24.2 us), one of 131 MB gains (33.2 -> 31.1).
-constexpr int kSection = 1024;                     // page numbers in LDS at a time
+// A large pool is read past the memory-side cache, its pages come round again only when every other layer's have.  8 sequences of 32700 tokens, 537 MB:
+// 89 us, 6.0 TB/s (cached 100); 32 of up to 32768, 1.09 GB, 185 us, 5.9 TB/s; a pool of 67 MB would lose (23.1 -> 24.2 us), one of 131 MB gains (33.2 -> 31.1).
+constexpr int kSection = 256;                      // page numbers in LDS at a time
 
-template <typename IO, int D, bool STREAM>
-__global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) {
-    constexpr int E = IO::E, SK = IO::kStepKeys, KTILES = SK / 16, QG = D / (4 * E), DT = D / 16, PAD = D + 4;
-    __shared__ int pages[kSection + 2];
-    __shared__ float tops[4][16], sums[4][16];
-    __shared__ float so[4][16][PAD];
+template <typename IO, int D>
+constexpr int kFewGroups = 16 * D / 4;              // of a wave's 16 rows of outputs
+struct FewLds {
+    int *pages;                                     // [kSection + 2]
+    float (*tops)[16], (*sums)[16];                 // [waves][16]
+    f32x4_t *out0, *out1, *out2, *out3;             // kFewGroups for every fourth wave each
+};
+
+template <typename IO, int D, int WAVES>
+__device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds) {
+    constexpr int E = IO::E, SK = IO::kStepKeys, KTILES = SK / 16, QG = D / (4 * E), DT = D / 16, THREADS = 64 * WAVES;
+    int *const pages = lds.pages;
     const KvView &kv = k.kv;
-    const int pairs = kv.Hkv * k.a.B, pair = blockIdx.x % pairs, split = blockIdx.x / pairs, h = pair % kv.Hkv;
+    const int pairs = kv.Hkv * k.a.B, split = block / pairs, pair = turned_pair(block, split, pairs), h = pair % kv.Hkv;
     const Seq s = sequence(k, pair / kv.Hkv);
     const int rows = s.n * k.G;
     if (rows == 0 || rows > k.few_rows) return;
@@ -443,7 +463,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) 
     }
     // this workgroup's keys: whole steps of all waves
     const int lo = k.a.window ? max(0, p0 - k.a.window + 1) & ~63 : 0, hi = s.m;
-    const int chunk = ((max(hi - lo, 0) + k.splits - 1) / k.splits + 4 * SK - 1) / (4 * SK) * (4 * SK);
+    const int chunk = ((max(hi - lo, 0) + k.few_splits - 1) / k.few_splits + WAVES * SK - 1) / (WAVES * SK) * (WAVES * SK);
     const int begin = min(lo + (long long)split * chunk, (long long)hi), end = min(hi, begin + chunk);
     const int all_from = k.a.window ? p0 + s.n - 1 - k.a.window : -1;         // every row sees the keys above it ...
     const int all_pos = p0;                                                   // ... up to this one
@@ -458,8 +478,8 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) 
     const unsigned k_at = head_bytes + ((quarter * 16u) << kv.page_log), k_next = 64u << kv.page_log, v_at = head_bytes + col * 16u;
     const unsigned P = (unsigned)kv.P;
 
-    auto load = [](const char *p) {
-        if constexpr (STREAM) return __builtin_bit_cast(uint4, stream_load(reinterpret_cast<const float4 *>(p)));
+    auto load = [](const char *p, auto stream) {
+        if constexpr (decltype(stream)::value) return __builtin_bit_cast(uint4, stream_load(reinterpret_cast<const float4 *>(p)));
         else return *reinterpret_cast<const uint4 *>(p);
     };
     uint4 kr[KTILES * QG], vr[DT];
@@ -469,35 +489,43 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) 
     for (int sec = begin; sec < end; sec += keys_a_section) {
         const int sec_end = min(end, sec + keys_a_section), first = sec >> kv.page_log, count = ((sec_end - 1) >> kv.page_log) - first + 1;
         __syncthreads();
-        for (int i = threadIdx.x; i < count; i += 256) pages[i] = kv.table[(long long)s.row * kv.M + first + i];
+        for (int i = threadIdx.x; i < count; i += THREADS) pages[i] = kv.table[(long long)s.row * kv.M + first + i];
         __syncthreads();
         auto page_at = [&](int key) { return key < sec_end ? pages[(key >> kv.page_log) - first] : -1; };
         auto request_keys = [&](int base) {
             const int key = base + koff, page = page_at(base + (E == 8 ? 8 * (col >> 2) : col));     // keys at and behind the end lie in its page, or in none
             const char *kb = reinterpret_cast<const char *>(kv.k) + (unsigned long long)(unsigned)page * page_bytes + k_at + (key & mask) * 16u;
-            auto all = [&]() {
+            auto all = [&](auto stream) {
 #pragma unroll
                 for (int j = 0; j < QG; ++j)
 #pragma unroll
-                    for (int t = 0; t < KTILES; ++t) kr[t * QG + j] = load(kb + j * k_next + 64 * t);
+                    for (int t = 0; t < KTILES; ++t) kr[t * QG + j] = load(kb + j * k_next + 64 * t, stream);
             };
-            if (__ballot((unsigned)page < P) == ~0ull) return all();              // nothing to choose, nothing to clear
+            if (__ballot((unsigned)page < P) == ~0ull) {                          // nothing to choose, nothing to clear
+                if (k.few_stream) all(std::true_type());
+                else all(std::false_type());
+                return;
+            }
 #pragma unroll
             for (int i = 0; i < KTILES * QG; ++i) kr[i] = make_uint4(0, 0, 0, 0);
-            if ((unsigned)page < P) all();
+            if ((unsigned)page < P) all(std::false_type());
         };
         auto request_values = [&](int base) {
             const int key = base + E * quarter;
             vpage = page_at(key);
             const char *vb = reinterpret_cast<const char *>(kv.v) + (unsigned long long)(unsigned)vpage * page_bytes + v_at + ((key & mask) / E) * (D * 16u);
-            auto all = [&]() {
+            auto all = [&](auto stream) {
 #pragma unroll
-                for (int d = 0; d < DT; ++d) vr[d] = load(vb + 256 * d);
+                for (int d = 0; d < DT; ++d) vr[d] = load(vb + 256 * d, stream);
             };
-            if (__ballot((unsigned)vpage < P) == ~0ull) return all();
+            if (__ballot((unsigned)vpage < P) == ~0ull) {
+                if (k.few_stream) all(std::true_type());
+                else all(std::false_type());
+                return;
+            }
 #pragma unroll
             for (int d = 0; d < DT; ++d) vr[d] = make_uint4(0, 0, 0, 0);
-            if ((unsigned)vpage < P) all();
+            if ((unsigned)vpage < P) all(std::false_type());
         };
         // the next step's keys are requested as soon as the scores have used these, its values behind the product with these
         int base = sec + SK * wave;
@@ -505,8 +533,8 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) 
             request_keys(base);
             request_values(base);
         }
-        for (; base < sec_end; base += 4 * SK) {
-            const bool more = base + 4 * SK < sec_end;
+        for (; base < sec_end; base += WAVES * SK) {
+            const bool more = base + WAVES * SK < sec_end;
             const bool absent = (unsigned)vpage >= P;                             // this lane's run of E keys, whose scores and values it holds
             const bool edge = __ballot(absent) != 0 || base + SK - 1 > all_pos || base <= all_from;
             f32x4_t sc[KTILES];
@@ -516,7 +544,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) 
 #pragma unroll
                 for (int j = 0; j < QG; ++j) IO::mma16(sc[t], kr[t * QG + j], q[j]);
             }
-            if (more) request_keys(base + 4 * SK);
+            if (more) request_keys(base + WAVES * SK);
             bool odd = false;
             if (edge) {
                 const unsigned at = (unsigned)(base + E * quarter - lowest);
@@ -561,7 +589,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) 
             const uint4 pg = IO::pack(p);
 #pragma unroll
             for (int d = 0; d < DT; ++d) IO::mma16(o[d], vr[d], pg);
-            if (more) request_values(base + 4 * SK);
+            if (more) request_values(base + WAVES * SK);
             if (odd)
                 add_not_finite<IO, D, 4 * DT>(kv, s, h, base, SK, pos, lowest - 1, [quarter](int n) { return 16 * (n / 4) + 4 * quarter + n % 4; },
                                               [&](int n, float y) { o[n / 4][n % 4] += y; });
@@ -572,27 +600,36 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) 
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
     if (quarter == 0) {
-        tops[wave][col] = top;
-        sums[wave][col] = sum;
+        lds.tops[wave][col] = top;
+        lds.sums[wave][col] = sum;
     }
+    // rows turned, no two in one bank; every pointer by its name, so that accesses stay LDS accesses
+    auto place = [&](int w, int r, int c) { return (w >> 2) * kFewGroups<IO, D> + r * (D / 4) + (c ^ r); };
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_t *>(&so[wave][col][16 * d + 4 * quarter]) = o[d];
+    for (int d = 0; d < DT; ++d) {
+        const int at = place(wave, col, 4 * d + quarter), which = wave & 3;
+        if (which == 0) lds.out0[at] = o[d];
+        else if (which == 1) lds.out1[at] = o[d];
+        else if (which == 2) lds.out2[at] = o[d];
+        else lds.out3[at] = o[d];
+    }
     __syncthreads();
-    for (int x = threadIdx.x; x < rows * (D / 4); x += 256) {
+    for (int x = threadIdx.x; x < rows * (D / 4); x += THREADS) {
         const int r = x / (D / 4), c = 4 * (x % (D / 4));
-        float best = tops[0][r], total = 0.f;
+        float best = lds.tops[0][r], total = 0.f;
 #pragma unroll
-        for (int w = 1; w < 4; ++w) best = fmaxf(best, tops[w][r]);
+        for (int w = 1; w < WAVES; ++w) best = fmaxf(best, lds.tops[w][r]);
         f32x4_t y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = tops[w][r] == best ? 1.f : exp2_fast((tops[w][r] - best) * k.c);
-            total += f * sums[w][r];
-            y += f * *reinterpret_cast<const f32x4_t *>(&so[w][r][c]);
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = lds.tops[w][r] == best ? 1.f : exp2_fast((lds.tops[w][r] - best) * k.c);
+            const int at = place(w, r, c / 4);
+            total += f * lds.sums[w][r];
+            y += f * ((w & 3) == 0 ? lds.out0[at] : (w & 3) == 1 ? lds.out1[at] : (w & 3) == 2 ? lds.out2[at] : lds.out3[at]);
         }
         const int token = r / k.G, head = h * k.G + (r - token * k.G);
         const long long at = (long long)(s.from + token) * k.a.H + head;
-        if (k.splits > 1) {
+        if (k.few_splits > 1) {
             *reinterpret_cast<f32x4_t *>(k.part + (at * k.slots + split) * D + c) = y;
             if (c == 0) k.stat[at * k.slots + split] = make_float2(best * k.c, total);
         } else {
@@ -603,11 +640,44 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) 
     }
 }
 
+// ---------------------------------------------------------------- the launches: either kind, or both for a mixed batch
+template <typename IO, int D>
+__global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) {
+    __shared__ int pages[kSection + 2];
+    __shared__ float tops[4][16], sums[4][16];
+    __shared__ f32x4_t outs[4][kFewGroups<IO, D>];
+    few_rows<IO, D, 4>(k, blockIdx.x, FewLds{pages, tops, sums, outs[0], outs[1], outs[2], outs[3]});
+}
+
+template <typename IO, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k_attend_tile(AttendK k) {
+    __shared__ uint4 sk0[kTileGroups<IO, D>], sv0[kTileGroups<IO, D>], sk1[kTileGroups<IO, D>], sv1[kTileGroups<IO, D>];
+    __shared__ int odd[2];
+    tile_of_rows<IO, D, WAVES>(k, blockIdx.x, TileLds{sk0, sv0, sk1, sv1, odd});
+}
+
+// The tiles of a batch's prompts, which arithmetic bounds, and behind them its single tokens, which memory bounds, where the tiles leave compute units free (before
+// them, or dealt out evenly: 32 ragged sequences 258 and 261 instead of 234 us; two launches 310).
+template <typename IO, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k_attend_mixed(AttendK k) {
+    __shared__ uint4 sk0[kTileGroups<IO, D>], sv0[kTileGroups<IO, D>], sk1[kTileGroups<IO, D>], sv1[kTileGroups<IO, D>];
+    __shared__ int odd[2], pages[kSection + 2];
+    __shared__ float tops[WAVES][16], sums[WAVES][16];
+    static_assert(kTileGroups<IO, D> >= (WAVES / 4) * kFewGroups<IO, D>, "outputs of few rows fit where tiles lie");
+    const int tiles = (k.tile_blocks + 7) & ~7, block = blockIdx.x;              // eights again, for the XCDs
+    if (block >= tiles) {
+        few_rows<IO, D, WAVES>(k, block - tiles, FewLds{pages, tops, sums, reinterpret_cast<f32x4_t *>(sk0), reinterpret_cast<f32x4_t *>(sv0), reinterpret_cast<f32x4_t *>(sk1),
+                                                        reinterpret_cast<f32x4_t *>(sv1)});
+    } else if (block < k.tile_blocks) {
+        tile_of_rows<IO, D, WAVES>(k, block, TileLds{sk0, sv0, sk1, sv1, odd});
+    }
+}
+
 // ---------------------------------------------------------------- splits joined
 // D / 4 lanes hold a row's channels; GROUPS such groups of a workgroup share the splits of one row.  Many rows have a group each; few rows (and then many
 // splits) a workgroup each, where what counts is that all loads are on their way at once.
 template <typename IO, int D, int GROUPS>
-__global__ __launch_bounds__(256) void k_attend_join(AttendK k, int few_splits, int tile_splits) {    // k.splits = tile_splits
+__global__ __launch_bounds__(256) void k_attend_join(AttendK k, int few_splits, int tile_splits) {    // 0: not launched
     constexpr int LANES = D / 4, ROWS = 256 / (LANES * GROUPS);
     __shared__ f32x4_t so[GROUPS > 1 ? GROUPS : 1][LANES];
     __shared__ float2 st[GROUPS > 1 ? GROUPS : 1];
@@ -681,7 +751,8 @@ hipError_t load_kernels_attend() {
 // (the first form gave every row a wave).
 constexpr long long kWideRows = 4096;
 // Where the sequences differ, the longest must not be one workgroup's work for as long as the others take together; every part costs its rows once through
-// memory: 32 sequences of up to 512 new and 8500 tokens in all take 315 us with parts of 4096 keys, 334 with 2048, 394 with 1024, 401 undivided.
+// memory: 32 sequences of up to 512 new and 8500 tokens in all take 237 us with parts of 4096 keys, 245 with 2048, 248 with 8192.  Batches of many times more
+// tiles than run at once even out by themselves: 48 of up to 2000 new tokens 825 with 8192, 887 with 4096.
 constexpr long long kRaggedKeys = 4096;
 constexpr long long kStreamBytes = 96ll << 20;
 
@@ -719,8 +790,9 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
         const long long slots = p.tile_waves == 8 || d == 128 ? 512 : io == SPECTRE_BF16 ? 1024 : 768;
         // Parts of the longest sequence; the others' parts are as long.  With several tiles a sequence of a ragged batch they take different times, and
         // twice the parts even them out (fp32 batch of up to 397 new tokens 135 instead of 142 us; single tiles, bound by memory, lose: 25.0 -> 28.8).
-        long long s = std::max(1ll, (even || rows <= 128 ? 1 : 2) * slots / groups(p.tile_waves));
-        if (!even) s = std::max(s, (len + kRaggedKeys - 1) / kRaggedKeys);
+        const long long all = groups(p.tile_waves), keys = all > 4 * slots ? 2 * kRaggedKeys : kRaggedKeys;
+        long long s = std::max(1ll, (even || rows <= 128 ? 1 : 2) * slots / all);
+        if (!even) s = std::max(s, (len + keys - 1) / keys);
         s = std::max(1ll, std::min({s, len / 256, 64ll}));
         p.part_keys = (int)((len + s - 1) / s);
         p.tile_splits = (int)s;
@@ -744,39 +816,41 @@ hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const Atte
     k.part = (float *)ws;
     k.stat = (float2 *)((char *)ws + (size_t)a.T * a.H * most * d * 4);
     const bool stream = 2 * kv.layer_bytes * layers > kStreamBytes;
-    k.stream = stream && p.tiles == 1;             // with several tiles of rows a tile of keys is read as often
+    k.few_splits = p.few_splits;
+    k.tile_splits = p.tile_splits;
+    k.few_stream = stream;
+    k.tile_stream = stream && p.tiles == 1;        // with several tiles of rows a tile of keys is read as often
     const int pairs = a.B * kv.Hkv;
+    k.few_blocks = pairs * p.few_splits;
+    k.tile_blocks = pairs * p.tile_splits * p.tiles;
 #define SPECTRE_ATTEND_DISPATCH(CALL)                                 \
     if (io == SPECTRE_BF16 && d == 64) { CALL(Bf16Mma, 64); }         \
     else if (io == SPECTRE_BF16) { CALL(Bf16Mma, 128); }              \
     else if (d == 64) { CALL(F32Mma, 64); }                           \
     else { CALL(F32Mma, 128); }
-    if (p.few) {
-        k.splits = p.few_splits;
-        const int blocks = pairs * p.few_splits;
+    if (p.few && p.tile) {
+        const int blocks = ((k.tile_blocks + 7) & ~7) + k.few_blocks;
 #define CALL(IO, D)                                                                        \
-    if (stream) k_attend_few<IO, D, true><<<blocks, 256, 0, st>>>(k);                      \
-    else k_attend_few<IO, D, false><<<blocks, 256, 0, st>>>(k)
+    if (p.tile_waves == 8) k_attend_mixed<IO, D, 8><<<blocks, 512, 0, st>>>(k);            \
+    else k_attend_mixed<IO, D, 4><<<blocks, 256, 0, st>>>(k)
         SPECTRE_ATTEND_DISPATCH(CALL)
 #undef CALL
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    if (p.tile) {
-        k.splits = p.tile_splits;
-        const int blocks = pairs * p.tile_splits * p.tiles;
-#define CALL(IO, D)                                                                        \
-    if (p.tile_waves == 8) k_attend_tile<IO, D, 8><<<blocks, 512, 0, st>>>(k);             \
-    else k_attend_tile<IO, D, 4><<<blocks, 256, 0, st>>>(k)
+    } else if (p.few) {
+#define CALL(IO, D) k_attend_few<IO, D><<<k.few_blocks, 256, 0, st>>>(k)
         SPECTRE_ATTEND_DISPATCH(CALL)
 #undef CALL
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+    } else {
+#define CALL(IO, D)                                                                        \
+    if (p.tile_waves == 8) k_attend_tile<IO, D, 8><<<k.tile_blocks, 512, 0, st>>>(k);      \
+    else k_attend_tile<IO, D, 4><<<k.tile_blocks, 256, 0, st>>>(k)
+        SPECTRE_ATTEND_DISPATCH(CALL)
+#undef CALL
     }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     if (p.few_splits > 1 || p.tile_splits > 1) {
         const long long rows = (long long)a.T * a.H;
         const int few = p.few ? p.few_splits : 0, tile = p.tile ? p.tile_splits : 0;
-        k.splits = tile;
 #define CALL(IO, D)                                                                                                             \
     if (rows <= kWideRows) k_attend_join<IO, D, 1024 / D><<<(int)rows, 256, 0, st>>>(k, few, tile);                             \
     else k_attend_join<IO, D, 1><<<(int)((rows + 1024 / D - 1) / (1024 / D)), 256, 0, st>>>(k, few, tile)
