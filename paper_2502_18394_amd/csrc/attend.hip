@@ -169,7 +169,12 @@ __device__ __forceinline__ void add_not_finite(const KvView &kv, const Seq &s, i
 #pragma unroll
         for (int r = 0; r < N; ++r) {
             const float x = IO::value(v[channel(r) * IO::E]);
-            if (!isfinite(x)) add(r, x);
+            if constexpr (N > 32) {
+                // one condition at a time: 64 pairs of scalar registers are taken from the loop around otherwise (its addresses then live in lanes of a
+                // vector register: 540 instead of 499 us for 2048 rows over 28672, d = 128; with 32 channels a lane the plain form is the faster one)
+                add(r, isfinite(x) ? 0.f : x);
+                __builtin_amdgcn_sched_barrier(0);
+            } else if (!isfinite(x)) add(r, x);
         }
     }
 }
@@ -212,9 +217,13 @@ __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 
 // What bounds it at d = 64: per 64 keys and 32 rows a wave issues 16 products (32 clocks each on the matrix cores) and about 130 vector instructions
 // that cannot be saved (32 each of scale-and-shift, 2^x, sum; 16 each of maximum and packing), 2^x taking two slots.  Measured on their own in that proportion with their
 // LDS reads, products and vector work overlap only in part: 26.5 ns a product, against 17.5 for products alone and 15.7 for the rest alone.  The kernel takes 35.
-// An 8192-token prompt, 32 heads: 315 us, 872 TFLOP/s (all-zero inputs, which draw less power, 289); 2048 tokens over 28672 558 us, 892 TFLOP/s.
+// An 8192-token prompt, 32 heads: 308 us, 893 TFLOP/s (all-zero inputs, which draw less power, take 13 % less); 2048 tokens over 28672 544 us, 916 TFLOP/s.
+// At d = 128 there are twice the products for the same vector work, two waves a SIMD: the same prompt with 16 heads 279 us, 986 TFLOP/s, the same chunk 494 us,
+// 1009 TFLOP/s.  A large matrix product of the library reaches 1326.
+// Where a page holds a whole tile its address is scalar work and the lanes' offsets stay the same from tile to tile; pages of less than a tile give every lane its
+// own address (which took 614 us where this took 540: 2048 over 28672, d = 128, pages of 64).
 // Measured and not taken: two sets of 32 rows a wave (half the LDS reads, two waves a SIMD: 4 % slower), scores of the next tile formed between the steps of this tile's
-// softmax within a wave (17 % slower), two tiles a barrier (3 % slower), raised priority around the products (no difference), tiles through registers (4 % slower).
+// softmax within a wave (17 % slower, d = 128 1 % faster), two tiles a barrier (3 % slower), raised priority around the products (no difference), tiles through registers (4 % slower).
 template <typename IO, int D>
 constexpr int kTileGroups = IO::kTileKeys * D / IO::E;
 struct TileLds {
@@ -278,63 +287,123 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
     const unsigned P = (unsigned)kv.P;
     // bytes of a page, and of this head and thread inside one: a 64-bit product a lane (keys) or a wave (values), 32-bit sums for the rest
     const unsigned page_bytes = (unsigned)kv.Hkv * (D * IO::kBytes) << kv.page_log, head_bytes = (unsigned)h * (D * IO::kBytes) << kv.page_log;
-    const unsigned k_at = head_bytes + ((threadIdx.x / KT * 16u) << kv.page_log), v_at = head_bytes + threadIdx.x % D * 16u;
-    const unsigned k_next = ((unsigned)THREADS / KT * 16u) << kv.page_log;
+    const unsigned k_at = (threadIdx.x / KT * 16u) << kv.page_log, k_lane = k_at + (lane & (KT - 1)) * 16u;
+    const char *const k_head = reinterpret_cast<const char *>(kv.k) + head_bytes, *const v_head = reinterpret_cast<const char *>(kv.v) + head_bytes;
     // Groups of a tile straight from memory into LDS, in the order they have there: a wave's 64 lanes write 1 KB from its first group on.  Absent keys leave
     // what lies there.
-    auto request = [&](int t, int page, uint4 *to_k, uint4 *to_v) {
-        const char *kb = reinterpret_cast<const char *>(kv.k) + (unsigned long long)(unsigned)page * page_bytes + (k_at + ((t * KT + (lane & (KT - 1))) & mask) * 16u);
-        if ((unsigned)page < P) {
+    const bool one_page = (1 << kv.page_log) >= KT;                          // a tile lies in one page: its address is scalar work
+    auto copy_keys = [&](const char *kb, unsigned off, uint4 *to, auto stream) {
+        unsigned k_next = ((unsigned)THREADS / KT * 16u) << kv.page_log;
+        int wave_now = wave;
+        asm volatile("" : "+s"(k_next), "+s"(wave_now));                      // opaque: its multiples are not kept in registers from tile to tile
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                if (k.tile_stream) to_lds<true>(kb + i * k_next, to_k + 64 * wave + THREADS * i);
-                else to_lds<false>(kb + i * k_next, to_k + 64 * wave + THREADS * i);
-            }
+        for (int i = 0; i < PER; ++i) to_lds<decltype(stream)::value>(kb + i * k_next + off, to + 64 * wave_now + THREADS * i);
+    };
+    auto copy_values = [&](const char *vb, uint4 *to, auto stream) {
+        int wave_now = wave;
+        asm volatile("" : "+s"(wave_now));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) to_lds<decltype(stream)::value>(vb + i * (THREADS * 16u) + threadIdx.x * 16u, to + 64 * wave_now + THREADS * i);
+    };
+    auto request_keys = [&](int t, int page, uint4 *to) {
+        if (one_page) {
+            const unsigned p = (unsigned)__builtin_amdgcn_readfirstlane(page);
+            if (p >= P) return;
+            const char *kb = k_head + (unsigned long long)p * page_bytes + ((t * KT) & mask) * 16u;
+            if (k.tile_stream) copy_keys(kb, k_lane, to, std::true_type());
+            else copy_keys(kb, k_lane, to, std::false_type());
+            return;
         }
-#pragma unroll
+        if ((unsigned)page >= P) return;
+        const char *kb = k_head + (unsigned long long)(unsigned)page * page_bytes + (k_at + ((t * KT + (lane & (KT - 1))) & mask) * 16u);
+        if (k.tile_stream) copy_keys(kb, 0u, to, std::true_type());
+        else copy_keys(kb, 0u, to, std::false_type());
+    };
+    auto request_values = [&](int t, int page, uint4 *to) {
+        if (one_page) {
+            const unsigned p = (unsigned)__builtin_amdgcn_readfirstlane(page);
+            if (p >= P) return;
+            const char *vb = v_head + (unsigned long long)p * page_bytes + ((t * KT) & mask) / E * (D * 16u);
+            if (k.tile_stream) copy_values(vb, to, std::true_type());
+            else copy_values(vb, to, std::false_type());
+            return;
+        }
+        int wave_now = wave;
+        asm volatile("" : "+s"(wave_now));
+#pragma unroll 1
         for (int i = 0; i < PER; ++i) {
-            const int kg = (64 * wave + THREADS * i) / D * E;
+            const int kg = (64 * wave_now + THREADS * i) / D * E;
             const unsigned p = (unsigned)__builtin_amdgcn_readlane(page, kg);
-            const char *vb = reinterpret_cast<const char *>(kv.v) + (unsigned long long)p * page_bytes + (((t * KT + kg) & mask) / E) * (D * 16u);
-            if (p >= P) continue;
-            if (k.tile_stream) to_lds<true>(vb + v_at, to_v + 64 * wave + THREADS * i);
-            else to_lds<false>(vb + v_at, to_v + 64 * wave + THREADS * i);
+            const char *vb = v_head + (unsigned long long)p * page_bytes + (((t * KT + kg) & mask) / E) * (D * 16u);
+            if (p < P) to_lds<false>(vb + threadIdx.x % D * 16u, to + 64 * wave_now + THREADS * i);
         }
     };
-    if (threadIdx.x < 2) odd[threadIdx.x] = -1;
-    int page = page_of(t_lo), next = page_of(t_lo + 1);
-    if (t_lo < t_hi) request(t_lo, page, sk0, sv0);
-    const int krow = IO::key_of_row(lane & 31);
-
-    auto tile_step = [&](int t, uint4 *sk, uint4 *sv, uint4 *next_k, uint4 *next_v, int *flag) {
-        const unsigned long long there = __ballot((unsigned)page < P);      // bit = key of the tile (fp32: twice 32 keys)
-        const bool edge = there != ~0ull || t * KT + KT - 1 > first_pos || t * KT <= last_pos - (k.a.window ? k.a.window : last_pos + 1);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                     // this wave's part of the tile has arrived ...
-        __syncthreads();                                                    // ... and everybody's, and nobody reads the other buffer any more
-        page = next;
-        if (t + 1 < t_hi) {
-            request(t + 1, page, next_k, next_v);
-            next = page_of(t + 2);
-        }
-        if (edge) {                                                 // values of no one's keys, and those that are not finite
-            bool fine = true;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int kg = (64 * wave + THREADS * i) / D * E;
-                uint4 x = sv[threadIdx.x + THREADS * i];
-                x = keep_first<IO>(x, ((there >> kg) & 1) ? s.m - (t * KT + kg) : 0);
-                if (!all_finite<IO>(x)) {
-                    fine = false;
-                    x = finite_only<IO>(x);
-                }
-                sv[threadIdx.x + THREADS * i] = x;
+    auto arrived = [&]() {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                     // this wave's part has arrived ...
+        __syncthreads();                                                    // ... and everybody's, and nobody reads the other buffers any more
+    };
+    const int back = k.a.window ? k.a.window : 1 << 30;
+    // Tile t's values of no one's keys, and those that are not finite, where rows of the workgroup see different keys.
+    auto clean = [&](int t, unsigned long long there, uint4 *sv, int *flag) {
+        if (there == ~0ull && t * KT + KT - 1 <= first_pos && t * KT > last_pos - back) return;
+        bool fine = true;
+#pragma unroll 1
+        for (int i = 0; i < PER; ++i) {
+            const int kg = (64 * wave + THREADS * i) / D * E;
+            uint4 x = sv[threadIdx.x + THREADS * i];
+            x = keep_first<IO>(x, ((there >> kg) & 1) ? s.m - (t * KT + kg) : 0);
+            if (!all_finite<IO>(x)) {
+                fine = false;
+                x = finite_only<IO>(x);
             }
-            if (!fine) *flag = t;
-            __syncthreads();
+            sv[threadIdx.x + THREADS * i] = x;
         }
-        if (!busy || t * KT > wave_last) return;
-
-        f32x16_t sc[NK];
+        if (!fine) *flag = t;
+        __syncthreads();
+    };
+    // Scores that the row does not see are replaced.
+    auto hide = [&](int t, unsigned long long there, f32x16_t(&sc)[NK]) {
+        if (there == ~0ull && t * KT + KT - 1 <= wave_first && t * KT > wave_last - back) return;
+        const unsigned at0 = (unsigned)(t * KT + IO::kHalf * half - lowest);
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (at0 + (32 * n + IO::key_of_acc(i)) >= span) sc[n][i] = -INFINITY;
+        if (there != ~0ull) {                                           // pages that are not there
+            const unsigned long long mates = there >> (IO::kHalf * half);
+#pragma unroll
+            for (int n = 0; n < NK; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {                              // by bits: conditions would want a pair of scalar registers each
+                    const int gone = (int)(~(unsigned)(mates >> (32 * n + IO::key_of_acc(i))) << 31) >> 31;
+                    sc[n][i] = __int_as_float((__float_as_int(sc[n][i]) & ~gone) | ((int)0xff800000 & gone));
+                }
+        }
+    };
+    auto largest = [&](const f32x16_t(&sc)[NK]) {
+        float mx = sc[0][0];
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = larger(mx, sc[n][i]);
+        return mx;
+    };
+    auto keep_up = [&](float mx) {                                      // with the maximum mx of a tile's scores, of both halves
+        if (!__ballot(lags(mx, top, lag))) return;
+        const float f = follow(mx, k.c, &top);
+        sum *= f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= f;
+    };
+    auto add_odd = [&](int t) {
+        add_not_finite<IO, D, 16 * DT>(kv, s, h, t * KT, KT, pos, lowest - 1, [half](int i) { return 32 * (i / 16) + 8 * ((i % 16) / 4) + 4 * half + i % 4; },
+                                       [&](int i, float x) { o[i / 16][i % 16] += x; });
+    };
+    const int krow = IO::key_of_row(lane & 31);
+    auto scores = [&](const uint4 *sk, f32x16_t(&sc)[NK]) {
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
 #pragma unroll
@@ -346,37 +415,28 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
 #pragma unroll
             for (int i = 0; i < QG; ++i) IO::mma32(sc[n], a[i], q[i]);
         }
-        const bool some = there != ~0ull || t * KT + KT - 1 > wave_first || t * KT <= wave_last - (k.a.window ? k.a.window : wave_last + 1);
-        if (some) {
-            const unsigned at0 = (unsigned)(t * KT + IO::kHalf * half - lowest);
-#pragma unroll
-            for (int n = 0; n < NK; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (at0 + (32 * n + IO::key_of_acc(i)) >= span) sc[n][i] = -INFINITY;
-            if (there != ~0ull) {                                   // pages that are not there
-                const unsigned long long mates = there >> (IO::kHalf * half);
-#pragma unroll
-                for (int n = 0; n < NK; ++n)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!((mates >> (32 * n + IO::key_of_acc(i))) & 1)) sc[n][i] = -INFINITY;
-            }
+    };
+    if (threadIdx.x < 2) odd[threadIdx.x] = -1;
+    int page = page_of(t_lo), next = page_of(t_lo + 1);
+    if (t_lo < t_hi) {
+        request_keys(t_lo, page, sk0);
+        request_values(t_lo, page, sv0);
+    }
+    auto tile_step = [&](int t, uint4 *sk, uint4 *sv, uint4 *next_k, uint4 *next_v, int *flag) {
+        const unsigned long long there = __ballot((unsigned)page < P);      // bit = key of the tile (fp32: twice 32 keys)
+        arrived();
+        page = next;
+        if (t + 1 < t_hi) {
+            request_keys(t + 1, page, next_k);
+            request_values(t + 1, page, next_v);
+            next = page_of(t + 2);
         }
-        float mx = sc[0][0];
-#pragma unroll
-        for (int n = 0; n < NK; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mx = larger(mx, sc[n][i]);
-        mx = max_halves(mx);
-        if (__ballot(lags(mx, top, lag))) {
-            const float f = follow(mx, k.c, &top);
-            sum *= f;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= f;
-        }
+        clean(t, there, sv, flag);
+        if (!busy || t * KT > wave_last) return;
+        f32x16_t sc[NK];
+        scores(sk, sc);
+        hide(t, there, sc);
+        keep_up(max_halves(largest(sc)));
         const float shift = shift_of(top, k.c);
         float p[NK * 16];
 #pragma unroll
@@ -392,10 +452,7 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
 #pragma unroll
             for (int d = 0; d < DT; ++d) IO::mma32(o[d], sv[(2 * g + half) * D + 32 * d + (lane & 31)], pg);
         }
-        if (*flag == t) {
-            add_not_finite<IO, D, 16 * DT>(kv, s, h, t * KT, KT, pos, lowest - 1, [half](int i) { return 32 * (i / 16) + 8 * ((i % 16) / 4) + 4 * half + i % 4; },
-                                           [&](int i, float x) { o[i / 16][i % 16] += x; });
-        }
+        if (*flag == t) add_odd(t);
     };
     for (int t = t_lo; t < t_hi; t += 2) {
         tile_step(t, sk0, sv0, sk1, sv1, &odd[0]);
@@ -782,9 +839,10 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
             const long long tiles = (rows + 32 * waves - 1) / (32 * waves), filled = ((long long)T * G + 32 * waves - 1) / (32 * waves);
             return Hkv * (even ? B * tiles : std::max(1ll, std::min(B * tiles, filled)));
         };
-        // 256 rows a workgroup halve the keys' way through LDS (8192-token prompt 315 instead of 322 us, d = 128 120 instead of 130); with fewer than a workgroup
-        // a compute unit 128 fill the card better (512 tokens over 16000, d = 128: 97 instead of 109 us; a ragged fp32 batch 155 instead of 167).
-        p.tile_waves = groups(8) >= 256 ? 8 : 4;
+        // 256 rows a workgroup halve the keys' way through LDS (8192-token prompt, d = 128: 281 instead of 304 us); with fewer than a workgroup a compute unit
+        // 128 fill the card better (512 tokens over 16000, d = 128: 88 instead of 100 us; a ragged fp32 batch 155 instead of 167), but half a workgroup is enough
+        // where many keys are left to split (2048 over 28672, d = 128: 494 instead of 518 us; a 1024-token prompt of its own would lose, 44 instead of 34).
+        p.tile_waves = groups(8) >= (even && len >= 8192 ? 128 : 256) ? 8 : 4;
         p.tiles = (int)((rows + 32 * p.tile_waves - 1) / (32 * p.tile_waves));
         // workgroups that run at once, by their registers and LDS; keys are split where rows leave some of them free
         const long long slots = p.tile_waves == 8 || d == 128 ? 512 : io == SPECTRE_BF16 ? 1024 : 768;
