@@ -48,6 +48,7 @@ struct AttendK {
     float c;                                       // scale * log2(e)
     float *part;                                   // [T * H][slots][d]
     float2 *stat;                                  // [T * H][slots]: maximum in powers of two, sum
+    int *count;                                    // [T * H] parts of the row's keys, 0: the output is written
 };
 
 struct Seq {
@@ -462,6 +463,7 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
     sum += __shfl_xor(sum, 32, 64);
     const long long at = (long long)(s.from + token) * k.a.H + head;
     const float top2 = top * k.c;
+    if (k.slots > 1 && split == 0 && half == 0) k.count[at] = parts > 1 ? parts : 0;
     if (parts > 1) {
         if (half == 0) k.stat[at * k.slots + split] = make_float2(top2, sum);
         if (sum == 0.f) return;
@@ -686,6 +688,7 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
         }
         const int token = r / k.G, head = h * k.G + (r - token * k.G);
         const long long at = (long long)(s.from + token) * k.a.H + head;
+        if (k.slots > 1 && split == 0 && c == 0) k.count[at] = k.few_splits > 1 ? k.few_splits : 0;
         if (k.few_splits > 1) {
             *reinterpret_cast<f32x4_t *>(k.part + (at * k.slots + split) * D + c) = y;
             if (c == 0) k.stat[at * k.slots + split] = make_float2(best * k.c, total);
@@ -731,50 +734,59 @@ __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k
 }
 
 // ---------------------------------------------------------------- splits joined
-// D / 4 lanes hold a row's channels; GROUPS such groups of a workgroup share the splits of one row.  Many rows have a group each; few rows (and then many
-// splits) a workgroup each, where what counts is that all loads are on their way at once.
+// D / 4 lanes hold a row's channels; GROUPS such groups of a workgroup share the parts of one row.  Many rows have a group each; few rows (and then many
+// parts) a workgroup each, where what counts is that all loads are on their way at once: the first parts' before the row's own number of them is known, as the
+// row has room for the launch's largest number (with the number found first, from the row's sequence: one sequence of 32700 tokens 20.2 instead of 18.9 us in all,
+// 16 windows of 5 tokens over 9000, d = 128, 36.7 instead of 34.0).
 template <typename IO, int D, int GROUPS>
-__global__ __launch_bounds__(256) void k_attend_join(AttendK k, int few_splits, int tile_splits) {    // 0: not launched
-    constexpr int LANES = D / 4, ROWS = 256 / (LANES * GROUPS);
+__global__ __launch_bounds__(256) void k_attend_join(AttendK k) {
+    constexpr int LANES = D / 4, ROWS = 256 / (LANES * GROUPS), AT_ONCE = 4;
     __shared__ f32x4_t so[GROUPS > 1 ? GROUPS : 1][LANES];
     __shared__ float2 st[GROUPS > 1 ? GROUPS : 1];
     const int c = threadIdx.x % LANES, g = threadIdx.x / LANES % GROUPS;
-    const long long row = (long long)blockIdx.x * ROWS + threadIdx.x / (LANES * GROUPS), rows = (long long)k.a.T * k.a.H;
-    int splits = 0;
-    if (row < rows) {
-        const int t = (int)(row / k.a.H);
-        splits = few_splits;
-        if (tile_splits) {                         // the row's sequence, the last one with start <= t, says which kernel had it, and in how many parts
-            int lo = 0, hi = k.a.B;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (k.a.start[mid] <= t) lo = mid;
-                else hi = mid;
-            }
-            const Seq s = sequence(k, lo);
-            if ((long long)s.n * k.G > k.few_rows) splits = s.parts(k);
-        }
-        if (t >= k.a.start[k.a.B] || splits == 1) splits = 0;
-    }
+    const long long rows = (long long)k.a.T * k.a.H, mine = (long long)blockIdx.x * ROWS + threadIdx.x / (LANES * GROUPS), row = min(mine, rows - 1);
+    int splits = min(k.count[row], k.slots);
+    if (mine >= rows || (int)(row / k.a.H) >= k.a.start[k.a.B]) splits = 0;    // behind the last sequence nothing was written
+    const int last = (GROUPS > 1 ? k.slots : splits) - 1;
     const float2 *stat = k.stat + row * k.slots;
     const float *part = k.part + row * k.slots * D + 4 * c;
     float best = -INFINITY, total = 0.f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = g; s < splits; s += GROUPS) {
-        const float2 x = stat[s];
-        if (x.y != 0.f) best = fmaxf(best, x.x);   // a part whose sum is zero saw nothing and wrote nothing
-    }
-#pragma unroll 4
-    for (int s = g; s < splits; s += GROUPS) {
-        const float2 x = stat[s];
-        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(part + (long long)s * D);
-        const float f = x.x == best ? 1.f : exp2_fast(x.x - best);
-        if (x.y != 0.f) {
-            total += f * x.y;
-            o += f * y;
+    int from = g;
+    do {
+        float2 x[AT_ONCE];
+        f32x4_t y[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int s = from + i * GROUPS;
+            x[i] = make_float2(0.f, 0.f);
+            y[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if (s <= last) {
+                x[i] = stat[s];
+                y[i] = *reinterpret_cast<const f32x4_t *>(part + (long long)s * D);
+            }
         }
-    }
+        float higher = best;
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            if (from + i * GROUPS >= splits) x[i].y = 0.f;
+            if (x[i].y != 0.f) higher = fmaxf(higher, x[i].x);                // a part whose sum is zero saw nothing and wrote nothing
+        }
+        if (higher != best) {
+            const float f = exp2_fast(best - higher);
+            total *= f;
+            o *= f;
+            best = higher;
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i)
+            if (x[i].y != 0.f) {
+                const float f = x[i].x == best ? 1.f : exp2_fast(x[i].x - best);
+                total += f * x[i].y;
+                o += f * y[i];
+            }
+        from += AT_ONCE * GROUPS;
+    } while (from < splits);
     if constexpr (GROUPS > 1) {
         so[g][c] = o;
         if (c == 0) st[g] = make_float2(best, total);
@@ -791,7 +803,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendK k, int few_splits, 
             o += f * so[i][c];
         }
     }
-    if (!splits) return;
+    if (splits <= 0) return;
     const float inv = inverse(total);
     store4<IO>(k.a.out, row * D + 4 * c, make_float4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv));
     if (k.a.lse && c == 0) k.a.lse[row] = lse_of(best, total);
@@ -804,9 +816,9 @@ hipError_t load_kernels_attend() {
     return hipFuncGetAttributes(&a, reinterpret_cast<const void *>(k_attend_join<Bf16Mma, 64, 1>));
 }
 
-// Up to this many rows a joining workgroup has one row, beyond it a row for each D / 4 lanes: 32 rows of 64 parts 4.5 instead of 8 us, 131072 of two 27 instead of 64
-// (the first form gave every row a wave).
-constexpr long long kWideRows = 4096;
+// Up to this many rows a joining workgroup has one row, beyond it a row for each D / 4 lanes: 512 rows of 16 parts and more 17.3 instead of 19.6 us, the windows' 1280
+// 34.0 instead of 36.9; 4096 of eight 64.2 where workgroups of their own take 67.9 (with the attention before them).
+constexpr long long kWideRows = 2048;
 // Where the sequences differ, the longest must not be one workgroup's work for as long as the others take together; every part costs its rows once through
 // memory: 32 sequences of up to 512 new and 8500 tokens in all take 237 us with parts of 4096 keys, 245 with 2048, 248 with 8192.  Batches of many times more
 // tiles than run at once even out by themselves: 48 of up to 2000 new tokens 825 with 8192, 887 with 4096.
@@ -856,7 +868,7 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
         p.tile_splits = (int)s;
     }
     const int most = std::max(p.few_splits, p.tile_splits);
-    if (most > 1) p.partial_bytes = (size_t)T * H * most * ((size_t)d * 4 + 8);
+    if (most > 1) p.partial_bytes = (size_t)T * H * (most * ((size_t)d * 4 + 8) + 4);
     return p;
 }
 
@@ -873,6 +885,7 @@ hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const Atte
     k.slots = (int)most;
     k.part = (float *)ws;
     k.stat = (float2 *)((char *)ws + (size_t)a.T * a.H * most * d * 4);
+    k.count = (int *)(k.stat + (size_t)a.T * a.H * most);
     const bool stream = 2 * kv.layer_bytes * layers > kStreamBytes;
     k.few_splits = p.few_splits;
     k.tile_splits = p.tile_splits;
@@ -908,10 +921,9 @@ hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const Atte
     if (e != hipSuccess) return e;
     if (p.few_splits > 1 || p.tile_splits > 1) {
         const long long rows = (long long)a.T * a.H;
-        const int few = p.few ? p.few_splits : 0, tile = p.tile ? p.tile_splits : 0;
 #define CALL(IO, D)                                                                                                             \
-    if (rows <= kWideRows) k_attend_join<IO, D, 1024 / D><<<(int)rows, 256, 0, st>>>(k, few, tile);                             \
-    else k_attend_join<IO, D, 1><<<(int)((rows + 1024 / D - 1) / (1024 / D)), 256, 0, st>>>(k, few, tile)
+    if (rows <= kWideRows) k_attend_join<IO, D, 1024 / D><<<(int)rows, 256, 0, st>>>(k);                                        \
+    else k_attend_join<IO, D, 1><<<(int)((rows + 1024 / D - 1) / (1024 / D)), 256, 0, st>>>(k)
         SPECTRE_ATTEND_DISPATCH(CALL)
 #undef CALL
     }

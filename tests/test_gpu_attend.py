@@ -292,6 +292,24 @@ def test_rows_behind_the_last_sequence_are_left_alone():
         check(out[:2 * n], None, q[:2 * n], [n, n], rows, 0.125, torch.bfloat16)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("news", [(1, 1), (40, 40), (1, 40), (300, 300), (300, 1), (0, 300)])
+def test_rows_behind_the_last_sequence_are_left_alone_where_keys_are_split(d, news):
+    """Few and many rows to join, of sequences with many parts, one part and none; what lies in the memory of the parts behind them is nobody's."""
+    print(f"case d={d} news={news}", flush=True)
+    pool, rows = make("bf16", d, 1, 64, [5000, 310], d)
+    q, start = queries(news, 4, d, "bf16", 5)
+    n = q.shape[0]
+    q = torch.cat((q, torch.full_like(q[:1], float("nan")).expand(3, -1, -1)))
+    for trash in (float("nan"), 1.0):
+        junk = [torch.full((16 << 20,), trash, device="cuda") for _ in range(2)]     # freed: the workspace may get it
+        del junk
+        out = torch.full_like(q, 9.0)
+        _, lse = pool.attend(0, q, start, max_new=max(news), max_len=5000, out=out, want_lse=True)
+        assert (out[n:] == 9.0).all()
+        check(out[:n], lse[:n], q[:n], news, rows, d ** -0.5, torch.bfloat16)
+
+
 def test_offsets_beyond_32_bits():
     """A pool of more than 2^32 bytes of keys: its last pages are found."""
     page, Hkv, d = 256, 8, 128
