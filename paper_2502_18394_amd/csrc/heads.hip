@@ -172,11 +172,12 @@ struct Run {
 };
 
 __device__ __forceinline__ bool find_run(const KvView &kv, const int *start, const int *seqs, int B, int T, int block, Run *r) {
-    int lo = 0, hi = B;             // the last b with start[b] / kTokens + 2 b <= block
+    int lo = 0, hi = B;             // the last b with start[b] / kTokens + 2 b <= block: 64 asked at once (19 fp32 sequences of up to 700 tokens 18.6 us, by halves 19.0)
     while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (start[mid] / kTokens + 2 * mid <= block) lo = mid;
-        else hi = mid;
+        const int step = (hi - lo + 63) >> 6, mid = lo + step * (int)(threadIdx.x & 63);
+        const bool behind = mid == lo || (mid < hi && start[mid] / kTokens + 2 * mid <= block);
+        lo += step * (__popcll(__ballot(behind)) - 1);
+        hi = min(hi, lo + step);
     }
     const int from = start[lo], to = min(start[lo + 1], T), n = to - from;
     const int row = seqs ? seqs[lo] : lo;
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
     const int heads = X.H + X.Hkv, step = ROWS >> tl;          // ROWS >= kTokens
     const uint4 *q = reinterpret_cast<const uint4 *>(X.q), *k = reinterpret_cast<const uint4 *>(X.k);
     const int first = (threadIdx.x / LANES) >> tl;
-    constexpr int AHEAD = 4;                                   // rows on their way at once
+    constexpr int AHEAD = 4;                                   // rows on their way at once (the first of them before the angles are formed: 3 to 7 % slower)
     for (int h0 = first + (int)blockIdx.y * AHEAD * step; h0 - first < heads; h0 += AHEAD * step * (int)gridDim.y) {
         uint4 raw[AHEAD];
 #pragma unroll

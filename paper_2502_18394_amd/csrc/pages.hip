@@ -4,7 +4,8 @@
 // uses is free; pages are taken lowest number first, in the order of the call's list, so results do not depend on what ran when.  Each call checks
 // everything it is given before it changes anything: one that cannot be done as a whole sets bits of the status and changes nothing.
 // Bookkeeping is one workgroup's work (a scan over the page users, latency of a launch); the page data moves in a second launch over the whole
-// card, bound by memory.
+// card, bound by memory: 200 pages of 4 layers (210 MB read and written) 41 us, 5.1 TB/s, a large copy's rate; 537 MB of pages moved by a compaction 94 us, 5.7 TB/s.
+// The bookkeeping takes 3.5 (free) to 7.5 us (reserve).
 #include "common.h"
 #include "paged.h"
 

@@ -194,6 +194,32 @@ def test_append(io, page, d, H, Hkv):
             assert (same | (written if L == layer else torch.zeros_like(written))).all()
 
 
+@pytest.mark.parametrize("B", [1, 2, 63, 64, 65, 130, 4200])
+def test_append_of_many_sequences_is_that_of_each(B):
+    """Which sequence a token is of is found among all of them; sequences without a new token in between, at the front and at the end."""
+    print(f"case B={B}", flush=True)
+    g = torch.Generator().manual_seed(B)
+    news = torch.randint(0, 4, (B,), generator=g)
+    news[B // 3] = 19
+    news[0], news[-1] = (0, 0) if B > 2 else (3, 5)
+    lens = (news + torch.randint(0, 13, (B,), generator=g)).tolist()
+    pools = [_pool("bf16", 64, 1, 16, lens, 3) for _ in range(2)]
+    start = torch.tensor([0] + news.tolist()).cumsum(0).int()
+    T = int(start[-1])
+    q, k, (wq, wk), _ = _inputs(T, 2, 1, 64, "bf16", 8)
+    v, rope = k.flip(0).contiguous(), binding.Rope.of(64)
+    out = pools[0].append(0, q, k, v, start.cuda(), None, rope, wq, wk)
+    rows = torch.arange(B, dtype=torch.int32).cuda()
+    for b in range(B):
+        lo, hi = int(start[b]), int(start[b + 1])
+        if hi > lo:
+            one = torch.tensor([0, hi - lo], dtype=torch.int32).cuda()
+            got = pools[1].append(0, q[lo:hi], k[lo:hi], v[lo:hi], one, rows[b:b + 1], rope, wq, wk)
+            assert torch.equal(got, out[lo:hi]), b
+    for x, y in ((pools[0].k_pages, pools[1].k_pages), (pools[0].v_pages, pools[1].v_pages)):
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
 def test_append_leaves_out_what_has_no_place():
     """Rows outside the table, sequences shorter than their new tokens, page numbers outside the pool: nothing is written anywhere."""
     pool = _pool("bf16", 64, 1, 16, [40, 3, 20], 1)
