@@ -532,6 +532,14 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _like(t, stream):
+    """The same with the shape and type of t, contiguous (half a microsecond less than by shape, type and device)."""
+    if stream is None:
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _now(stream):
     """Raw handle of `stream` or the current one, for the calls that take tensors (so that the device is there): a serving step makes several."""
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
@@ -583,9 +591,9 @@ def qk_norm_rotate(q, k, positions=None, rope=None, wq=None, wk=None, eps=1e-6, 
         raise ValueError("q and k differ in d")
     P = _heads(d, rope, wq, wk, eps)
     if q_out is None:
-        q_out = _new((T, H, d), q.dtype, q.device, stream)
+        q_out = _like(q, stream)
     if k_out is None:
-        k_out = _new((T, Hkv, d), q.dtype, q.device, stream)
+        k_out = _like(k, stream)
     _same(q_out, q, "q_out")
     _same(k_out, k, "k_out")
     _check(lib().spectre_heads_forward(ctypes.byref(P), qa, qs, ka, ks, None if positions is None else _ints(positions, "positions", T), T, H, Hkv, io,
@@ -608,7 +616,7 @@ def qk_norm_rotate_backward(dq, dk, q, k, positions=None, rope=None, wq=None, wk
         raise ValueError("dq and dk must have the shapes of q [T,H,d] and k [T,Hkv,d]")
     P = _heads(d, rope, wq, wk, eps)
     rows = [_rows(t, name, q.dtype) for t, name in ((dq, "dq"), (dk, "dk"), (q, "q"), (k, "k"))]
-    gq, gk = _new((T, H, d), q.dtype, q.device, stream), _new((T, Hkv, d), q.dtype, q.device, stream)
+    gq, gk = _like(q, stream), _like(k, stream)
     gw, wsp, wsn = (None, None), None, 0
     if wq is not None:
         gw = _new((2, d), torch.float32, q.device, stream).unbind(0)
@@ -737,7 +745,7 @@ class KvPages:
             raise ValueError(f"q, k and v must have d = {self.d}")
         P = _heads(d, rope, wq, wk, eps)
         if q_out is None:
-            q_out = _new((T, H, d), q.dtype, q.device, stream)
+            q_out = _like(q, stream)
         else:
             _same(q_out, q, "q_out")
         _check(lib().spectre_kv_append(self._ref, layer, ctypes.byref(P), qa, qs, ka, ks, va, vs, _ints(start, "start"),
@@ -762,7 +770,7 @@ class KvPages:
         if max_len is None:
             max_len = self.max_pages * self.page
         if out is None:
-            out = _new((T, H, d), q.dtype, q.device, stream)
+            out = _like(q, stream)
         else:
             _same(out, q, "out")
         if lse is None:
