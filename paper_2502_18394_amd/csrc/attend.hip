@@ -854,14 +854,22 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
         // 256 rows a workgroup halve the keys' way through LDS (8192-token prompt, d = 128: 281 instead of 304 us); with fewer than a workgroup a compute unit
         // 128 fill the card better (512 tokens over 16000, d = 128: 88 instead of 100 us; a ragged fp32 batch 155 instead of 167), but half a workgroup is enough
         // where many keys are left to split (2048 over 28672, d = 128: 494 instead of 518 us; a 1024-token prompt of its own would lose, 44 instead of 34).
-        p.tile_waves = groups(8) >= (even && len >= 8192 ? 128 : 256) ? 8 : 4;
+        // A ragged fp32 batch has 128: its products take longer than the keys' way.
+        // So have rows that fit 128 (256 sequences of 32 tokens 30 instead of 37 us, 90 of 16 over 1000, d = 128, 41 instead of 54).
+        const bool slow = io != SPECTRE_BF16 && !even && rows > 128;
+        p.tile_waves = groups(8) >= (even && len >= 8192 ? 128 : 256) && !slow && rows > 128 ? 8 : 4;
         p.tiles = (int)((rows + 32 * p.tile_waves - 1) / (32 * p.tile_waves));
-        // workgroups that run at once, by their registers and LDS; keys are split where rows leave some of them free
-        const long long slots = p.tile_waves == 8 || d == 128 ? 512 : io == SPECTRE_BF16 ? 1024 : 768;
+        // workgroups that run at once, by their registers and LDS; keys are split where rows leave some of them free.  Of single tiles, which memory bounds, two a
+        // compute unit are enough: the join costs more than a third and fourth gain (64 sequences of 8 tokens over 2000 48 instead of 55 us, 16 over 9000 53 instead
+        // of 58; one a compute unit: 50 and 73).
+        const long long slots = p.tile_waves == 8 || d == 128 || rows <= 128 ? 512 : io == SPECTRE_BF16 ? 1024 : 768;
         // Parts of the longest sequence; the others' parts are as long.  With several tiles a sequence of a ragged batch they take different times, and
         // twice the parts even them out (fp32 batch of up to 397 new tokens 135 instead of 142 us; single tiles, bound by memory, lose: 25.0 -> 28.8).
         const long long all = groups(p.tile_waves), keys = all > 4 * slots ? 2 * kRaggedKeys : kRaggedKeys;
         long long s = std::max(1ll, (even || rows <= 128 ? 1 : 2) * slots / all);
+        // fp32: four times, of 768 keys or more (24 sequences of up to 300 new and 4300 tokens, 32 heads, d = 64: 428 us, with 1024 keys or more 459, with
+        // 256 rows and twice the parts 535; 12 of up to 1500 new: 150, with parts down to 500 keys 160; bf16 with four times 133 instead of 111).
+        if (slow) s = std::max(s, std::min(4 * slots / all, len / 768));
         if (!even) s = std::max(s, (len + keys - 1) / keys);
         s = std::max(1ll, std::min({s, len / 256, 64ll}));
         p.part_keys = (int)((len + s - 1) / s);
@@ -870,6 +878,17 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
     const int most = std::max(p.few_splits, p.tile_splits);
     if (most > 1) p.partial_bytes = (size_t)T * H * (most * ((size_t)d * 4 + 8) + 4);
     return p;
+}
+
+template <typename IO, int D>
+void launch_mixed(int waves, int blocks, const AttendK &k, hipStream_t st) {
+    if constexpr (IO::E == 8) {                    // the plan gives a ragged fp32 batch 128 rows
+        if (waves == 8) {
+            k_attend_mixed<IO, D, 8><<<blocks, 512, 0, st>>>(k);
+            return;
+        }
+    }
+    k_attend_mixed<IO, D, 4><<<blocks, 256, 0, st>>>(k);
 }
 
 hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const AttendArgs &a, const AttendPlan &p, void *ws, hipStream_t st) {
@@ -901,9 +920,7 @@ hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const Atte
     else { CALL(F32Mma, 128); }
     if (p.few && p.tile) {
         const int blocks = ((k.tile_blocks + 7) & ~7) + k.few_blocks;
-#define CALL(IO, D)                                                                        \
-    if (p.tile_waves == 8) k_attend_mixed<IO, D, 8><<<blocks, 512, 0, st>>>(k);            \
-    else k_attend_mixed<IO, D, 4><<<blocks, 256, 0, st>>>(k)
+#define CALL(IO, D) launch_mixed<IO, D>(p.tile_waves, blocks, k, st)
         SPECTRE_ATTEND_DISPATCH(CALL)
 #undef CALL
     } else if (p.few) {
