@@ -351,7 +351,8 @@ __global__ __launch_bounds__(kThreads) void k_heads_backward(HeadParams P, HeadR
                     sq += x[e] * x[e];
                     dot += g[e] * w[e] * x[e];
                 }
-                const float r = rsqrtf(row_sum<LANES>(sq) * (1.f / D) + P.eps);
+                // a row that only pads adds nothing: without an epsilon its root would be infinite, and its sums NaN
+                const float rms = rsqrtf(row_sum<LANES>(sq) * (1.f / D) + P.eps), r = there && h < heads ? rms : 0.f;
                 const float m = row_sum<LANES>(dot) * r * (1.f / D);          // mean(h r x)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {

@@ -1,0 +1,60 @@
+"""Norm and rotation of heads where sums, padding rows and untouched channels can go wrong."""
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as ref
+from paper_2502_18394_amd import binding
+from test_gpu_heads import DT, U32, _check, _inputs, _pool, _turn_size
+
+pytestmark = pytest.mark.gpu
+CHAIN = 128                                          # rows that a thread adds in 32 bits before they go into 64, at most
+
+
+def _weights_close(got, want, terms, d):
+    """A product of three roundings around a sum of d squares, sums of up to CHAIN products in 32 bits, the rest in 64, one rounding."""
+    tol = (d + 16 + CHAIN) * U32 * terms + U32 * np.abs(want) + 1e-300
+    err = np.abs(ref.f64(got) - want)
+    assert np.isfinite(ref.f64(got)).all() and (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,Hkv,d", [(1, 1, 1, 64), (1, 3, 2, 128), (7, 4, 1, 64), (9, 5, 5, 64), (9, 2, 1, 128), (16, 3, 4, 64)])
+def test_no_epsilon(T, H, Hkv, d, io):
+    """eps = 0 is a norm like any other while no row is all zero: what pads a workgroup's tokens and heads is no row."""
+    print(f"case T={T} H={H} Hkv={Hkv} d={d} {io}", flush=True)
+    q, k, w, g = _inputs(T, H, Hkv, d, io, T + H + d)
+    dy = [torch.randn(x.shape, generator=g).to(DT[io]).cuda() for x in (q, k)]
+    rope, pos = binding.Rope.of(d), np.arange(T)
+    freq = ref.f64(rope.inv_freq)
+    got = binding.qk_norm_rotate(q, k, None, rope, *w, 0.0)
+    grads = binding.qk_norm_rotate_backward(*dy, q, k, None, rope, *w, 0.0)
+    for n, (x, weight) in enumerate(((q, w[0]), (k, w[1]))):
+        x64, w64, d64 = ref.f64(x), ref.f64(weight), ref.f64(dy[n])
+        _check(got[n], ref.heads(x64, w64, pos, freq, 0.0), _turn_size(ref.heads(x64, w64, pos, np.zeros(0), 0.0), d // 2, False), DT[io], d)
+        want, want_w = ref.heads_backward(d64, x64, w64, pos, freq, 0.0)
+        size = _turn_size(d64, d // 2, False)
+        r = 1 / np.sqrt((x64 * x64).mean(-1, keepdims=True))
+        h, xh = size * np.abs(w64), np.abs(x64 * r)
+        _check(grads[n], want, 3 * r * (h + xh * (h * xh).mean(-1, keepdims=True)), DT[io], d)
+        _weights_close(grads[2 + n], want_w, (size * xh).sum((0, 1)), d)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,Hkv,d", [(9001, 2, 1, 64), (33003, 1, 1, 64), (25001, 3, 1, 128)])
+def test_backward_of_several_runs_a_workgroup(T, H, Hkv, d, io):
+    """So many tokens that a workgroup has more than one run of them, whole and ragged ones."""
+    print(f"case T={T} H={H} Hkv={Hkv} d={d} {io}", flush=True)
+    q, k, w, g = _inputs(T, H, Hkv, d, io, T)
+    dy = [torch.randn(x.shape, generator=g).to(DT[io]).cuda() for x in (q, k)]
+    rope, pos = binding.Rope.of(d, 500000.0), np.arange(T)
+    freq = ref.f64(rope.inv_freq)
+    grads = binding.qk_norm_rotate_backward(*dy, q, k, None, rope, *w, 1e-5)
+    for n, (x, weight) in enumerate(((q, w[0]), (k, w[1]))):
+        x64, w64, d64 = ref.f64(x), ref.f64(weight), ref.f64(dy[n])
+        want, want_w = ref.heads_backward(d64, x64, w64, pos, freq, 1e-5)
+        size = _turn_size(d64, d // 2, False)
+        r = 1 / np.sqrt((x64 * x64).mean(-1, keepdims=True) + 1e-5)
+        h, xh = size * np.abs(w64), np.abs(x64 * r)
+        _check(grads[n], want, 3 * r * (h + xh * (h * xh).mean(-1, keepdims=True)), DT[io], d)
+        _weights_close(grads[2 + n], want_w, (size * xh).sum((0, 1)), d)
