@@ -504,7 +504,7 @@ int spectre_heads_forward(const spectre_heads *P /*host*/, const void *q, long l
                           int T, int H, int Hkv, spectre_dtype io, void *q_out, void *k_out, void *stream);
 
 /* Its gradients: from dq, dk (of q_out and k_out; strides of their own) and the inputs, gq [T, H, d], gk [T, Hkv, d] (dense) and, with a norm,
- * gwq, gwk fp32 [d].  The sums over tokens and heads are formed in fp64 in a fixed order. */
+ * gwq, gwk fp32 [d].  Their sums over tokens and heads: fewer than 128 rows at a time in fp32, those sums in fp64, all in a fixed order. */
 size_t spectre_heads_backward_workspace_bytes(int T, int d);
 int spectre_heads_backward(const spectre_heads *P /*host*/, const void *dq, long long dq_stride, const void *dk, long long dk_stride, const void *q,
                            long long q_stride, const void *k, long long k_stride, const int *positions, int T, int H, int Hkv, spectre_dtype io,

@@ -40,6 +40,22 @@ def test_no_epsilon(T, H, Hkv, d, io):
         _weights_close(grads[2 + n], want_w, (size * xh).sum((0, 1)), d)
 
 
+@pytest.mark.parametrize("T,H,Hkv", [(1, 65536, 1), (1, 1, 40000), (17, 5000, 300)])
+def test_weight_gradients_of_very_many_heads(T, H, Hkv):
+    """Heads that are all alike: a long sum of equal terms in 32 bits is off by much more than its terms are."""
+    print(f"case T={T} H={H} Hkv={Hkv}", flush=True)
+    d = 64
+    q, k, w, g = _inputs(T, 1, 1, d, "f32", 4)
+    dq, dk = (torch.randn(T, 1, d, generator=g).cuda() for _ in "qk")
+    many = lambda x, n: x.expand(T, n, d).contiguous()
+    grads = binding.qk_norm_rotate_backward(many(dq, H), many(dk, Hkv), many(q, H), many(k, Hkv), None, None, *w, 1e-6)
+    for n, (x, dy, heads) in enumerate(((q, dq, H), (k, dk, Hkv))):
+        _, want = ref.heads_backward(ref.f64(dy), ref.f64(x), ref.f64(w[n]), np.zeros(T), np.zeros(0), 1e-6)
+        x64 = ref.f64(x)
+        xh = np.abs(x64 / np.sqrt((x64 * x64).mean(-1, keepdims=True) + 1e-6))
+        _weights_close(grads[2 + n], heads * want, heads * (np.abs(ref.f64(dy)) * xh).sum((0, 1)), d)
+
+
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("T,H,Hkv,d", [(9001, 2, 1, 64), (33003, 1, 1, 64), (25001, 3, 1, 128)])
 def test_backward_of_several_runs_a_workgroup(T, H, Hkv, d, io):
