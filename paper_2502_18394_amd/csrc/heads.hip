@@ -96,10 +96,13 @@ struct Lane {
             }
         }
     }
-    // y of this lane's channels, z of their partners'
+    // y of this lane's channels, z of their partners'.  Channels that are not turned (whole lanes of them) pass through: a zero times an infinite neighbour is NaN.
     __device__ __forceinline__ void turn(const HeadParams &P, const float (&y)[E], const float (&z)[E], float (&o)[E]) const {
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = y[e] * c[e] + (P.interleaved ? y[e ^ 1] : z[e]) * s[e];
+        for (int e = 0; e < E; ++e) {
+            const float t = y[e] * c[e] + (P.interleaved ? y[e ^ 1] : z[e]) * s[e];
+            o[e] = turned ? t : y[e];
+        }
     }
 };
 

@@ -74,3 +74,36 @@ def test_backward_of_several_runs_a_workgroup(T, H, Hkv, d, io):
         h, xh = size * np.abs(w64), np.abs(x64 * r)
         _check(grads[n], want, 3 * r * (h + xh * (h * xh).mean(-1, keepdims=True)), DT[io], d)
         _weights_close(grads[2 + n], want_w, (size * xh).sum((0, 1)), d)
+
+
+def _same_bits(a, b):
+    bits = torch.int16 if a.dtype == torch.bfloat16 else torch.int32
+    return torch.equal(a.contiguous().view(bits), b.contiguous().view(bits))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,rot", [(64, 16), (64, 48), (128, 32)])
+def test_channels_that_are_not_turned_pass_through(d, rot, interleaved, io):
+    """Without a norm they are copies, whatever they hold, and nothing of theirs reaches another channel: forward, backward and into pages."""
+    print(f"case d={d} rot={rot} interleaved={interleaved} {io}", flush=True)
+    T, H, Hkv = 11, 4, 2
+    q, k, _, _ = _inputs(T, H, Hkv, d, io, rot)
+    odd = [x.clone() for x in (q, k)]
+    for x in odd:
+        x[:, :, rot + 1] = float("inf")
+        x[::2, :, rot + 4] = float("nan")
+        x[1::2, :, d - 1] = -float("inf")
+        x[:, :, rot + 2] = -0.0
+    rope = binding.Rope.of(rot, 10000.0, interleaved)
+    pos = torch.arange(5, 5 + T, dtype=torch.int32, device="cuda")
+    for call in (lambda q, k: binding.qk_norm_rotate(q, k, pos, rope), lambda q, k: binding.qk_norm_rotate_backward(q, k, q, k, pos, rope)[:2]):
+        for got, plain, x in zip(call(*odd), call(q, k), odd):
+            assert _same_bits(got[..., rot:], x[..., rot:])
+            assert _same_bits(got[..., :rot], plain[..., :rot])
+    pool = _pool(io, d, Hkv, 16, [T], 1)
+    start = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    out = pool.append(0, odd[0], odd[1], odd[1], start, None, rope)
+    keys, _ = ref.pool_rows(pool.k_pages.cpu(), pool.v_pages.cpu(), 0, pool.table[0, :1].cpu().long())
+    assert _same_bits(out[..., rot:], odd[0][..., rot:]) and _same_bits(keys[:T, :, rot:], odd[1][..., rot:].cpu())
+    assert torch.isfinite(out[..., :rot]).all() and torch.isfinite(keys[:T, :, :rot]).all()
