@@ -827,6 +827,7 @@ constexpr long long kStreamBytes = 96ll << 20;
 
 AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new, int max_len, int window) {
     AttendPlan p{};
+    if (T == 0 || B == 0) return p;                                // nothing to launch
     const int G = H / Hkv;
     const long long rows = (long long)max_new * G;
     const bool even = T == (long long)B * max_new;                 // every sequence has max_new tokens
