@@ -523,7 +523,7 @@ int spectre_kv_append(const spectre_kv *kv /*host*/, int layer, const spectre_he
  * denominator.  A row that sees no key gets out = 0 and lse = -inf; keys that a row does not see, and what lies behind a sequence's
  * last token, take no part even if they are infinite or NaN.
  *   max_new, max_len   bounds of the sequences' new tokens and lengths, which the launch is sized by: a sequence with more new tokens than
- *                      max_new is left out, in part or as a whole; a length above max_len costs time only
+ *                      max_new is left out, in part or as a whole (the rows left out stay as they are); a length above max_len costs time only
  *   scale              1e-30 to 1e30
  */
 size_t spectre_kv_attend_workspace_bytes(const spectre_kv *kv /*host*/, int B, int T, int H, int max_new, int max_len, int window);

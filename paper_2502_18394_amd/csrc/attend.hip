@@ -71,6 +71,14 @@ __device__ __forceinline__ Seq sequence(const AttendK &k, int b) {
     return s;
 }
 
+// Rows from `r` on of a sequence with more new tokens than the launch is sized for: nobody takes them, and the join leaves them as they are.
+__device__ __forceinline__ void left_out(const AttendK &k, const Seq &s, int h, int r, int threads) {
+    for (r += threadIdx.x; r < s.n * k.G; r += threads) {
+        const int token = r / k.G;
+        k.count[(long long)(s.from + token) * k.a.H + h * k.G + (r - token * k.G)] = 0;
+    }
+}
+
 // Which sequence and key head a workgroup works on: all of them in turn, for each `rest` (tile, part) turned on by eight.  Eight keep a pair on one XCD, whose L2 then has its
 // keys; without the turn the workgroups of a long sequence come at a fixed distance, often a multiple of what an XCD deals out at a time, and
 // land on the same few compute units (24 ragged sequences, d = 128: 302 instead of 137 us).
@@ -244,6 +252,7 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
     const Seq s = sequence(k, pair / kv.Hkv);
     const int rows = s.n * k.G, r0 = tile * kTileRows, parts = s.parts(k);
     if (rows <= k.few_rows || r0 >= rows || split >= parts) return;
+    if (k.slots > 1 && split == 0 && tile == 0) left_out(k, s, h, k.tiles * kTileRows, THREADS);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int r = min(r0 + 32 * wave + (lane & 31), rows - 1), token = r / k.G, head = h * k.G + (r - token * k.G);
@@ -508,6 +517,7 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
     const int pairs = kv.Hkv * k.a.B, split = block / pairs, pair = turned_pair(block, split, pairs), h = pair % kv.Hkv;
     const Seq s = sequence(k, pair / kv.Hkv);
     const int rows = s.n * k.G;
+    if (rows > k.few_rows && k.tiles == 0 && k.slots > 1 && split == 0) left_out(k, s, h, 0, THREADS);
     if (rows == 0 || rows > k.few_rows) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
     const int p0 = s.m - s.n, mask = (1 << kv.page_log) - 1;
