@@ -834,11 +834,14 @@ constexpr long long kWideRows = 2048;
 // tiles than run at once even out by themselves: 48 of up to 2000 new tokens 825 with 8192, 887 with 4096.
 constexpr long long kRaggedKeys = 4096;
 constexpr long long kStreamBytes = 96ll << 20;
+constexpr long long kMostThreads = (1ll << 32) - 1;
 
 AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new, int max_len, int window) {
     AttendPlan p{};
+    p.fits = true;
     if (T == 0 || B == 0) return p;                                // nothing to launch
     const int G = H / Hkv;
+    max_new = std::min(max_new, T);
     const long long rows = (long long)max_new * G;
     const bool even = T == (long long)B * max_new;                 // every sequence has max_new tokens
     const long long len = window ? std::min<long long>(max_len, (long long)window + max_new) : max_len;
@@ -883,9 +886,18 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
         if (slow) s = std::max(s, std::min(4 * slots / all, len / 768));
         if (!even) s = std::max(s, (len + keys - 1) / keys);
         s = std::max(1ll, std::min({s, len / 256, 64ll}));
-        p.part_keys = (int)((len + s - 1) / s);
         p.tile_splits = (int)s;
     }
+    // A launch has fewer than 2^32 threads: batches of loose bounds get fewer parts, and what is too large even so none at all.
+    const long long threads = p.tile ? 64 * p.tile_waves : 256;
+    auto blocks = [&]() { return pairs * ((p.few ? p.few_splits : 0) + (long long)p.tile_splits * p.tiles) + 8; };
+    while (blocks() * threads > kMostThreads && (p.few_splits > 1 || p.tile_splits > 1)) {
+        p.few_splits = (p.few_splits + 1) / 2;
+        p.tile_splits = (p.tile_splits + 1) / 2;
+    }
+    if ((long long)T * H * (d / 4) + 256 > kMostThreads) p.few_splits = p.tile_splits = 1;       // no join
+    p.fits = blocks() * threads <= kMostThreads;
+    p.part_keys = (int)((len + p.tile_splits - 1) / p.tile_splits);
     const int most = std::max(p.few_splits, p.tile_splits);
     if (most > 1) p.partial_bytes = (size_t)T * H * (most * ((size_t)d * 4 + 8) + 4);
     return p;

@@ -60,6 +60,7 @@ hipError_t launch_kv_copy(const KvView &kv, int layers, const int *src, const in
 
 // attend.hip
 struct AttendPlan {
+    bool fits;                       // a launch can have that many workgroups
     int few, tile;                   // whether each kernel is launched
     int few_rows;                    // rows (new tokens x heads of a key head) that the kernel of few rows takes, 0 if it is not launched
     int few_splits, tile_splits, tiles, tile_waves, part_keys;

@@ -106,6 +106,10 @@ int check_attend(const spectre_kv *kv, int B, int T, int H, int max_new, int max
     return SPECTRE_OK;
 }
 
+int check_plan(const AttendPlan &p, int B, int H, int max_new, const char *who) {
+    return p.fits ? SPECTRE_OK : fail(SPECTRE_EUNSUPPORTED, "%s: %d sequences of %d new tokens, %d heads: more workgroups than a launch has", who, B, max_new, H);
+}
+
 }  // namespace
 }  // namespace spectre
 
@@ -263,7 +267,9 @@ int spectre_kv_append(const spectre_kv *kv, int layer, const spectre_heads *P, c
 size_t spectre_kv_attend_workspace_bytes(const spectre_kv *kv, int B, int T, int H, int max_new, int max_len, int window) {
     if (check_sizes(kv, "kv_attend") || check_attend(kv, B, T, H, max_new, max_len, window, "kv_attend")) return 0;
     if (window >= kLongest) window = 0;
-    return align256(attend_plan(kv->d, (int)kv->dtype, B, T, H, kv->Hkv, max_new, max_len, window).partial_bytes + 1);
+    const AttendPlan p = attend_plan(kv->d, (int)kv->dtype, B, T, H, kv->Hkv, max_new, max_len, window);
+    if (check_plan(p, B, H, max_new, "kv_attend")) return 0;
+    return align256(p.partial_bytes + 1);
 }
 
 int spectre_kv_attend(const spectre_kv *kv, int layer, const void *q, long long q_stride, const int *start, const int *seqs, int B, int T, int H, int max_new, int max_len,
@@ -283,6 +289,7 @@ int spectre_kv_attend(const spectre_kv *kv, int layer, const void *q, long long 
     if ((rc = check_rows({out, (long long)H * kv->d, H, "out"}, kv->d, kv->dtype, who))) return rc;
     if (overlap(x, out, H, T, kv->d, kv->dtype)) return fail(SPECTRE_EINVAL, "%s: out overlaps q", who);
     const AttendPlan p = attend_plan(kv->d, (int)kv->dtype, B, T, H, kv->Hkv, max_new, max_len, window);
+    if ((rc = check_plan(p, B, H, max_new, who))) return rc;
     if (p.partial_bytes && (rc = check_ws(ws, ws_bytes, align256(p.partial_bytes + 1), who))) return rc;
     const AttendArgs a = {q, q_stride, start, seqs, B, T, H, window, scale, out, lse};
     return done(launch_attend(kv_view(kv, layer), kv->layers, kv->d, (int)kv->dtype, a, p, ws, static_cast<hipStream_t>(stream)), who);

@@ -1,8 +1,13 @@
-"""How much workspace an attention call asks for (no device is touched)."""
+"""How much workspace an attention call asks for, and which batches are too large for a launch (no device is touched)."""
+import ctypes
 import subprocess
 import sys
 
-from test_paged_refusals import lib  # noqa: F401
+import pytest
+
+from paper_2502_18394_amd import binding
+from test_paged_refusals import FAKE, FAR, OUT, lib, pool  # noqa: F401
+
 
 
 def test_an_empty_batch_has_a_plan(lib):  # noqa: F811
@@ -18,3 +23,19 @@ def test_an_empty_batch_has_a_plan(lib):  # noqa: F811
             "            assert 0 < L.spectre_kv_attend_workspace_bytes(c, B, T, 4, new, 300, 0) <= 4096, (B, T, new)\n")
     done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=__file__.rsplit("/", 2)[0])
     assert done.returncode == 0, (done.returncode, done.stderr[-500:])
+
+
+def _sizes(lib, B, T, H, new, most, **change):
+    c = pool(layers=1, pages=1 << 16, Hkv=8, page=64, seqs=4096, max_pages=1 << 14, **change)
+    return lib.spectre_kv_attend_workspace_bytes(ctypes.byref(c), B, T, H, new, most, 0)
+
+
+@pytest.mark.parametrize("dtype", [binding.F32, binding.BF16])
+def test_batches_too_large_for_a_launch(lib, dtype):  # noqa: F811
+    """The call and the size query agree, before anything is launched; what can be launched with fewer parts is."""
+    assert _sizes(lib, 256, 32768, 32, 32768, 131072, dtype=dtype) > 0
+    c = ctypes.byref(pool(layers=1, pages=1 << 16, Hkv=8, page=64, seqs=4096, max_pages=1 << 14, dtype=dtype))
+    B, T, new = 1024, 1 << 16, 1 << 16                      # 1024 tiles of 512 threads for each of 8192 pairs: 2^32 threads, one more than there can be
+    assert lib.spectre_kv_attend_workspace_bytes(c, B, T, 32, new, 131072, 0) == 0
+    assert lib.spectre_kv_attend(c, 0, FAKE, 2048, FAKE, None, B, T, 32, new, 131072, 0.1, 0, OUT, None, FAKE, 1 << 40, None) == 2
+    assert lib.spectre_last_error()
