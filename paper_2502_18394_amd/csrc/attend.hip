@@ -41,22 +41,28 @@ struct AttendK {
     KvView kv;
     AttendArgs a;
     int G, tiles, few_rows;                        // heads of a key head; tiles of a sequence; the rows up to which a sequence is the business of `few`
-    int few_splits, tile_splits, slots;            // parts of a sequence's keys, at most; parts that a row has room for
+    int few_splits, tile_splits, slots;            // parts of a sequence's keys, at most; of either kind
     int part_keys;                                 // of a part of a tile's rows, at least
     int few_blocks, tile_blocks;                   // workgroups of each kind, where both are in one launch
     bool few_stream, tile_stream;                  // pages are read past the memory-side cache
     float c;                                       // scale * log2(e)
-    float *part;                                   // [T * H][slots][d]
-    float2 *stat;                                  // [T * H][slots]: maximum in powers of two, sum
+    // Places of partial results: `slots` for every row, or, where that would be too many (`packed`), as many as each row has parts: first those of few rows, few_tokens
+    // tokens a sequence (0: every token of the batch has them), then those of tiles' rows, tile_places in all.
+    bool packed;
+    int few_tokens;
+    long long few_places, tile_places;
+    float *part;                                   // [places][d]
+    float2 *stat;                                  // [places]: maximum in powers of two, sum
     int *count;                                    // [T * H] parts of the row's keys, 0: the output is written
+    unsigned *first;                               // [T * H] the row's first place, if `packed`
 };
 
 struct Seq {
     int from, n, m, row;                           // first new token, new tokens, tokens, row of the table
-    // parts that the keys of a tile's rows are divided into
-    __device__ __forceinline__ int parts(const AttendK &k) const {
+    // parts that the keys of a tile's rows are divided into, of part_keys keys or more
+    __device__ __forceinline__ int parts(const AttendK &k, int part_keys) const {
         const int keys = k.a.window ? min(m, k.a.window + n) : m;
-        return max(1, min(k.tile_splits, (keys + k.part_keys - 1) / k.part_keys));
+        return max(1, min(k.tile_splits, (keys + part_keys - 1) / part_keys));
     }
 };
 __device__ __forceinline__ Seq sequence(const AttendK &k, int b) {
@@ -69,6 +75,36 @@ __device__ __forceinline__ Seq sequence(const AttendK &k, int b) {
     if ((unsigned)s.row < (unsigned)k.kv.S) s.m = min(max(k.kv.lens[s.row], 0), k.kv.M << k.kv.page_log);
     else s.row = 0;
     return s;
+}
+
+// Length of parts and the tokens x parts of the sequences in front of sequence b, where places are shared out: to the sequences that have more than one part, in turn.  If
+// all of them together want more places than there are, parts become longer until they fit.  Every workgroup of a sequence finds the same (a wave looks at
+// 64 sequences at once).
+struct Room {
+    int part_keys, before;
+};
+__device__ __forceinline__ long long wave_sum(long long x) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m, 64);
+    return x;
+}
+__device__ __forceinline__ Room room_of(const AttendK &k, int b) {
+    const int lane = threadIdx.x & 63, B = k.a.B;
+    int part_keys = k.part_keys;
+    auto want = [&](const Seq &s) -> long long {
+        const int parts = s.n * k.G > k.few_rows ? s.parts(k, part_keys) : 1;
+        return parts > 1 ? (long long)s.n * parts : 0;
+    };
+    Seq mine = sequence(k, min(lane, B - 1));
+    if (lane >= B) mine.n = 0;
+    for (;; part_keys += part_keys / 8 + 1) {                    // ends where every sequence is one part
+        long long all = want(mine);
+        for (int i = lane + 64; i < B; i += 64) all += want(sequence(k, i));
+        if (wave_sum(all) * k.a.H <= k.tile_places) break;
+    }
+    long long before = lane < b ? want(mine) : 0;
+    for (int i = lane + 64; i < b; i += 64) before += want(sequence(k, i));
+    return Room{part_keys, (int)wave_sum(before)};
 }
 
 // Rows from `r` on of a sequence with more new tokens than the launch is sized for: nobody takes them, and the join leaves them as they are.
@@ -237,7 +273,7 @@ template <typename IO, int D>
 constexpr int kTileGroups = IO::kTileKeys * D / IO::E;
 struct TileLds {
     uint4 *sk0, *sv0, *sk1, *sv1;                   // kTileGroups each, arrays of their own: the compiler sees which loads a read need not wait for
-    int *odd;                                       // [2] the last tile whose values were not all finite
+    int *odd;                                       // [2] the last tile whose values were not all finite; [2]: tokens x parts in front of the sequence's places
 };
 
 template <typename IO, int D, int WAVES>
@@ -250,8 +286,17 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
     const int pairs = kv.Hkv * k.a.B, rest = block / pairs, pair = turned_pair(block, rest, pairs);
     const int h = pair % kv.Hkv, split = rest % k.tile_splits, tile = k.tiles - 1 - rest / k.tile_splits;   // long rows first
     const Seq s = sequence(k, pair / kv.Hkv);
-    const int rows = s.n * k.G, r0 = tile * kTileRows, parts = s.parts(k);
-    if (rows <= k.few_rows || r0 >= rows || split >= parts) return;
+    const int rows = s.n * k.G, r0 = tile * kTileRows;
+    if (rows <= k.few_rows || r0 >= rows) return;
+    int parts = s.parts(k, k.part_keys);
+    if (split >= parts) return;
+    if (k.packed && parts > 1) {
+        const Room room = room_of(k, pair / kv.Hkv);
+        parts = s.parts(k, __builtin_amdgcn_readfirstlane(room.part_keys));
+        if (split >= parts) return;
+        if (threadIdx.x == 0) odd[2] = room.before;          // for the end
+        __syncthreads();
+    }
     if (k.slots > 1 && split == 0 && tile == 0) left_out(k, s, h, k.tiles * kTileRows, THREADS);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
@@ -474,9 +519,15 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
     const float top2 = top * k.c;
     if (k.slots > 1 && split == 0 && half == 0) k.count[at] = parts > 1 ? parts : 0;
     if (parts > 1) {
-        if (half == 0) k.stat[at * k.slots + split] = make_float2(top2, sum);
+        long long place = at * k.slots;
+        if (k.packed) {
+            place = k.few_places + (long long)odd[2] * k.a.H + ((long long)token * k.a.H + head) * parts;
+            if (split == 0 && half == 0) k.first[at] = (unsigned)place;
+        }
+        place += split;
+        if (half == 0) k.stat[place] = make_float2(top2, sum);
         if (sum == 0.f) return;
-        float *to = k.part + (at * k.slots + split) * D;
+        float *to = k.part + place * D;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -700,8 +751,14 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
         const long long at = (long long)(s.from + token) * k.a.H + head;
         if (k.slots > 1 && split == 0 && c == 0) k.count[at] = k.few_splits > 1 ? k.few_splits : 0;
         if (k.few_splits > 1) {
-            *reinterpret_cast<f32x4_t *>(k.part + (at * k.slots + split) * D + c) = y;
-            if (c == 0) k.stat[at * k.slots + split] = make_float2(best * k.c, total);
+            long long place = at * k.slots;
+            if (k.packed) {
+                place = (k.few_tokens ? ((long long)(pair / kv.Hkv) * k.few_tokens + token) * k.a.H + head : at) * k.few_splits;
+                if (split == 0 && c == 0) k.first[at] = (unsigned)place;
+            }
+            place += split;
+            *reinterpret_cast<f32x4_t *>(k.part + place * D + c) = y;
+            if (c == 0) k.stat[place] = make_float2(best * k.c, total);
         } else {
             const float inv = inverse(total);
             store4<IO>(k.a.out, at * D + c, make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv));
@@ -722,7 +779,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) 
 template <typename IO, int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k_attend_tile(AttendK k) {
     __shared__ uint4 sk0[kTileGroups<IO, D>], sv0[kTileGroups<IO, D>], sk1[kTileGroups<IO, D>], sv1[kTileGroups<IO, D>];
-    __shared__ int odd[2];
+    __shared__ int odd[3];
     tile_of_rows<IO, D, WAVES>(k, blockIdx.x, TileLds{sk0, sv0, sk1, sv1, odd});
 }
 
@@ -731,7 +788,7 @@ __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k
 template <typename IO, int D, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k_attend_mixed(AttendK k) {
     __shared__ uint4 sk0[kTileGroups<IO, D>], sv0[kTileGroups<IO, D>], sk1[kTileGroups<IO, D>], sv1[kTileGroups<IO, D>];
-    __shared__ int odd[2], pages[kSection + 2];
+    __shared__ int odd[3], pages[kSection + 2];
     __shared__ float tops[WAVES][16], sums[WAVES][16];
     static_assert(kTileGroups<IO, D> >= (WAVES / 4) * kFewGroups<IO, D>, "outputs of few rows fit where tiles lie");
     const int tiles = (k.tile_blocks + 7) & ~7, block = blockIdx.x;              // eights again, for the XCDs
@@ -757,9 +814,14 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendK k) {
     const long long rows = (long long)k.a.T * k.a.H, mine = (long long)blockIdx.x * ROWS + threadIdx.x / (LANES * GROUPS), row = min(mine, rows - 1);
     int splits = min(k.count[row], k.slots);
     if (mine >= rows || (int)(row / k.a.H) >= k.a.start[k.a.B]) splits = 0;    // behind the last sequence nothing was written
-    const int last = (GROUPS > 1 ? k.slots : splits) - 1;
-    const float2 *stat = k.stat + row * k.slots;
-    const float *part = k.part + row * k.slots * D + 4 * c;
+    long long place = row * k.slots;
+    if (k.packed) {
+        place = splits > 0 ? k.first[row] : 0;
+        if (place + splits > k.few_places + k.tile_places) splits = 0;         // a row that no sequence has
+    }
+    const int last = (GROUPS > 1 && !k.packed ? k.slots : splits) - 1;
+    const float2 *stat = k.stat + place;
+    const float *part = k.part + place * D + 4 * c;
     float best = -INFINITY, total = 0.f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
     int from = g;
@@ -835,6 +897,12 @@ constexpr long long kWideRows = 2048;
 constexpr long long kRaggedKeys = 4096;
 constexpr long long kStreamBytes = 96ll << 20;
 constexpr long long kMostThreads = (1ll << 32) - 1;
+// Partial results: a place for every part of every row up to this many bytes (or to what sharing would take); beyond it rows of tiles share five places for two rows, or half as
+// many bytes if that is more, and few rows have as many parts as this many bytes hold.  One chunk of 8192 tokens beside 31 decoding sequences, lengths of up to 131072,
+// 32 heads, d = 128: 0.5 GB, where a place for every part would be 8.8.  Sharing is free until parts have to become longer (32 sequences of up to 1500 new tokens over
+// 36000, 0.2 instead of 1.7 GB: 1885 us, before 1880; 40 over 20000, 0.4 instead of 1.6 GB: 1684, before 1672); then it costs the even end of the launch (20 of up to
+// 4000 over 60000, d = 128, 0.4 instead of 4.6 GB: 7102, before 6786).
+constexpr long long kPartBytes = 256ll << 20;
 
 AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new, int max_len, int window) {
     AttendPlan p{};
@@ -851,13 +919,16 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
     p.tile = rows > 16;
     p.few_rows = !p.few ? 0 : p.tile ? 16 : (int)rows;
     p.few_splits = p.tile_splits = 1;
-    const long long pairs = (long long)B * Hkv;
+    const long long pairs = (long long)B * Hkv, place = 4 * d + 8;         // bytes of a part's results
+    p.few_tokens = p.tile && p.few && (long long)B * (16 / G) < T ? 16 / G : 0;
+    const long long few_rows = (long long)H * (p.few_tokens ? (long long)B * p.few_tokens : T);
     if (p.few) {
         // two workgroups a compute unit of at least 256 keys each: four of 128 cost the join what they gain (one sequence of 32700 tokens 21.9 instead of
         // 19.8 us, 64 of 2000, which need no join then, 48 instead of 43), one leaves the memory waiting (16 fp32 sequences of 4000: 52.7 instead of 47.5).
         // No part longer than 2048 keys, for sequences of different lengths (32 of up to 32768: 202 us, with 4096 205).
         long long s = std::max((512 + pairs - 1) / pairs, (len + 2047) / 2048);
         s = std::min(s, (len + 255) / 256);
+        s = std::min(s, std::max((512 + pairs - 1) / pairs, kPartBytes / (few_rows * (place + 4))));
         p.few_splits = (int)std::max(1ll, std::min(s, 256ll));
     }
     if (p.tile) {
@@ -898,8 +969,15 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
     if ((long long)T * H * (d / 4) + 256 > kMostThreads) p.few_splits = p.tile_splits = 1;       // no join
     p.fits = blocks() * threads <= kMostThreads;
     p.part_keys = (int)((len + p.tile_splits - 1) / p.tile_splits);
-    const int most = std::max(p.few_splits, p.tile_splits);
-    if (most > 1) p.partial_bytes = (size_t)T * H * (most * ((size_t)d * 4 + 8) + 4);
+    const long long most = std::max(p.few_splits, p.tile_splits), rows_all = (long long)T * H;
+    if (most == 1) return p;
+    const long long few = p.few_splits > 1 ? few_rows * p.few_splits : 0;
+    const long long tile = p.tile_splits > 1 ? std::min(rows_all * p.tile_splits, std::max(5 * rows_all / 2, kPartBytes / 2 / place)) : 0;
+    const long long all = rows_all * (most * place + 4), shared = (few + tile) * place + 8 * rows_all;
+    p.packed = all > std::max(kPartBytes, shared);
+    p.few_places = p.packed ? few : 0;
+    p.tile_places = p.packed ? tile : rows_all * most;
+    p.partial_bytes = (size_t)(p.packed ? shared : all);
     return p;
 }
 
@@ -923,11 +1001,16 @@ hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const Atte
     k.part_keys = p.part_keys;
     k.tiles = p.tiles;
     k.c = a.scale * kLog2E;
-    const size_t most = std::max(p.few_splits, p.tile_splits);
-    k.slots = (int)most;
+    const size_t places = (size_t)(p.few_places + p.tile_places);
+    k.slots = std::max(p.few_splits, p.tile_splits);
+    k.packed = p.packed;
+    k.few_tokens = p.few_tokens;
+    k.few_places = p.few_places;
+    k.tile_places = p.tile_places;
     k.part = (float *)ws;
-    k.stat = (float2 *)((char *)ws + (size_t)a.T * a.H * most * d * 4);
-    k.count = (int *)(k.stat + (size_t)a.T * a.H * most);
+    k.stat = (float2 *)((char *)ws + places * d * 4);
+    k.count = (int *)(k.stat + places);
+    k.first = (unsigned *)(k.count + (size_t)a.T * a.H);
     const bool stream = 2 * kv.layer_bytes * layers > kStreamBytes;
     k.few_splits = p.few_splits;
     k.tile_splits = p.tile_splits;

@@ -64,6 +64,9 @@ struct AttendPlan {
     int few, tile;                   // whether each kernel is launched
     int few_rows;                    // rows (new tokens x heads of a key head) that the kernel of few rows takes, 0 if it is not launched
     int few_splits, tile_splits, tiles, tile_waves, part_keys;
+    bool packed;                     // rows have as many places for partial results as parts, not all the same number
+    int few_tokens;                  // of a sequence, that have places of their own for few rows (0: all tokens of the batch)
+    long long few_places, tile_places;
     size_t partial_bytes;            // of all rows' split results
 };
 struct AttendArgs {

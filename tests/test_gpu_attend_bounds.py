@@ -1,7 +1,10 @@
-"""Bounds that the sequences do not keep."""
+"""Bounds that the sequences do not keep, and batches whose parts of keys share a small workspace."""
+import numpy as np
 import pytest
 import torch
 
+import paged_ref as ref
+from paper_2502_18394_amd import binding
 from test_gpu_attend import DT, check, make, queries
 
 pytestmark = pytest.mark.gpu
@@ -49,3 +52,41 @@ def test_lengths_above_their_bound(io, news, lens, window):
             b = int(t >= news[0])
             p = lens[b] - news[b] + t - b * news[0]
             check(out[t:t + 1], lse[t:t + 1], q[t:t + 1], [1], [(rows[b][0][:p + 1], rows[b][1][:p + 1])], 0.125, DT[io], window)
+
+
+@pytest.mark.parametrize("io,d,H,Hkv", [("bf16", 64, 32, 2), ("bf16", 128, 16, 4), ("f32", 64, 16, 8), ("bf16", 64, 32, 1)])
+@pytest.mark.parametrize("news,lens", [([1, 700, 3, 0, 1500, 1, 200], [9100, 9500, 20, 500, 8000, 4000, 14000]), ([2000, 1, 2500, 2300], [9000, 70, 9700, 8800])])
+def test_parts_share_a_workspace(io, d, H, Hkv, news, lens):
+    """A bound of lengths far above most of them: rows have as many parts as their own sequence needs, and fewer where all parts together would not fit."""
+    print(f"case {io} d={d} H={H} Hkv={Hkv} {news}", flush=True)
+    most = 131072
+    pool, rows = make(io, d, Hkv, 64, lens, d + H)
+    q, start = queries(news, H, d, io, 7)
+    T = sum(news)
+    need = max(pool.attend_workspace_bytes(len(news), T, H, max(news), most, window) for window in (0, 6000))
+    assert need <= max(128 << 20, 5 * T * H // 2 * (4 * d + 8)) + (256 << 20) + 8 * T * H + 4096
+    given = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")       # NaN everywhere, counts of -1
+    behind = torch.full((1 << 20,), 77, dtype=torch.uint8, device="cuda")
+    for window in (0, 6000):
+        out, lse = pool.attend(0, q, start, max_new=max(news), max_len=most, window=window, want_lse=True, ws=given)
+        again = pool.attend(0, q, start, max_new=max(news), max_len=most, window=window, ws=given)
+        assert torch.equal(out, again) and torch.isfinite(out).all() and torch.isfinite(lse).all()
+        r = np.random.default_rng(3)
+        for b, (n, m) in enumerate(zip(news, lens)):
+            for i in sorted({0, n - 1, *r.integers(0, n, 3).tolist()}) if n else []:
+                t, p = int(start[b]) + i, m - n + i
+                check(out[t:t + 1], lse[t:t + 1], q[t:t + 1], [1], [(rows[b][0][:p + 1], rows[b][1][:p + 1])], d ** -0.5, DT[io], window)
+    assert (behind == 77).all()
+
+
+def test_bounds_so_loose_that_parts_are_left_out():
+    """64 single tokens at the front of a batch that could be 65536 new tokens of sequences of 131072: as many parts as a launch can have."""
+    H, Hkv, B = 32, 8, 64
+    lens = [300 + 37 * b for b in range(B)]
+    pool, rows = make("bf16", 64, Hkv, 64, lens, 2)
+    q, start = queries([1] * B, H, 64, "bf16", 3)
+    wide = torch.cat((q, q.new_zeros((1 << 16) - B, H, 64)))
+    out = torch.full_like(wide, 9.0)
+    _, lse = pool.attend(0, wide, start, max_new=1 << 16, max_len=131072, out=out, want_lse=True)
+    assert (out[B:] == 9.0).all()
+    check(out[:B], lse[:B], q, [1] * B, rows, 0.125, DT["bf16"])

@@ -8,6 +8,7 @@ import pytest
 from paper_2502_18394_amd import binding
 from test_paged_refusals import FAKE, FAR, OUT, lib, pool  # noqa: F401
 
+MB = 1 << 20
 
 
 def test_an_empty_batch_has_a_plan(lib):  # noqa: F811
@@ -28,6 +29,20 @@ def test_an_empty_batch_has_a_plan(lib):  # noqa: F811
 def _sizes(lib, B, T, H, new, most, **change):
     c = pool(layers=1, pages=1 << 16, Hkv=8, page=64, seqs=4096, max_pages=1 << 14, **change)
     return lib.spectre_kv_attend_workspace_bytes(ctypes.byref(c), B, T, H, new, most, 0)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_workspaces_are_in_proportion(lib, d):  # noqa: F811
+    size = lambda *a: _sizes(lib, *a, d=d)
+    row = 4 * d + 8
+    # a chunk beside decoding sequences, at the longest lengths; many ragged sequences; the chunk alone, of one length
+    assert 0 < size(32, 8192 + 31, 32, 8192, 131072) < 512 * MB
+    assert 0 < size(32, 2048 + 31, 32, 2048, 131072) < 300 * MB
+    assert 0 < size(48, 60000, 32, 2000, 36000) < 60000 * 32 * (5 * row // 2 + 8) + 64 * MB
+    assert 0 < size(1, 8192, 32, 8192, 131072) < 4 * MB
+    # many single tokens of long sequences
+    assert 0 < size(4096, 4096, 32, 1, 131072) < 300 * MB
+    assert 0 < size(256, 256, 32, 1, 131072) < 300 * MB
 
 
 @pytest.mark.parametrize("dtype", [binding.F32, binding.BF16])
