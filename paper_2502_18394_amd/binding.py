@@ -545,6 +545,14 @@ def _now(stream):
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
 
 
+def _capturing(stream):
+    """Whether work on `stream` (None: the current one) is being captured into a graph."""
+    if stream is None:
+        return torch._C._cuda_isCurrentStreamCapturing()
+    with torch.cuda.stream(stream):
+        return torch._C._cuda_isCurrentStreamCapturing()
+
+
 _kv_prepared = set()
 
 
@@ -694,10 +702,10 @@ class KvPages:
     def table(self):
         return self.book[8 + self.seqs + self.pages:].view(self.seqs, self.max_pages)
 
-    def _scratch(self, kind, stream, need=0):
-        """(address, bytes) of the pool's workspace, kept between calls (one for the attention, one for the pages: a pool works on one stream at a time)."""
+    def _scratch(self, kind, stream, now, need=0):
+        """(address, bytes) of the pool's workspace, kept between calls (one for the attention, one for the pages: a pool works on one stream at a time);
+        now: the stream's handle.  Captured calls have memory of their own instead, which lives as long as their graph: this one is replaced as soon as a call needs more."""
         own, raw, at, have = self._ws.get(kind, (None, 0, None, 0))
-        now = _now(stream)
         if have < need:
             own = _new((need + 256,), torch.uint8, self.book.device, stream)
             at, have = _given(own)
@@ -706,18 +714,29 @@ class KvPages:
             own.record_stream(torch.cuda.current_stream() if stream is None else stream)
         return at, have
 
-    def _pages_ws(self, n, ws, stream):
-        return _given(ws) if ws is not None else self._scratch("pages", stream, lib().spectre_kv_workspace_bytes(self._ref, n))
+    def _fresh(self, need, stream):
+        """Workspace of one captured call.  Its caller holds it until the call has been captured; the graph keeps the memory from then on."""
+        return _new((need + 256,), torch.uint8, self.book.device, stream)
+
+    def _pages_call(self, call, lists, n, ws, stream):
+        """reserve, fork or compact with their lists, a workspace (of a list of n) and the stream."""
+        now = _now(stream)
+        if ws is None:
+            need = lib().spectre_kv_workspace_bytes(self._ref, n)
+            if _capturing(stream):
+                ws = self._fresh(need, stream)
+        at, have = self._scratch("pages", stream, now, need) if ws is None else _given(ws)
+        _check(call(self._ref, *lists, at, have, now))
 
     def reserve(self, seqs, add, ws=None, stream=None):
         """Sequence seqs[i] grows by add[i] tokens (int32 on the device); room that is missing is reported in `status`, and then nothing changes."""
         n = seqs.numel()
-        _check(lib().spectre_kv_reserve(self._ref, _ints(seqs, "seqs"), _ints(add, "add", n), n, *self._pages_ws(n, ws, stream), _now(stream)))
+        self._pages_call(lib().spectre_kv_reserve, (_ints(seqs, "seqs"), _ints(add, "add", n), n), n, ws, stream)
 
     def fork(self, src, dst, ws=None, stream=None):
         """The empty sequences dst[i] become what src[i] are: full pages shared, the last one copied."""
         n = src.numel()
-        _check(lib().spectre_kv_fork(self._ref, _ints(src, "src"), _ints(dst, "dst", n), n, *self._pages_ws(n, ws, stream), _now(stream)))
+        self._pages_call(lib().spectre_kv_fork, (_ints(src, "src"), _ints(dst, "dst", n), n), n, ws, stream)
 
     def free(self, seqs, stream=None):
         """The sequences end; pages that nobody else uses are free."""
@@ -725,7 +744,7 @@ class KvPages:
 
     def compact(self, ws=None, stream=None):
         """Pages in use move to the front of the pool; status[2] = how many there are."""
-        _check(lib().spectre_kv_compact(self._ref, *self._pages_ws(0, ws, stream), _now(stream)))
+        self._pages_call(lib().spectre_kv_compact, (), 0, ws, stream)
 
     def copy(self, src, dst, stream=None):
         """Contents of page src[i] of every layer to page dst[i]."""
@@ -780,10 +799,13 @@ class KvPages:
             raise ValueError("lse must be float32 [T, H]")
         args = (self._ref, layer, qa, qs, _ints(start, "start"), None if seqs is None else _ints(seqs, "seqs", B), B, T, H, max_new, max_len,
                 1.0 / d ** 0.5 if scale is None else scale, window, _ptr(out, "out"), None if lse is None else _ptr(lse, "lse"))
-        at, have = _given(ws) if ws is not None else self._scratch("attend", stream)
-        rc = lib().spectre_kv_attend(*args, at, have, _now(stream))
+        now = _now(stream)
+        if ws is None and _capturing(stream):
+            ws = self._fresh(lib().spectre_kv_attend_workspace_bytes(self._ref, B, T, H, max_new, max_len, window), stream)
+        at, have = _given(ws) if ws is not None else self._scratch("attend", stream, now)
+        rc = lib().spectre_kv_attend(*args, at, have, now)
         if rc == EWORKSPACE and ws is None:    # the library checks the size; asking for it first is a call of its own
-            at, have = self._scratch("attend", stream, lib().spectre_kv_attend_workspace_bytes(self._ref, B, T, H, max_new, max_len, window))
-            rc = lib().spectre_kv_attend(*args, at, have, _now(stream))
+            at, have = self._scratch("attend", stream, now, lib().spectre_kv_attend_workspace_bytes(self._ref, B, T, H, max_new, max_len, window))
+            rc = lib().spectre_kv_attend(*args, at, have, now)
         _check(rc)
         return (out, lse) if lse is not None else out
