@@ -473,7 +473,8 @@ int spectre_kv_init(const spectre_kv *kv /*host*/, void *stream);
  * Page management; seqs, src, dst, add are device int32 [n], n = 0 is a call that does nothing.  Pages are taken lowest number first, in the
  * order of the list.  A call that cannot be carried out as a whole sets bits of the status and changes nothing else
  * (spectre_kv_free and _copy: leave out what is out of range).
- *   reserve  sequence seqs[i] grows by add[i] >= 0 tokens, whose contents are whatever the pages hold.  No sequence twice.
+ *   reserve  sequence seqs[i] grows by add[i] >= 0 tokens, whose contents are whatever the pages hold.  No sequence twice.  After one that failed
+ *            spectre_kv_append writes nothing until the caller has cleared the status, so a captured step that runs out of pages does no harm.
  *   fork     dst[i], empty, becomes what src[i] is: full pages are shared, the tokens of a last page that is not full are copied (in
  *            whole 16-byte groups of V) into a page of its own, in every layer.  No dst twice, none that is a src.
  *   free     the sequences' pages lose a user each; the sequences are empty.
@@ -512,7 +513,8 @@ int spectre_heads_backward(const spectre_heads *P /*host*/, const void *dq, long
 
 /* Serving: the new tokens are the last ones of their sequences (spectre_kv_reserve has made room): token i of the n of sequence seqs[b] (NULL: b) has
  * position lens - n + i.  Queries go to q_out [T, H, d], keys, with norm and rotation, and values into the pages of `layer`.  A sequence of
- * fewer than n tokens, or a row outside the table, is left out.  No sequence twice. */
+ * fewer than n tokens, or a row outside the table, is left out.  No sequence twice.  While one of the bits that a failed reserve sets (NO_PAGES, TOO_LONG,
+ * BAD_ARGUMENT) stands in the status, whichever call set it, every sequence is left out: without the reserve the places of the new tokens are those of the last ones. */
 int spectre_kv_append(const spectre_kv *kv /*host*/, int layer, const spectre_heads *P /*host*/, const void *q, long long q_stride, const void *k,
                       long long k_stride, const void *v, long long v_stride, const int *start, const int *seqs, int B, int T, int H,
                       void *q_out, void *stream);

@@ -729,7 +729,8 @@ class KvPages:
         _check(call(self._ref, *lists, at, have, now))
 
     def reserve(self, seqs, add, ws=None, stream=None):
-        """Sequence seqs[i] grows by add[i] tokens (int32 on the device); room that is missing is reported in `status`, and then nothing changes."""
+        """Sequence seqs[i] grows by add[i] tokens (int32 on the device); room that is missing is reported in `status`, and then nothing changes, nor does
+        append() write anything until status[0] has been cleared."""
         n = seqs.numel()
         self._pages_call(lib().spectre_kv_reserve, (_ints(seqs, "seqs"), _ints(add, "add", n), n), n, ws, stream)
 

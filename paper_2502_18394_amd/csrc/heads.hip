@@ -174,7 +174,12 @@ struct Run {
     int seq;                        // its row of the table
 };
 
+// Bits of the status that a reserve which could not be done leaves.  Its sequences have not grown, so what would be taken for the new tokens' places holds their last ones:
+// nothing is written while a bit stands.
+constexpr int kNotReserved = SPECTRE_KV_NO_PAGES | SPECTRE_KV_TOO_LONG | SPECTRE_KV_BAD_ARGUMENT;
+
 __device__ __forceinline__ bool find_run(const KvView &kv, const int *start, const int *seqs, int B, int T, int block, Run *r) {
+    const int status = kv.status[0];
     int lo = 0, hi = B;             // the last b with start[b] / kTokens + 2 b <= block: 64 asked at once (19 fp32 sequences of up to 700 tokens 18.6 us, by halves 19.0)
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) >> 6, mid = lo + step * (int)(threadIdx.x & 63);
@@ -184,7 +189,7 @@ __device__ __forceinline__ bool find_run(const KvView &kv, const int *start, con
     }
     const int from = start[lo], to = min(start[lo + 1], T), n = to - from;
     const int row = seqs ? seqs[lo] : lo;
-    if (from < 0 || n <= 0 || (unsigned)row >= (unsigned)kv.S) return false;
+    if ((status & kNotReserved) || from < 0 || n <= 0 || (unsigned)row >= (unsigned)kv.S) return false;
     const int had = kv.lens[row] - n;          // tokens before the new ones
     if (had < 0) return false;
     const int run = block - (from / kTokens + 2 * lo);
