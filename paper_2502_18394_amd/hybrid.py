@@ -56,8 +56,20 @@ class HybridDecoder:
         o = self.pool.attend(self.order[layer], q, start, seqs, max_new, self.window)
         return x + o.view(T, self.width) @ w["out"]
 
+    def _room(self, more):
+        """The spectral layers' window and the rows of the pool's table end here."""
+        if self.tokens + more > self.window:
+            raise ValueError(f"{self.tokens} tokens and {more} more: the window has {self.window}")
+
+    def check(self):
+        """What the calls on the pool found wrong (the host waits for them here, once a run; after a failed reserve they have written nothing)."""
+        status = int(self.pool.status[0])
+        if status:
+            raise RuntimeError(f"pool status {status}")
+
     def prompt(self, tokens, chunk):
         """The prompt (sequence 0) in chunks; returns the last token's row."""
+        self._room(tokens.numel())
         seq = self.all[:1]
         for part in tokens.split(chunk):
             T = part.numel()
@@ -114,6 +126,7 @@ class HybridDecoder:
 
     def step(self, tokens, captured=True):
         """One token for every sample; returns their rows."""
+        self._room(1)
         x = self.embed[tokens]
         self.pool.reserve(self.all[1:], self.one[1:])
         for layer in range(len(self.attention) + len(self.spectral)):
@@ -146,6 +159,7 @@ def run(prompt, chunk, samples, new, noise, captured=True, **sizes):
     for i in range(new):
         got.append(m.choose(x, noise[i]))
         x = m.step(got[-1], captured)
+    m.check()
     return torch.stack(got, 1), m
 
 
