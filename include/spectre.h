@@ -458,7 +458,7 @@ enum { SPECTRE_KV_K = 0, SPECTRE_KV_V = 1, SPECTRE_KV_BOOK = 2 };
 
 /* Words of the status (book[0 .. 7]): [0] bits of what calls found wrong, kept until the caller clears them; [1] pages that the last
  * spectre_kv_fork or _compact copied; [2] pages in use after the last _compact. */
-enum { SPECTRE_KV_NO_PAGES = 1, SPECTRE_KV_TOO_LONG = 2, SPECTRE_KV_BAD_ARGUMENT = 4, SPECTRE_KV_NOT_EMPTY = 8 };
+enum { SPECTRE_KV_NO_PAGES = 1, SPECTRE_KV_TOO_LONG = 2, SPECTRE_KV_BAD_ARGUMENT = 4, SPECTRE_KV_NOT_EMPTY = 8, SPECTRE_KV_SHARED = 16 };
 
 /* Bytes of the pool's arrays (which: SPECTRE_KV_K, _V, _BOOK); 0 for a pool that is not supported.  Only sizes and dtype are read. */
 size_t spectre_kv_bytes(const spectre_kv *kv /*host*/, int which);
@@ -514,7 +514,8 @@ int spectre_heads_backward(const spectre_heads *P /*host*/, const void *dq, long
 /* Serving: the new tokens are the last ones of their sequences (spectre_kv_reserve has made room): token i of the n of sequence seqs[b] (NULL: b) has
  * position lens - n + i.  Queries go to q_out [T, H, d], keys, with norm and rotation, and values into the pages of `layer`.  A sequence of
  * fewer than n tokens, or a row outside the table, is left out.  No sequence twice.  While one of the bits that a failed reserve sets (NO_PAGES, TOO_LONG,
- * BAD_ARGUMENT) stands in the status, whichever call set it, every sequence is left out: without the reserve the places of the new tokens are those of the last ones. */
+ * BAD_ARGUMENT) stands in the status, whichever call set it, every sequence is left out: without the reserve the places of the new tokens are those of the last ones.
+ * Nothing is written into a page that several sequences use: SPECTRE_KV_SHARED is set instead. */
 int spectre_kv_append(const spectre_kv *kv /*host*/, int layer, const spectre_heads *P /*host*/, const void *q, long long q_stride, const void *k,
                       long long k_stride, const void *v, long long v_stride, const int *start, const int *seqs, int B, int T, int H,
                       void *q_out, void *stream);

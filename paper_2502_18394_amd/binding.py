@@ -645,7 +645,7 @@ class KvPages:
     k_pages [layers, pages, Hkv, d/E, page, E], v_pages [layers, pages, Hkv, page/E, d, E] (E = 8 bf16 or 4 f32 elements),
     book int32 [8 + seqs + pages + seqs * max_pages]."""
 
-    NO_PAGES, TOO_LONG, BAD_ARGUMENT, NOT_EMPTY = 1, 2, 4, 8          # bits of the status
+    NO_PAGES, TOO_LONG, BAD_ARGUMENT, NOT_EMPTY, SHARED = 1, 2, 4, 8, 16          # bits of the status
 
     def __init__(self, k_pages, v_pages, book, seqs, max_pages):
         io = _dtype_code(k_pages)

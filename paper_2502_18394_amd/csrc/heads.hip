@@ -216,17 +216,19 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
         weights[0][i] = P.wq ? P.wq[i] : 1.f;
         weights[1][i] = P.wk ? P.wk[i] : 1.f;
     }
-    __syncthreads();
-    fill_turns(P, pos, run.count, turns);
-    __syncthreads();
-
     int page = 0, slot = 0;
     if (SERVE) {                                   // kTokens divides a page: one page a workgroup
         const int p = run.index >> kv.page_log;
         page = p < kv.M ? kv.table[(long long)run.seq * kv.M + p] : -1;
         slot = run.index & ((1 << kv.page_log) - 1);
     }
+    __syncthreads();
+    fill_turns(P, pos, run.count, turns);
+    __syncthreads();
+
+    // A page with several users holds another sequence's tokens, too: a reserve would have given the new ones a page of their own.  (Looked at where keys are written.)
     const bool in_pool = SERVE && (unsigned)page < (unsigned)kv.P;
+    const int users = in_pool ? kv.refs[page] : 0;
 
     // rows in the order (head, token), tokens padded to a power of two, so that a thread stays with one token and one group of channels
     int tl = 0;
@@ -256,13 +258,17 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
             if (!there || h >= heads) continue;
             if (!key) put(&q_out[(t * X.H + h) * LANES + L.lane], o, stream);
             else if (!SERVE) put(&k_out[(t * X.Hkv + h - X.H) * LANES + L.lane], o, stream);
-            else if (in_pool) {
+            else if (in_pool && users <= 1) {
                 const long long block = ((long long)page * X.Hkv + h - X.H) * LANES + L.lane;
                 reinterpret_cast<uint4 *>(kv.k)[(block << kv.page_log) + slot + token] = o;
             }
         }
     }
     if (!in_pool) return;
+    if (users > 1) {
+        if (threadIdx.x == 0) atomicOr(&kv.status[0], SPECTRE_KV_SHARED);
+        return;
+    }
     // values: a lane holds one channel of every token of the run and writes whole groups where the run has them
     typedef typename IO::elem_t elem_t;
     const elem_t *v = reinterpret_cast<const elem_t *>(X.v);

@@ -97,3 +97,23 @@ def test_a_captured_step_that_runs_out_of_pages():
         graph.replay()
         torch.cuda.synchronize()
         _untouched(pool, full, binding.KvPages.NO_PAGES)
+
+
+def test_pages_with_several_users_are_not_written():
+    pool = _pool(8, 3, 4)
+    pool.reserve(_ints(0), _ints(2 * page))
+    pool.fork(_ints(0), _ints(1))
+    before = _all(pool)
+    start, rope = _ints(0, 3), binding.Rope.of(d)
+    for s in (0, 1):                                         # no reserve: the last tokens of both lie in a page of both
+        pool.append(1, *_tokens(3), start, _ints(s), rope)
+        _untouched(pool, before, binding.KvPages.SHARED)
+    pool.status.zero_()
+    pool.reserve(_ints(1), _ints(3))
+    pool.append(1, *_tokens(3), start, _ints(1), rope)
+    assert int(pool.status[0]) == 0
+    number = int(pool.table[1, 2])
+    assert not torch.equal(pool.k_pages[1, number, :, :, :3], before[0][1, number, :, :, :3])
+    rest = torch.ones(8, dtype=torch.bool)
+    rest[number] = False
+    assert torch.equal(pool.k_pages[:, rest], before[0][:, rest]) and torch.equal(pool.v_pages[:, rest], before[1][:, rest])
