@@ -476,7 +476,8 @@ int spectre_kv_init(const spectre_kv *kv /*host*/, void *stream);
  *   reserve  sequence seqs[i] grows by add[i] >= 0 tokens, whose contents are whatever the pages hold.  No sequence twice.  After one that failed
  *            spectre_kv_append writes nothing until the caller has cleared the status, so a captured step that runs out of pages does no harm.
  *   fork     dst[i], empty, becomes what src[i] is: full pages are shared, the tokens of a last page that is not full are copied (in
- *            whole 16-byte groups of V) into a page of its own, in every layer.  No dst twice, none that is a src.
+ *            whole 16-byte groups of V) into a page of its own, in every layer (one that is outside the pool is so in the child, too).  No dst twice, none
+ *            that is a src.
  *   free     the sequences' pages lose a user each; the sequences are empty.
  *   compact  pages in use move so that their numbers are 0 .. in use - 1: the i-th page in use above goes to the i-th free one below.
  *   copy     the contents of page src[i] of every layer to page dst[i]; no dst twice, none that is a src.

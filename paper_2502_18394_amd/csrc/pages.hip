@@ -136,12 +136,17 @@ __global__ __launch_bounds__(kScan) void k_kv_reserve(KvView kv, const int *seqs
     }
 }
 
+// Whether the last page of sequence s, of `len` tokens, has to be copied for a child: it is not full, and in the pool (one that is absent is absent in the child, too).
+__device__ __forceinline__ bool copies_last(const KvView &kv, int s, int len) {
+    if ((len & ((1 << kv.page_log) - 1)) == 0) return false;
+    return (unsigned)kv.table[(long long)s * kv.M + (len >> kv.page_log)] < (unsigned)kv.P;
+}
+
 // Which parents' last pages have to be copied, and the pages that take them: ws [0] done, list[i] = page of child i or -1.
 __global__ __launch_bounds__(kScan) void k_kv_fork_plan(KvView kv, const int *src, const int *dst, int n, int *ws) {
     __shared__ uint32_t from[kSeqWords], to[kSeqWords];
     __shared__ int waves[kScan / 64];
     __shared__ int bad;
-    const int page = 1 << kv.page_log;
     for (int i = threadIdx.x; i < (kv.S + 31) / 32; i += kScan) from[i] = to[i] = 0;
     if (threadIdx.x == 0) bad = 0;
     __syncthreads();
@@ -158,7 +163,7 @@ __global__ __launch_bounds__(kScan) void k_kv_fork_plan(KvView kv, const int *sr
                 if (kv.lens[b] != 0) atomicOr(&bad, SPECTRE_KV_NOT_EMPTY);
                 const int len = kv.lens[a];
                 if (len < 0 || len > (long long)kv.M << kv.page_log) atomicOr(&bad, SPECTRE_KV_BAD_ARGUMENT);
-                mine = (len & (page - 1)) != 0;
+                else mine = copies_last(kv, a, len);
             }
         }
         int total;
@@ -182,7 +187,7 @@ __global__ __launch_bounds__(kScan) void k_kv_fork_plan(KvView kv, const int *sr
     int first = 0;
     for (int base = 0; base < n; base += kScan) {
         const int i = base + threadIdx.x;
-        const int mine = i < n && (kv.lens[src[i]] & (page - 1)) != 0;
+        const int mine = i < n && copies_last(kv, src[i], kv.lens[src[i]]);
         int total;
         const int at = first + scan_before(mine, &total, waves);
         if (i < n) child[i] = mine ? list[at] : -1;
@@ -199,7 +204,7 @@ __global__ __launch_bounds__(256) void k_kv_fork(KvView kv, int layers, int d, i
     if (blockIdx.y == 0) {
         for (int j = threadIdx.x; j < kv.M; j += 256) {
             int p = -1;
-            if (j < full) {
+            if (j < full || (j == full && rest && fresh < 0)) {
                 p = kv.table[(long long)a * kv.M + j];
                 if ((unsigned)p < (unsigned)kv.P) atomicAdd(&kv.refs[p], 1);
             } else if (j == full && rest) {
@@ -210,9 +215,8 @@ __global__ __launch_bounds__(256) void k_kv_fork(KvView kv, int layers, int d, i
         }
         if (threadIdx.x == 0) kv.lens[b] = len;
     }
-    if (!rest) return;
+    if (!rest || fresh < 0) return;
     const int old = kv.table[(long long)a * kv.M + full];
-    if ((unsigned)old >= (unsigned)kv.P) return;
     // The 16-byte groups that hold the tokens: K rows of `some` groups of a page's `page`, V rows one after the other.
     const int some = (rest + E - 1) / E * E, lanes = d / E;
     const long long block = (long long)kv.Hkv * lanes << kv.page_log;          // groups of one page

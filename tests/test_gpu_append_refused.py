@@ -117,3 +117,24 @@ def test_pages_with_several_users_are_not_written():
     rest = torch.ones(8, dtype=torch.bool)
     rest[number] = False
     assert torch.equal(pool.k_pages[:, rest], before[0][:, rest]) and torch.equal(pool.v_pages[:, rest], before[1][:, rest])
+
+
+@pytest.mark.parametrize("absent", [-1, 8, 2 ** 31 - 1])
+def test_a_fork_of_a_last_page_that_is_absent(absent):
+    """The child is what its parent is: the tokens of a page outside the pool are absent in both, and no page is taken for them."""
+    pool = _pool(8, 4, 3)
+    pool.reserve(_ints(0, 1), _ints(page + 5, 7))
+    pool.table[0, 1] = absent
+    refs = pool.refs.clone()
+    before = _all(pool)
+    pool.fork(_ints(0, 1), _ints(2, 3))
+    assert pool.table[2].tolist() == [int(before[2][12 + 8]), absent, -1] and pool.lens.tolist() == [page + 5, 7, page + 5, 7]
+    fresh = int(pool.table[3, 0])
+    refs[int(pool.table[0, 0])] += 1
+    refs[fresh] += 1
+    assert torch.equal(pool.refs, refs) and pool.status[:2].tolist() == [0, 1]
+    q = torch.randn(1, H, d, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()
+    one = _ints(0, 1)
+    assert torch.equal(pool.attend(0, q, one, _ints(0), 1), pool.attend(0, q, one, _ints(2), 1))
+    pool.free(_ints(0, 1, 2, 3))
+    assert int((pool.refs > 0).sum()) == 1                    # the page that the table lost
