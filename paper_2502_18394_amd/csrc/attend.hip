@@ -8,8 +8,11 @@
 // formed transposed, S^T = K Q^T and O^T = V^T P^T, so that a row of scores lies in one lane (and its mate 32 or 16 lanes on): the softmax needs almost no
 // exchange, and what a lane holds of P^T after S^T is what the second product wants of it, without a move.  For that the keys of a bf16 tile are
 // given to the matrix instruction in an order in which each lane ends up with runs of 8.
-// Probabilities go to the matrix cores in the type of the rows: bf16 rounds each to half a step of 2^-8, errors of independent signs that average
-// out like the values they weigh, so outputs are as far off as by their own rounding; the sum in the denominator is of the unrounded ones.
+// Probabilities go to the matrix cores in the type of the rows.  Of few rows, where memory leaves the matrix cores idle, a bf16 probability goes as two terms, itself rounded and
+// the rest: outputs are off by their own rounding (1.64e-3 over all, 2.1e-3 with one term; 32 sequences of up to 32768 tokens 186 us, with one 185).  In tiles, which the matrix
+// cores and the vector unit bound, it goes as one, rounded to half a step of 2^-8: errors of independent signs that average out like the values they weigh, 2.2e-3
+// where the output's rounding alone is 1.65e-3 (an 8192-token prompt 336 us, with two terms 449; 16 tokens over 1000 for 90 sequences, d = 128, 41 and 49).
+// The sum in the denominator is of the unrounded ones.
 // Keys that nobody of the row's may see take no part whatever lies there: their scores are replaced, not shifted, and values that are infinite or NaN are
 // taken out of the tiles where rows see different keys and added for the rows that do see them.
 #include <math.h>
@@ -140,6 +143,17 @@ struct Bf16Mma {
         return make_uint4(IoBf16::pack(make_float2(p[0], p[1])), IoBf16::pack(make_float2(p[2], p[3])), IoBf16::pack(make_float2(p[4], p[5])),
                           IoBf16::pack(make_float2(p[6], p[7])));
     }
+    // what pack() left of the numbers
+    __device__ static __forceinline__ uint4 pack_rest(const float *p, uint4 g) {
+        const uint32_t w[4] = {g.x, g.y, g.z, g.w};
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = p[2 * i] - __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = p[2 * i + 1] - __uint_as_float(w[i] & 0xffff0000u);
+        }
+        return pack(x);
+    }
     __device__ static __forceinline__ bool finite(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (w & 0x7f800000u) != 0x7f800000u; }
     __device__ static __forceinline__ uint32_t finite_only(uint32_t w) {
         return ((w & 0x7f80u) == 0x7f80u ? 0u : w & 0xffffu) | ((w & 0x7f800000u) == 0x7f800000u ? 0u : w & 0xffff0000u);
@@ -183,6 +197,19 @@ __device__ __forceinline__ uint4 keep_first(uint4 g, int n) {
 }
 template <typename IO>
 __device__ __forceinline__ bool all_finite(uint4 g) { return IO::finite(g.x) && IO::finite(g.y) && IO::finite(g.z) && IO::finite(g.w); }
+// The same of N groups of bf16: the largest of all magnitudes, two at a time.
+template <int N>
+__device__ __forceinline__ bool all_finite_bf16(const uint4 (&g)[N]) {
+    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+    u16x2_t most = {0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t w[4] = {g[i].x, g[i].y, g[i].z, g[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2_t, w[j] & 0x7fff7fffu));
+    }
+    return most[0] < 0x7f80 && most[1] < 0x7f80;
+}
 template <typename IO>
 __device__ __forceinline__ uint4 finite_only(uint4 g) {
     return make_uint4(IO::finite_only(g.x), IO::finite_only(g.y), IO::finite_only(g.z), IO::finite_only(g.w));
@@ -673,6 +700,11 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (absent || at + (4 * t + e) >= span) sc[t][e] = -INFINITY;
+            }
+            // two terms of a probability may be of different signs, or one of them zero: infinite values go their own way in every step
+            bool look = edge;
+            if constexpr (E == 8) look = look || __ballot(!all_finite_bf16<DT>(vr)) != 0;
+            if (look) {
                 const int have = s.m - (base + E * quarter);
                 bool fine = true;
 #pragma unroll
@@ -709,6 +741,11 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
             const uint4 pg = IO::pack(p);
 #pragma unroll
             for (int d = 0; d < DT; ++d) IO::mma16(o[d], vr[d], pg);
+            if constexpr (E == 8) {                        // the rest of the probabilities: four more products a step cost nothing here
+                const uint4 rest = IO::pack_rest(p, pg);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) IO::mma16(o[d], vr[d], rest);
+            }
             if (more) request_values(base + WAVES * SK);
             if (odd)
                 add_not_finite<IO, D, 4 * DT>(kv, s, h, base, SK, pos, lowest - 1, [quarter](int n) { return 16 * (n / 4) + 4 * quarter + n % 4; },
