@@ -692,7 +692,6 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
                 for (int j = 0; j < QG; ++j) IO::mma16(sc[t], kr[t * QG + j], q[j]);
             }
             if (more) request_keys(base + WAVES * SK);
-            bool odd = false;
             if (edge) {
                 const unsigned at = (unsigned)(base + E * quarter - lowest);
 #pragma unroll
@@ -700,22 +699,6 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (absent || at + (4 * t + e) >= span) sc[t][e] = -INFINITY;
-            }
-            // two terms of a probability may be of different signs, or one of them zero: infinite values go their own way in every step
-            bool look = edge;
-            if constexpr (E == 8) look = look || __ballot(!all_finite_bf16<DT>(vr)) != 0;
-            if (look) {
-                const int have = s.m - (base + E * quarter);
-                bool fine = true;
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    if (have < E) vr[d] = keep_first<IO>(vr[d], have);
-                    if (!all_finite<IO>(vr[d])) {
-                        fine = false;
-                        vr[d] = finite_only<IO>(vr[d]);
-                    }
-                }
-                odd = __ballot(!fine) != 0;
             }
             float mx = sc[0][0];
 #pragma unroll
@@ -738,6 +721,22 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
                     p[4 * t + e] = exp2_fast(fmaf(sc[t][e], k.c, shift));
                     sum += p[4 * t + e];
                 }
+            // two terms of a probability may be of different signs, or one of them zero: infinite values go their own way in every step
+            bool look = edge, odd = false;
+            if constexpr (E == 8) look = look || __ballot(!all_finite_bf16<DT>(vr)) != 0;
+            if (look) {
+                const int have = s.m - (base + E * quarter);
+                bool fine = true;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    if (have < E) vr[d] = keep_first<IO>(vr[d], have);
+                    if (!all_finite<IO>(vr[d])) {
+                        fine = false;
+                        vr[d] = finite_only<IO>(vr[d]);
+                    }
+                }
+                odd = __ballot(!fine) != 0;
+            }
             const uint4 pg = IO::pack(p);
 #pragma unroll
             for (int d = 0; d < DT; ++d) IO::mma16(o[d], vr[d], pg);
