@@ -778,7 +778,8 @@ class KvPages:
     def attend(self, layer, q, start, seqs=None, max_new=None, max_len=None, scale=None, window=0, out=None, lse=None, want_lse=False, ws=None,
                stream=None):
         """Attention of the new tokens (append has written their keys and values) over their sequences' pages (spectre_kv_attend).
-        max_new, max_len: bounds of the sequences' new tokens and lengths (None: T, and the table's width); scale None: d^-1/2; window > 0: each
+        max_new, max_len: bounds of the sequences' new tokens and lengths (None: T, and the table's width), which the launch, its workspace and with them its time are
+        sized by: give them wherever the program knows them (a batch of single tokens without max_new=1 runs as one of chunks of T); scale None: d^-1/2; window > 0: each
         query sees that many keys, its own the last.  Returns out [T,H,d], with want_lse or a tensor `lse` also lse float32 [T,H]."""
         T, H, d = q.shape
         B = start.numel() - 1

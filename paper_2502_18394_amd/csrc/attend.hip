@@ -289,9 +289,11 @@ __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 
 // What bounds it at d = 64: per 64 keys and 32 rows a wave issues 16 products (32 clocks each on the matrix cores) and about 130 vector instructions
 // that cannot be saved (32 each of scale-and-shift, 2^x, sum; 16 each of maximum and packing), 2^x taking two slots.  Measured on their own in that proportion with their
 // LDS reads, products and vector work overlap only in part: 26.5 ns a product, against 17.5 for products alone and 15.7 for the rest alone.  The kernel takes 35.
-// An 8192-token prompt, 32 heads: 308 us, 893 TFLOP/s (all-zero inputs, which draw less power, take 13 % less); 2048 tokens over 28672 544 us, 916 TFLOP/s.
-// At d = 128 there are twice the products for the same vector work, two waves a SIMD: the same prompt with 16 heads 279 us, 986 TFLOP/s, the same chunk 494 us,
-// 1009 TFLOP/s.  A large matrix product of the library reaches 1326.
+// Counters of that kernel: matrix cores busy in 41 % of the cycles, the vector unit in 65 %, no LDS conflict.
+// An 8192-token prompt, 32 heads: 302 to 341 us by the machine, 806 to 911 TFLOP/s (all-zero inputs, which draw less power, take 13 % less); 2048 tokens over 28672 534 to
+// 595 us, 837 to 933 TFLOP/s.
+// At d = 128 there are twice the products for the same vector work, two waves a SIMD: the same prompt with 16 heads 267 to 287 us, 958 to 1031 TFLOP/s, the same chunk 484 to 510,
+// 978 to 1031 TFLOP/s.  A large matrix product of the library reaches 1326.
 // Where a page holds a whole tile its address is scalar work and the lanes' offsets stay the same from tile to tile; pages of less than a tile give every lane its
 // own address (which took 614 us where this took 540: 2048 over 28672, d = 128, pages of 64).
 // Measured and not taken: two sets of 32 rows a wave (half the LDS reads, two waves a SIMD: 4 % slower), scores of the next tile formed between the steps of this tile's
@@ -988,7 +990,7 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
         // twice the parts even them out (fp32 batch of up to 397 new tokens 135 instead of 142 us; single tiles, bound by memory, lose: 25.0 -> 28.8).
         const long long all = groups(p.tile_waves), keys = all > 4 * slots ? 2 * kRaggedKeys : kRaggedKeys;
         long long s = std::max(1ll, (even || rows <= 128 ? 1 : 2) * slots / all);
-        // fp32: four times, of 768 keys or more (24 sequences of up to 300 new and 4300 tokens, 32 heads, d = 64: 428 us, with 1024 keys or more 459, with
+        // fp32: four times, as long as parts have 768 keys or more (24 sequences of up to 300 new and 4300 tokens, 32 heads, d = 64: 428 us, with 1024 keys or more 459, with
         // 256 rows and twice the parts 535; 12 of up to 1500 new: 150, with parts down to 500 keys 160; bf16 with four times 133 instead of 111).
         if (slow) s = std::max(s, std::min(4 * slots / all, len / 768));
         if (!even) s = std::max(s, (len + keys - 1) / keys);
