@@ -516,6 +516,7 @@ int spectre_heads_backward(const spectre_heads *P /*host*/, const void *dq, long
  * position lens - n + i.  Queries go to q_out [T, H, d], keys, with norm and rotation, and values into the pages of `layer`.  A sequence of
  * fewer than n tokens, or a row outside the table, is left out.  No sequence twice.  While one of the bits that a failed reserve sets (NO_PAGES, TOO_LONG,
  * BAD_ARGUMENT) stands in the status, whichever call set it, every sequence is left out: without the reserve the places of the new tokens are those of the last ones.
+ * Rows of q_out that belong to a sequence that is left out stay as they are.
  * Nothing is written into a page that several sequences use: SPECTRE_KV_SHARED is set instead. */
 int spectre_kv_append(const spectre_kv *kv /*host*/, int layer, const spectre_heads *P /*host*/, const void *q, long long q_stride, const void *k,
                       long long k_stride, const void *v, long long v_stride, const int *start, const int *seqs, int B, int T, int H,

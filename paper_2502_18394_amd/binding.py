@@ -755,7 +755,8 @@ class KvPages:
     def append(self, layer, q, k, v, start, seqs=None, rope=None, wq=None, wk=None, eps=1e-6, q_out=None, stream=None):
         """Norm and rotation of the new tokens' heads; keys and values go into the pages of `layer`, queries are returned.  q [T,H,d], k, v [T,Hkv,d] of the
         pool's dtype; start int32 [B+1]: first token of each sequence; seqs int32 [B]: their rows of the table (None: 0 .. B-1).  The new tokens are
-        the last ones of their sequences: reserve() comes first, once for all layers."""
+        the last ones of their sequences: reserve() comes first, once for all layers.  While NO_PAGES, TOO_LONG or BAD_ARGUMENT stands in status[0] nothing is
+        written, nor is anything into a page that several sequences use (SHARED)."""
         T, H, d = q.shape
         B = start.numel() - 1
         qa, qs = _rows(q, "q", self.dtype)

@@ -65,3 +65,25 @@ def test_page_calls_in_a_graph_keep_their_workspace():
         two.reserve(seqs, add)
         torch.cuda.synchronize()
         assert torch.equal(one.book, two.book) and all(bool((x == 77).all()) for x in taken)
+
+
+def test_a_capture_on_a_stream_that_is_given():
+    """The calls' own `stream` is the one being captured."""
+    H, d, lens = 4, 64, [9000]
+    pool, _ = make("bf16", d, 1, 64, lens, 1)
+    q, start = queries([1], H, d, "bf16", 2)
+    chunk, wide = queries([500], H, d, "bf16", 3)
+    want = pool.attend(0, q, start, max_new=1, max_len=9000)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        out = pool.attend(0, q, start, max_new=1, max_len=9000, stream=side)
+    first = pool.attend(0, chunk, wide, max_new=500, max_len=9000)
+    small = pool.attend_workspace_bytes(1, 1, H, 1, 9000)
+    taken = [torch.full((small + 256,), 77, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(pool.attend(0, chunk, wide, max_new=500, max_len=9000), first)
+    assert all(bool((x == 77).all()) for x in taken)
