@@ -493,15 +493,20 @@ int spectre_kv_copy(const spectre_kv *kv /*host*/, const int *src, const int *ds
  * Norm and rotation of query and key heads.  Per row x: y = w * x / sqrt(mean x^2 + eps), then each pair of the first `rot` channels is turned by
  * the angle position * inv_freq[i], formed in fp64: (a, b) -> (a cos - b sin, b cos + a sin); pair i is channels (i, i + rot/2), or (2i, 2i + 1)
  * when interleaved.  wq, wk device fp32 [d], both NULL: no norm.  rot = 0: no rotation; else a multiple of 16 up to d, inv_freq device fp64 [rot / 2].
+ * axes > 1 (time, height, width of images and video): a token has that many positions, and pair i goes by the one of axis[i], device int32 [rot / 2] (an
+ * entry outside 0 .. axes - 1 counts as the last axis).  Positions are then int32 [axes, T] and have to be given; axes 0 and 1: one position a token.
  */
+enum { SPECTRE_HEADS_MAX_AXES = 8 };
 typedef struct {
     int d, rot, interleaved;
     float eps;
     const double *inv_freq;
     const float *wq, *wk;
+    int axes;
+    const int *axis;
 } spectre_heads;
 
-/* q [T, H, d], k [T, Hkv, d] -> q_out, k_out of the same shapes, dense.  positions: device int32 [T], NULL: 0 .. T - 1. */
+/* q [T, H, d], k [T, Hkv, d] -> q_out, k_out of the same shapes, dense.  positions: device int32 [T] (several axes: [axes, T]), NULL: 0 .. T - 1. */
 int spectre_heads_forward(const spectre_heads *P /*host*/, const void *q, long long q_stride, const void *k, long long k_stride, const int *positions,
                           int T, int H, int Hkv, spectre_dtype io, void *q_out, void *k_out, void *stream);
 
@@ -517,7 +522,12 @@ int spectre_heads_backward(const spectre_heads *P /*host*/, const void *dq, long
  * fewer than n tokens, or a row outside the table, is left out.  No sequence twice.  While one of the bits that a failed reserve sets (NO_PAGES, TOO_LONG,
  * BAD_ARGUMENT) stands in the status, whichever call set it, every sequence is left out: without the reserve the places of the new tokens are those of the last ones.
  * Rows of q_out that belong to a sequence that is left out stay as they are.
- * Nothing is written into a page that several sequences use: SPECTRE_KV_SHARED is set instead. */
+ * Nothing is written into a page that several sequences use: SPECTRE_KV_SHARED is set instead.
+ * spectre_kv_append_at: the same with the positions that the rotation goes by given, device int32 [axes, T] (one axis: [T]; NULL: the places in the
+ * sequences).  They have no part in where keys are stored or what a query sees: that goes by the order of the tokens. */
+int spectre_kv_append_at(const spectre_kv *kv /*host*/, int layer, const spectre_heads *P /*host*/, const void *q, long long q_stride, const void *k,
+                         long long k_stride, const void *v, long long v_stride, const int *positions, const int *start, const int *seqs, int B, int T,
+                         int H, void *q_out, void *stream);
 int spectre_kv_append(const spectre_kv *kv /*host*/, int layer, const spectre_heads *P /*host*/, const void *q, long long q_stride, const void *k,
                       long long k_stride, const void *v, long long v_stride, const int *start, const int *seqs, int B, int T, int H,
                       void *q_out, void *stream);

@@ -58,7 +58,7 @@ class KvC(ctypes.Structure):
 
 class HeadsC(ctypes.Structure):
     _fields_ = [("d", ctypes.c_int), ("rot", ctypes.c_int), ("interleaved", ctypes.c_int), ("eps", ctypes.c_float),
-                ("inv_freq", ctypes.c_void_p), ("wq", ctypes.c_void_p), ("wk", ctypes.c_void_p)]
+                ("inv_freq", ctypes.c_void_p), ("wq", ctypes.c_void_p), ("wk", ctypes.c_void_p), ("axes", ctypes.c_int), ("axis", ctypes.c_void_p)]
 
 
 def lib():
@@ -102,6 +102,7 @@ def lib():
                 "spectre_heads_backward_workspace_bytes": (i, i),
                 "spectre_heads_backward": (p, p, ll, p, ll, p, ll, p, ll, p, i, i, i, i, p, p, p, p, p, n, p),
                 "spectre_kv_append": (p, i, p, p, ll, p, ll, p, ll, p, p, i, i, i, p, p),
+                "spectre_kv_append_at": (p, i, p, p, ll, p, ll, p, ll, p, p, p, i, i, i, p, p),
                 "spectre_kv_attend_workspace_bytes": (p, i, i, i, i, i, i),
                 "spectre_kv_attend": (p, i, p, ll, p, p, i, i, i, i, i, ctypes.c_float, i, p, p, p, n, p)}.items():
             getattr(L, name).argtypes = types
@@ -565,17 +566,29 @@ def _kv_prepare():
 
 class Rope:
     """Angles by which a head's channels are turned: position * inv_freq[i] for pair i.  inv_freq: float64 [rot / 2] (any rule a model has for
-    it), or use Rope.of for theta^(-2 i / rot)."""
+    it), or use Rope.of for theta^(-2 i / rot).  axes: for tokens with several positions (time, height, width), the axis of each pair, integers
+    [rot / 2] from 0 on; positions are then int32 [number of axes, T]."""
 
-    def __init__(self, inv_freq, interleaved=False, device="cuda"):
+    MAX_AXES = 8
+
+    def __init__(self, inv_freq, interleaved=False, device="cuda", axes=None):
         self.inv_freq = torch.as_tensor(inv_freq, dtype=torch.float64).to(device).contiguous()
         if self.inv_freq.dim() != 1:
             raise ValueError("inv_freq must be one-dimensional")
-        self.rot, self.interleaved = 2 * self.inv_freq.numel(), bool(interleaved)
+        self.rot, self.interleaved, self.axes, self.axis = 2 * self.inv_freq.numel(), bool(interleaved), 1, None
+        if axes is not None:
+            axis = torch.as_tensor(axes)
+            if axis.is_floating_point() or axis.is_complex() or axis.dtype == torch.bool or tuple(axis.shape) != tuple(self.inv_freq.shape):
+                raise ValueError("axes must be an integer for each of inv_freq")
+            if axis.numel():
+                if int(axis.min()) < 0 or int(axis.max()) >= self.MAX_AXES:
+                    raise ValueError(f"axes must be between 0 and {self.MAX_AXES - 1}")
+                self.axes = int(axis.max()) + 1
+                self.axis = axis.to(device=device, dtype=torch.int32).contiguous()
 
     @classmethod
-    def of(cls, rot, theta=10000.0, interleaved=False, device="cuda"):
-        return cls(theta ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot), interleaved, device)
+    def of(cls, rot, theta=10000.0, interleaved=False, device="cuda", axes=None):
+        return cls(theta ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot), interleaved, device, axes)
 
 
 def _heads(d, rope, wq, wk, eps):
@@ -584,12 +597,29 @@ def _heads(d, rope, wq, wk, eps):
         if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,)):
             raise ValueError(f"{name} must be float32 [{d}]")
     return HeadsC(d, rope.rot if rope else 0, int(rope.interleaved) if rope else 0, eps, rope.inv_freq.data_ptr() if rope else None,
-                  None if wq is None else _ptr(wq, "wq"), None if wk is None else _ptr(wk, "wk"))
+                  None if wq is None else _ptr(wq, "wq"), None if wk is None else _ptr(wk, "wk"), rope.axes if rope else 1,
+                  rope.axis.data_ptr() if rope and rope.axis is not None else None)
+
+
+def _positions(positions, rope, T):
+    """Address of the tokens' positions: int32 [T], or [axes, T]."""
+    axes = rope.axes if rope else 1
+    if positions is None:
+        if axes > 1:
+            raise ValueError(f"positions [{axes}, {T}] have to be given for a rotation by several axes")
+        return None
+    if positions.dim() == 1 and axes == 1:
+        return _ints(positions, "positions", T)
+    if positions.dtype != torch.int32:
+        raise TypeError("positions must be int32")
+    if tuple(positions.shape) != (axes, T):
+        raise ValueError(f"positions must have shape [{axes}, {T}]")
+    return _ptr(positions, "positions")
 
 
 def qk_norm_rotate(q, k, positions=None, rope=None, wq=None, wk=None, eps=1e-6, q_out=None, k_out=None, stream=None):
     """Norm of each query and key head and rotation by position in one pass (spectre_heads_forward).  q [T,H,d], k [T,Hkv,d] f32/bf16, tokens any
-    16-byte multiple apart; positions int32 [T] (None: 0 .. T-1); wq, wk float32 [d], both None: no norm.  Returns (q_out, k_out)."""
+    16-byte multiple apart; positions int32 [T] (None: 0 .. T-1), [axes, T] for a rope of several axes; wq, wk float32 [d], both None: no norm.  Returns (q_out, k_out)."""
     T, H, d = q.shape
     Hkv = k.shape[1]
     io = _dtype_code(q)
@@ -604,7 +634,7 @@ def qk_norm_rotate(q, k, positions=None, rope=None, wq=None, wk=None, eps=1e-6, 
         k_out = _like(k, stream)
     _same(q_out, q, "q_out")
     _same(k_out, k, "k_out")
-    _check(lib().spectre_heads_forward(ctypes.byref(P), qa, qs, ka, ks, None if positions is None else _ints(positions, "positions", T), T, H, Hkv, io,
+    _check(lib().spectre_heads_forward(ctypes.byref(P), qa, qs, ka, ks, _positions(positions, rope, T), T, H, Hkv, io,
                                        _ptr(q_out, "q_out"), _ptr(k_out, "k_out"), _now(stream)))
     return q_out, k_out
 
@@ -632,7 +662,7 @@ def qk_norm_rotate_backward(dq, dk, q, k, positions=None, rope=None, wq=None, wk
             ws = _new((lib().spectre_heads_backward_workspace_bytes(T, d) + 256,), torch.uint8, q.device, stream)
         wsp, wsn = _given(ws)
     _check(lib().spectre_heads_backward(ctypes.byref(P), *rows[0], *rows[1], *rows[2], *rows[3],
-                                        None if positions is None else _ints(positions, "positions", T), T, H, Hkv, io, gq.data_ptr(), gk.data_ptr(),
+                                        _positions(positions, rope, T), T, H, Hkv, io, gq.data_ptr(), gk.data_ptr(),
                                         None if gw[0] is None else gw[0].data_ptr(), None if gw[1] is None else gw[1].data_ptr(), wsp, wsn,
                                         _now(stream)))
     return gq, gk, gw[0], gw[1]
@@ -752,11 +782,12 @@ class KvPages:
         n = src.numel()
         _check(lib().spectre_kv_copy(self._ref, _ints(src, "src"), _ints(dst, "dst", n), n, _now(stream)))
 
-    def append(self, layer, q, k, v, start, seqs=None, rope=None, wq=None, wk=None, eps=1e-6, q_out=None, stream=None):
+    def append(self, layer, q, k, v, start, seqs=None, rope=None, wq=None, wk=None, eps=1e-6, q_out=None, stream=None, positions=None):
         """Norm and rotation of the new tokens' heads; keys and values go into the pages of `layer`, queries are returned.  q [T,H,d], k, v [T,Hkv,d] of the
         pool's dtype; start int32 [B+1]: first token of each sequence; seqs int32 [B]: their rows of the table (None: 0 .. B-1).  The new tokens are
         the last ones of their sequences: reserve() comes first, once for all layers.  While NO_PAGES, TOO_LONG or BAD_ARGUMENT stands in status[0] nothing is
-        written, nor is anything into a page that several sequences use (SHARED)."""
+        written, nor is anything into a page that several sequences use (SHARED).  positions: what the rotation goes by, int32 [T] or [axes, T] (None: the
+        places in the sequences, of a rope of one axis); where keys are stored and what a query sees goes by the order of the tokens."""
         T, H, d = q.shape
         B = start.numel() - 1
         qa, qs = _rows(q, "q", self.dtype)
@@ -769,8 +800,8 @@ class KvPages:
             q_out = _like(q, stream)
         else:
             _same(q_out, q, "q_out")
-        _check(lib().spectre_kv_append(self._ref, layer, ctypes.byref(P), qa, qs, ka, ks, va, vs, _ints(start, "start"),
-                                       None if seqs is None else _ints(seqs, "seqs", B), B, T, H, _ptr(q_out, "q_out"), _now(stream)))
+        _check(lib().spectre_kv_append_at(self._ref, layer, ctypes.byref(P), qa, qs, ka, ks, va, vs, _positions(positions, rope, T), _ints(start, "start"),
+                                          None if seqs is None else _ints(seqs, "seqs", B), B, T, H, _ptr(q_out, "q_out"), _now(stream)))
         return q_out
 
     def attend_workspace_bytes(self, B, T, H, max_new, max_len=None, window=0):

@@ -45,7 +45,8 @@ struct HeadRows {                    // token t, head h, channel c at base + (t 
     int T, H, Hkv;
 };
 hipError_t launch_heads_forward(const spectre_heads &P, int io, const HeadRows &x, const int *positions, void *q_out, void *k_out, hipStream_t st);
-hipError_t launch_heads_append(const spectre_heads &P, int io, const HeadRows &x, const KvView &kv, const int *start, const int *seqs, int B, void *q_out, hipStream_t st);
+hipError_t launch_heads_append(const spectre_heads &P, int io, const HeadRows &x, const KvView &kv, const int *positions, const int *start, const int *seqs, int B, void *q_out,
+                               hipStream_t st);
 int heads_backward_blocks(int T);
 hipError_t launch_heads_backward(const spectre_heads &P, int io, const HeadRows &x, const HeadRows &dy, const int *positions, void *gq, void *gk, float *gwq, float *gwk,
                                  double *partial, hipStream_t st);

@@ -67,7 +67,7 @@ bool overlap(const Span &in, const void *out, int out_heads, int T, int d, spect
     return a < b_end && b < a_end;
 }
 
-int check_heads(const spectre_heads *P, int T, int H, int Hkv, spectre_dtype io, const char *who) {
+int check_heads(const spectre_heads *P, const int *positions, int T, int H, int Hkv, spectre_dtype io, const char *who) {
     if (!P) return fail(SPECTRE_EINVAL, "%s: null parameters", who);
     int rc = check_dtype(io, who);
     if (rc) return rc;
@@ -79,6 +79,11 @@ int check_heads(const spectre_heads *P, int T, int H, int Hkv, spectre_dtype io,
     if (!P->wq != !P->wk) return fail(SPECTRE_EINVAL, "%s: one of wq and wk is null", who);
     if (P->wq && !(P->eps >= 0.f && std::isfinite(P->eps))) return fail(SPECTRE_EINVAL, "%s: eps", who);
     if (P->interleaved != 0 && P->interleaved != 1) return fail(SPECTRE_EINVAL, "%s: interleaved is neither 0 nor 1", who);
+    if (P->axes < 0) return fail(SPECTRE_EINVAL, "%s: axes below 0", who);
+    if (P->axes > SPECTRE_HEADS_MAX_AXES) return fail(SPECTRE_EUNSUPPORTED, "%s: %d axes (up to %d are supported)", who, P->axes, SPECTRE_HEADS_MAX_AXES);
+    if (P->axes > 1 && P->rot && !P->axis) return fail(SPECTRE_EINVAL, "%s: null axis", who);
+    if (P->axes > 1 && P->rot && !positions && T > 0) return fail(SPECTRE_EINVAL, "%s: null positions, which several axes need", who);
+    if (!aligned(positions, 4) || !aligned(P->axis, 4)) return fail(SPECTRE_EINVAL, "%s: positions or axis not aligned", who);
     return SPECTRE_OK;
 }
 
@@ -197,7 +202,7 @@ int spectre_kv_copy(const spectre_kv *kv, const int *src, const int *dst, int n,
 int spectre_heads_forward(const spectre_heads *P, const void *q, long long q_stride, const void *k, long long k_stride, const int *positions, int T, int H, int Hkv,
                           spectre_dtype io, void *q_out, void *k_out, void *stream) {
     const char *who = "heads_forward";
-    int rc = check_heads(P, T, H, Hkv, io, who);
+    int rc = check_heads(P, positions, T, H, Hkv, io, who);
     if (rc || T == 0) return rc;
     const Span in[2] = {{q, q_stride, H, "q"}, {k, k_stride, Hkv, "k"}};
     for (const Span &x : in)
@@ -222,7 +227,7 @@ int spectre_heads_backward(const spectre_heads *P, const void *dq, long long dq_
                            long long k_stride, const int *positions, int T, int H, int Hkv, spectre_dtype io, void *gq, void *gk, float *gwq, float *gwk, void *ws,
                            size_t ws_bytes, void *stream) {
     const char *who = "heads_backward";
-    int rc = check_heads(P, T, H, Hkv, io, who);
+    int rc = check_heads(P, positions, T, H, Hkv, io, who);
     if (rc) return rc;
     if (P->wq && (!gwq || !gwk)) return fail(SPECTRE_EINVAL, "%s: null gwq or gwk", who);
     if (T == 0) return P->wq ? done(launch_heads_backward(*P, (int)io, HeadRows{}, HeadRows{}, nullptr, nullptr, nullptr, gwq, gwk, nullptr, static_cast<hipStream_t>(stream)), who) : SPECTRE_OK;
@@ -246,11 +251,16 @@ int spectre_heads_backward(const spectre_heads *P, const void *dq, long long dq_
 
 int spectre_kv_append(const spectre_kv *kv, int layer, const spectre_heads *P, const void *q, long long q_stride, const void *k, long long k_stride, const void *v,
                       long long v_stride, const int *start, const int *seqs, int B, int T, int H, void *q_out, void *stream) {
+    return spectre_kv_append_at(kv, layer, P, q, q_stride, k, k_stride, v, v_stride, nullptr, start, seqs, B, T, H, q_out, stream);
+}
+
+int spectre_kv_append_at(const spectre_kv *kv, int layer, const spectre_heads *P, const void *q, long long q_stride, const void *k, long long k_stride, const void *v,
+                         long long v_stride, const int *positions, const int *start, const int *seqs, int B, int T, int H, void *q_out, void *stream) {
     const char *who = "kv_append";
     int rc = check_pool(kv, who);
     if (rc) return rc;
     if ((rc = check_layer(kv, layer, who))) return rc;
-    if ((rc = check_heads(P, T, H, kv->Hkv, kv->dtype, who))) return rc;
+    if ((rc = check_heads(P, positions, T, H, kv->Hkv, kv->dtype, who))) return rc;
     if (P->d != kv->d) return fail(SPECTRE_EINVAL, "%s: d = %d, the pool has %d", who, P->d, kv->d);
     if ((rc = check_batch(kv, start, B, T, H, who))) return rc;
     if (T == 0) return SPECTRE_OK;
@@ -261,7 +271,7 @@ int spectre_kv_append(const spectre_kv *kv, int layer, const spectre_heads *P, c
     for (const Span &x : in)
         if (overlap(x, q_out, H, T, kv->d, kv->dtype)) return fail(SPECTRE_EINVAL, "%s: q_out overlaps %s", who, x.name);
     const HeadRows x = {q, k, v, q_stride, k_stride, v_stride, T, H, kv->Hkv};
-    return done(launch_heads_append(*P, (int)kv->dtype, x, kv_view(kv, layer), start, seqs, B, q_out, static_cast<hipStream_t>(stream)), who);
+    return done(launch_heads_append(*P, (int)kv->dtype, x, kv_view(kv, layer), positions, start, seqs, B, q_out, static_cast<hipStream_t>(stream)), who);
 }
 
 size_t spectre_kv_attend_workspace_bytes(const spectre_kv *kv, int B, int T, int H, int max_new, int max_len, int window) {
