@@ -69,7 +69,8 @@ typedef enum {
     SPECTRE_ENOTREADY = 5     /* spectre_prepare has not been called for this length and device */
 } spectre_status;
 
-typedef enum { SPECTRE_F32 = 0, SPECTRE_BF16 = 1 } spectre_dtype;
+/* SPECTRE_E4M3 (8 bits: sign, four of exponent, three of mantissa; up to 448, no infinities) is a type of pages and of coded rows only. */
+typedef enum { SPECTRE_F32 = 0, SPECTRE_BF16 = 1, SPECTRE_E4M3 = 4 } spectre_dtype;
 
 /* Host string describing the last failure on the calling thread ("" if none). */
 const char *spectre_last_error(void);
@@ -442,6 +443,14 @@ int spectre_prefix_step(spectre_prefix_cache *cache /*host*/, const void *v_t, c
  * Sequence s of lens[s] tokens has them in the first ceil(lens[s] / page) pages of its row.  All of it is device state, so reserving pages
  * and decoding can be captured into a graph together.  A page number outside 0 .. pages - 1 is never followed: nothing is written
  * there, and attention treats its tokens as absent.  A pool is worked on by one stream at a time.
+ *
+ * Pages of 8 bits (dtype SPECTRE_E4M3; rows are bf16 then, wherever a call on the pool takes rows of its dtype): E = 16, and every
+ * SPECTRE_KV_BLOCK tokens of a page have a scale for each key/value head, of keys and of values:
+ *   scales  fp32 [layers, pages, Hkv, page / SPECTRE_KV_BLOCK, 2], powers of two from 2^-100 to 2^120; what is stored is code * scale
+ * spectre_kv_append takes the smallest power of two with which the largest finite magnitude of a block is no more than 448 (values of less than 2^-110 may
+ * become zero; magnitudes are cut at 1.875 * 2^127, non-finite values become NaN).  Tokens that join others in a block keep the larger of its scale and
+ * their own; where that grows, the others' codes are rounded to it, which leaves them as they are but for codes below the smallest normal one.
+ * fork, compact and copy move scales with their pages.  Contents that a caller writes itself have to be finite as bf16 numbers, or NaN codes.
  */
 typedef struct {
     int layers, pages;         /* pages: of each layer                                       */
@@ -451,16 +460,18 @@ typedef struct {
     spectre_dtype dtype;
     void *k, *v;               /* device, 16-byte aligned                                    */
     int *book;                 /* device                                                     */
+    float *scales;             /* device, 8-byte aligned; of pages of 8 bits only            */
 } spectre_kv;
 
 enum { SPECTRE_KV_MAX_SEQS = 65536, SPECTRE_KV_MAX_TABLE = 1 << 20 };      /* limits of seqs and max_pages */
-enum { SPECTRE_KV_K = 0, SPECTRE_KV_V = 1, SPECTRE_KV_BOOK = 2 };
+enum { SPECTRE_KV_K = 0, SPECTRE_KV_V = 1, SPECTRE_KV_BOOK = 2, SPECTRE_KV_SCALES = 3 };
+enum { SPECTRE_KV_BLOCK = 16 };                                             /* tokens of a page of 8 bits that share a scale */
 
 /* Words of the status (book[0 .. 7]): [0] bits of what calls found wrong, kept until the caller clears them; [1] pages that the last
  * spectre_kv_fork or _compact copied; [2] pages in use after the last _compact. */
 enum { SPECTRE_KV_NO_PAGES = 1, SPECTRE_KV_TOO_LONG = 2, SPECTRE_KV_BAD_ARGUMENT = 4, SPECTRE_KV_NOT_EMPTY = 8, SPECTRE_KV_SHARED = 16 };
 
-/* Bytes of the pool's arrays (which: SPECTRE_KV_K, _V, _BOOK); 0 for a pool that is not supported.  Only sizes and dtype are read. */
+/* Bytes of the pool's arrays (which: SPECTRE_KV_K, _V, _BOOK, with pages of 8 bits _SCALES); 0 for a pool that is not supported.  Only sizes and dtype are read. */
 size_t spectre_kv_bytes(const spectre_kv *kv /*host*/, int which);
 
 /* Set-up, once per device before any call below is captured into a graph: loads their kernels. */

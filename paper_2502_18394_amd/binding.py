@@ -13,7 +13,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libspectre_hip.so")
 
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 4
 READ_NEWEST, READ_WINDOW = 0, 1
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP, ENOTREADY = 0, 1, 2, 3, 4, 5
 OPT_LANES, OPT_SCRATCH_MB, OPT_FUSED_4096, OPT_SLAB_COMPILE_TIME, OPT_HEAD_AFFINE, OPT_GROUPS, OPT_LANE_SHUFFLES = 0, 1, 2, 3, 4, 5, 6
@@ -53,7 +53,7 @@ class PrefixCacheC(ctypes.Structure):
 class KvC(ctypes.Structure):
     _fields_ = [("layers", ctypes.c_int), ("pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("d", ctypes.c_int), ("page", ctypes.c_int),
                 ("seqs", ctypes.c_int), ("max_pages", ctypes.c_int), ("dtype", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
-                ("book", ctypes.c_void_p)]
+                ("book", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
 
 
 class HeadsC(ctypes.Structure):
@@ -672,25 +672,34 @@ class KvPages:
     """Keys and values of attention layers in pages, with their bookkeeping on the device (spectre_kv; layout and rules in spectre.h).
 
     KvPages.empty(...) allocates an empty pool; the constructor takes tensors that exist:
-    k_pages [layers, pages, Hkv, d/E, page, E], v_pages [layers, pages, Hkv, page/E, d, E] (E = 8 bf16 or 4 f32 elements),
-    book int32 [8 + seqs + pages + seqs * max_pages]."""
+    k_pages [layers, pages, Hkv, d/E, page, E], v_pages [layers, pages, Hkv, page/E, d, E] (E = 8 bf16, 4 f32 or 16 float8_e4m3fn elements),
+    book int32 [8 + seqs + pages + seqs * max_pages]; with pages of float8_e4m3fn, whose rows are bf16, also scales float32
+    [layers, pages, Hkv, page/16, 2], powers of two: of the keys and of the values of each 16 tokens of a head (what is stored is code * scale)."""
 
     NO_PAGES, TOO_LONG, BAD_ARGUMENT, NOT_EMPTY, SHARED = 1, 2, 4, 8, 16          # bits of the status
 
-    def __init__(self, k_pages, v_pages, book, seqs, max_pages):
-        io = _dtype_code(k_pages)
-        E = 8 if io == BF16 else 4
+    BLOCK = 16                          # tokens of a page of 8 bits that share a scale
+
+    def __init__(self, k_pages, v_pages, book, seqs, max_pages, scales=None):
+        io = E4M3 if k_pages.dtype == torch.float8_e4m3fn else _dtype_code(k_pages)
+        E = 16 // k_pages.element_size()
         if k_pages.dim() != 6 or k_pages.shape[5] != E:
             raise ValueError(f"k_pages must be [layers, pages, Hkv, d/{E}, page, {E}]")
         layers, pages, Hkv, groups, page, _ = k_pages.shape
         d = groups * E
         if tuple(v_pages.shape) != (layers, pages, Hkv, page // E, d, E) or v_pages.dtype != k_pages.dtype:
             raise ValueError(f"v_pages must be {k_pages.dtype} [layers, pages, Hkv, page/{E}, d, {E}]")
+        if (scales is not None) != (io == E4M3):
+            raise ValueError("pages of float8_e4m3fn have scales, others none")
+        if scales is not None and (scales.dtype != torch.float32 or tuple(scales.shape) != (layers, pages, Hkv, page // self.BLOCK, 2)):
+            raise ValueError(f"scales must be float32 [layers, pages, Hkv, page/{self.BLOCK}, 2]")
         if book.numel() != 8 + seqs + pages + seqs * max_pages:
             raise ValueError("book must have 8 + seqs + pages + seqs * max_pages entries")
         self.layers, self.pages, self.Hkv, self.d, self.page, self.seqs, self.max_pages = layers, pages, Hkv, d, page, seqs, max_pages
-        self.dtype, self.k_pages, self.v_pages, self.book = k_pages.dtype, k_pages, v_pages, book
-        self.c = KvC(layers, pages, Hkv, d, page, seqs, max_pages, io, _ptr(k_pages, "k_pages"), _ptr(v_pages, "v_pages"), _ints(book, "book"))
+        self.dtype, self.k_pages, self.v_pages, self.book, self.scales = k_pages.dtype, k_pages, v_pages, book, scales
+        self.rows = torch.bfloat16 if io == E4M3 else self.dtype               # type of the rows that calls take
+        self.c = KvC(layers, pages, Hkv, d, page, seqs, max_pages, io, _ptr(k_pages, "k_pages"), _ptr(v_pages, "v_pages"), _ints(book, "book"),
+                     None if scales is None else _ptr(scales, "scales"))
         self._ref = ctypes.byref(self.c)
         if lib().spectre_kv_bytes(self._ref, 0) == 0:
             raise SpectreError(EUNSUPPORTED, lib().spectre_last_error().decode())
@@ -699,15 +708,17 @@ class KvPages:
 
     @classmethod
     def empty(cls, layers, pages, Hkv, d, page, seqs, max_pages, dtype=torch.bfloat16, device="cuda"):
-        c = KvC(layers, pages, Hkv, d, page, seqs, max_pages, BF16 if dtype == torch.bfloat16 else F32, None, None, None)
+        codes = {torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+        c = KvC(layers, pages, Hkv, d, page, seqs, max_pages, codes.get(dtype, F32), None, None, None, None)
         n = lib().spectre_kv_bytes(ctypes.byref(c), 0)
         if n == 0:
             raise SpectreError(EUNSUPPORTED, lib().spectre_last_error().decode())
-        E = 8 if dtype == torch.bfloat16 else 4
+        E = 16 // dtype.itemsize
+        scales = torch.ones((layers, pages, Hkv, page // cls.BLOCK, 2), device=device) if dtype == torch.float8_e4m3fn else None
         k = torch.zeros((layers, pages, Hkv, d // E, page, E), dtype=dtype, device=device)
         v = torch.zeros((layers, pages, Hkv, page // E, d, E), dtype=dtype, device=device)
         book = torch.empty(8 + seqs + pages + seqs * max_pages, dtype=torch.int32, device=device)
-        pool = cls(k, v, book, seqs, max_pages)
+        pool = cls(k, v, book, seqs, max_pages, scales)
         pool.reset()
         return pool
 
@@ -784,15 +795,15 @@ class KvPages:
 
     def append(self, layer, q, k, v, start, seqs=None, rope=None, wq=None, wk=None, eps=1e-6, q_out=None, stream=None, positions=None):
         """Norm and rotation of the new tokens' heads; keys and values go into the pages of `layer`, queries are returned.  q [T,H,d], k, v [T,Hkv,d] of the
-        pool's dtype; start int32 [B+1]: first token of each sequence; seqs int32 [B]: their rows of the table (None: 0 .. B-1).  The new tokens are
+        pool's dtype (bf16 for pages of 8 bits); start int32 [B+1]: first token of each sequence; seqs int32 [B]: their rows of the table (None: 0 .. B-1).  The new tokens are
         the last ones of their sequences: reserve() comes first, once for all layers.  While NO_PAGES, TOO_LONG or BAD_ARGUMENT stands in status[0] nothing is
         written, nor is anything into a page that several sequences use (SHARED).  positions: what the rotation goes by, int32 [T] or [axes, T] (None: the
         places in the sequences, of a rope of one axis); where keys are stored and what a query sees goes by the order of the tokens."""
         T, H, d = q.shape
         B = start.numel() - 1
-        qa, qs = _rows(q, "q", self.dtype)
-        ka, ks = _rows(k, "k", self.dtype, T, self.Hkv)
-        va, vs = _rows(v, "v", self.dtype, T, self.Hkv)
+        qa, qs = _rows(q, "q", self.rows)
+        ka, ks = _rows(k, "k", self.rows, T, self.Hkv)
+        va, vs = _rows(v, "v", self.rows, T, self.Hkv)
         if d != self.d or k.shape[2] != d or v.shape[2] != d:
             raise ValueError(f"q, k and v must have d = {self.d}")
         P = _heads(d, rope, wq, wk, eps)
@@ -815,7 +826,7 @@ class KvPages:
         query sees that many keys, its own the last.  Returns out [T,H,d], with want_lse or a tensor `lse` also lse float32 [T,H]."""
         T, H, d = q.shape
         B = start.numel() - 1
-        qa, qs = _rows(q, "q", self.dtype)
+        qa, qs = _rows(q, "q", self.rows)
         if d != self.d:
             raise ValueError(f"q must have d = {self.d}")
         if max_new is None:

@@ -20,6 +20,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "e4m3.h"
 #include "paged.h"
 
 namespace spectre {
@@ -123,8 +124,10 @@ __device__ __forceinline__ void left_out(const AttendK &k, const Seq &s, int h, 
 // land on the same few compute units (24 ragged sequences, d = 128: 302 instead of 137 us).
 __device__ __forceinline__ int turned_pair(int block, int rest, int pairs) { return (int)((block - (long long)rest * pairs + 8ll * rest) % pairs); }
 
+// E, kBytes: of rows and of the matrix cores' operands.  PE: elements of a page's 16-byte groups.  kStepKeys: of a wave's step through few rows' keys.
 struct Bf16Mma {
-    static constexpr int E = 8, kBytes = 2;
+    static constexpr int E = 8, kBytes = 2, PE = 8, kPageBytes = 2;
+    static constexpr bool kCoded = false;
     static constexpr int kTileKeys = 64, kStepKeys = 32;
     typedef uint16_t elem_t;
     // 32 rows of A (keys, channels) x 32 columns: one group of 8 of the contraction a lane
@@ -163,7 +166,8 @@ struct Bf16Mma {
     __device__ static __forceinline__ uint32_t keep(uint32_t w, int i, int n) { return 2 * i + 1 < n ? w : 2 * i < n ? w & 0xffffu : 0u; }
 };
 struct F32Mma {
-    static constexpr int E = 4, kBytes = 4;
+    static constexpr int E = 4, kBytes = 4, PE = 4, kPageBytes = 4;
+    static constexpr bool kCoded = false;
     static constexpr int kTileKeys = 32, kStepKeys = 16;
     typedef uint32_t elem_t;
     __device__ static __forceinline__ void mma32(f32x16_t &acc, uint4 a, uint4 b) {
@@ -190,6 +194,27 @@ struct F32Mma {
     __device__ static __forceinline__ float value(elem_t e) { return __uint_as_float(e); }
     __device__ static __forceinline__ uint32_t keep(uint32_t w, int i, int n) { return i < n ? w : 0u; }
 };
+
+// Pages of 8 bits, rows of bf16: codes become bf16 numbers, exactly, on their way to the matrix cores, their block's scale with them.  A group is 16 channels of a
+// key, or 16 keys of a channel: two operands.
+struct E4m3Mma : Bf16Mma {
+    static constexpr int PE = 16, kPageBytes = 1, kStepKeys = 64;
+    static constexpr bool kCoded = true;
+    __device__ static __forceinline__ uint32_t keep8(uint32_t w, int i, int n) {
+        return n >= 4 * i + 4 ? w : n <= 4 * i ? 0u : w & ((1u << (8 * (n - 4 * i))) - 1u);
+    }
+    __device__ static __forceinline__ uint4 keep_codes(uint4 g, int n) { return make_uint4(keep8(g.x, 0, n), keep8(g.y, 1, n), keep8(g.z, 2, n), keep8(g.w, 3, n)); }
+    __device__ static __forceinline__ uint32_t nan_bits(uint4 g) { return e4m3_nan_bits(g.x) | e4m3_nan_bits(g.y) | e4m3_nan_bits(g.z) | e4m3_nan_bits(g.w); }
+    __device__ static __forceinline__ uint4 finite_codes(uint4 g) {
+        return make_uint4(e4m3_finite_only(g.x), e4m3_finite_only(g.y), e4m3_finite_only(g.z), e4m3_finite_only(g.w));
+    }
+};
+// Operand `half` of a group as it lies in a page.
+template <typename IO>
+__device__ __forceinline__ uint4 operand(uint4 g, int half, float scale) {
+    if constexpr (IO::kCoded) return half ? e4m3_decode8(g.z, g.w, scale) : e4m3_decode8(g.x, g.y, scale);
+    else return g;
+}
 
 template <typename IO>
 __device__ __forceinline__ uint4 keep_first(uint4 g, int n) {
@@ -237,10 +262,16 @@ __device__ __forceinline__ void add_not_finite(const KvView &kv, const Seq &s, i
     for (int key = base; key < base + count && key < s.m; ++key) {
         const int page = table[key >> kv.page_log], slot = key & ((1 << kv.page_log) - 1);
         if ((unsigned)page >= (unsigned)kv.P || key > pos || key <= from) continue;
-        const elem_t *v = reinterpret_cast<const elem_t *>(kv.v) + ((((long long)page * kv.Hkv + h) << kv.page_log) + slot / IO::E * IO::E) * D + slot % IO::E;
+        const long long head = (long long)page * kv.Hkv + h;
+        const elem_t *v = reinterpret_cast<const elem_t *>(kv.v) + ((head << kv.page_log) + slot / IO::E * IO::E) * D + slot % IO::E;
+        const uint8_t *codes = reinterpret_cast<const uint8_t *>(kv.v) + ((head << kv.page_log) + slot / IO::PE * IO::PE) * D + slot % IO::PE;
+        float scale = 0.f;
+        if constexpr (IO::kCoded) scale = kv.scales[2 * ((head << (kv.page_log - kKvBlockLog)) + (slot >> kKvBlockLog)) + 1];
 #pragma unroll
         for (int r = 0; r < N; ++r) {
-            const float x = IO::value(v[channel(r) * IO::E]);
+            float x;
+            if constexpr (IO::kCoded) x = e4m3_decode1(codes[channel(r) * IO::PE], scale);
+            else x = IO::value(v[channel(r) * IO::E]);
             if constexpr (N > 32) {
                 // one condition at a time: 64 pairs of scalar registers are taken from the loop around otherwise (its addresses then live in lanes of a
                 // vector register: 540 instead of 499 us for 2048 rows over 28672, d = 128; with 32 channels a lane the plain form is the faster one)
@@ -370,7 +401,7 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
     };
     const unsigned P = (unsigned)kv.P;
     // bytes of a page, and of this head and thread inside one: a 64-bit product a lane (keys) or a wave (values), 32-bit sums for the rest
-    const unsigned page_bytes = (unsigned)kv.Hkv * (D * IO::kBytes) << kv.page_log, head_bytes = (unsigned)h * (D * IO::kBytes) << kv.page_log;
+    const unsigned page_bytes = (unsigned)kv.Hkv * (D * IO::kPageBytes) << kv.page_log, head_bytes = (unsigned)h * (D * IO::kPageBytes) << kv.page_log;
     const unsigned k_at = (threadIdx.x / KT * 16u) << kv.page_log, k_lane = k_at + (lane & (KT - 1)) * 16u;
     const char *const k_head = reinterpret_cast<const char *>(kv.k) + head_bytes, *const v_head = reinterpret_cast<const char *>(kv.v) + head_bytes;
     // Groups of a tile straight from memory into LDS, in the order they have there: a wave's 64 lanes write 1 KB from its first group on.  Absent keys leave
@@ -422,8 +453,48 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
             if (p < P) to_lds<false>(vb + threadIdx.x % D * 16u, to + 64 * wave_now + THREADS * i);
         }
     };
+    // Pages of 8 bits go through registers: requested a tile ahead of being written to LDS as bf16 numbers, which is a tile ahead of their use.  A wave's 64 threads
+    // have the same 16 channels of a tile's keys, or groups of one (d = 128: of half a) block of its values.
+    constexpr int CODED = IO::kCoded ? 8 * D / THREADS : 1;                  // groups a thread, keys' first
+    uint4 code[CODED];
+    float code_scale[CODED];
+    auto request_codes = [&](int t, int page) {
+        if constexpr (IO::kCoded) {
+#pragma unroll
+            for (int i = 0; i < CODED; ++i) {
+                const int u = 64 * wave + THREADS * i;
+                code_scale[i] = -1.f;
+                const int kg = (u - 4 * D) / D;                              // block of values
+                const int p = u < 4 * D ? page : __builtin_amdgcn_readlane(page, 16 * (kg > 0 ? kg : 0));
+                if ((unsigned)p >= P) continue;
+                const int slot = (t * KT + (u < 4 * D ? lane : 16 * kg)) & mask;
+                const unsigned at = u < 4 * D ? (((u / KT) * 16u) << kv.page_log) + slot * 16u : (slot >> kKvBlockLog) * (D * 16u) + ((u - 4 * D) % D + lane) * 16u;
+                const char *from = (u < 4 * D ? k_head : v_head) + (unsigned long long)(unsigned)p * page_bytes + at;
+                code[i] = *reinterpret_cast<const uint4 *>(from);
+                code_scale[i] = kv.scales[2 * ((((long long)p * kv.Hkv + h) << (kv.page_log - kKvBlockLog)) + (slot >> kKvBlockLog)) + (u < 4 * D ? 0 : 1)];
+            }
+        }
+    };
+    auto write_codes = [&](uint4 *sk, uint4 *sv) {
+        if constexpr (IO::kCoded) {
+#pragma unroll
+            for (int i = 0; i < CODED; ++i) {
+                const int u = 64 * wave + THREADS * i;
+                if (code_scale[i] < 0.f) continue;                           // absent: what lies there stays
+                const uint4 lo = operand<IO>(code[i], 0, code_scale[i]), hi = operand<IO>(code[i], 1, code_scale[i]);
+                if (u < 4 * D) {
+                    sk[2 * (u / KT) * KT + lane] = lo;
+                    sk[(2 * (u / KT) + 1) * KT + lane] = hi;
+                } else {
+                    const int x = u - 4 * D, kg = x / D, c = x % D + lane;
+                    sv[2 * kg * D + c] = lo;
+                    sv[(2 * kg + 1) * D + c] = hi;
+                }
+            }
+        }
+    };
     auto arrived = [&]() {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                     // this wave's part has arrived ...
+        if constexpr (!IO::kCoded) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's part has arrived ...
         __syncthreads();                                                    // ... and everybody's, and nobody reads the other buffers any more
     };
     const int back = k.a.window ? k.a.window : 1 << 30;
@@ -501,16 +572,27 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
         }
     };
     if (threadIdx.x < 2) odd[threadIdx.x] = -1;
-    int page = page_of(t_lo), next = page_of(t_lo + 1);
+    int page = page_of(t_lo), next = page_of(t_lo + 1), later = IO::kCoded ? page_of(t_lo + 2) : -1;
     if (t_lo < t_hi) {
-        request_keys(t_lo, page, sk0);
-        request_values(t_lo, page, sv0);
+        if constexpr (IO::kCoded) {
+            request_codes(t_lo, page);
+            write_codes(sk0, sv0);
+            request_codes(t_lo + 1, next);
+        } else {
+            request_keys(t_lo, page, sk0);
+            request_values(t_lo, page, sv0);
+        }
     }
     auto tile_step = [&](int t, uint4 *sk, uint4 *sv, uint4 *next_k, uint4 *next_v, int *flag) {
         const unsigned long long there = __ballot((unsigned)page < P);      // bit = key of the tile (fp32: twice 32 keys)
         arrived();
         page = next;
-        if (t + 1 < t_hi) {
+        if constexpr (IO::kCoded) {
+            write_codes(next_k, next_v);
+            next = later;
+            request_codes(t + 2, next);
+            later = page_of(t + 3);
+        } else if (t + 1 < t_hi) {
             request_keys(t + 1, page, next_k);
             request_values(t + 1, page, next_v);
             next = page_of(t + 2);
@@ -591,7 +673,8 @@ struct FewLds {
 
 template <typename IO, int D, int WAVES>
 __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds) {
-    constexpr int E = IO::E, SK = IO::kStepKeys, KTILES = SK / 16, QG = D / (4 * E), DT = D / 16, THREADS = 64 * WAVES;
+    constexpr int E = IO::E, PE = IO::PE, SK = IO::kStepKeys, KTILES = SK / 16, DT = D / 16, THREADS = 64 * WAVES;
+    constexpr int GROUPS = D / (4 * PE), HALVES = PE == 16 ? 2 : 1, QG = GROUPS * HALVES;    // groups of a key a lane, operands of each
     int *const pages = lds.pages;
     const KvView &kv = k.kv;
     const int pairs = kv.Hkv * k.a.B, split = block / pairs, pair = turned_pair(block, split, pairs), h = pair % kv.Hkv;
@@ -608,7 +691,7 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
     {
         const char *base = reinterpret_cast<const char *>(k.a.q) + ((s.from + token) * k.a.q_stride + head * D) * IO::kBytes;
 #pragma unroll
-        for (int j = 0; j < QG; ++j) q[j] = reinterpret_cast<const uint4 *>(base)[4 * j + quarter];
+        for (int j = 0; j < QG; ++j) q[j] = reinterpret_cast<const uint4 *>(base)[HALVES * (4 * (j / HALVES) + quarter) + j % HALVES];
     }
     // this workgroup's keys: whole steps of all waves
     const int lo = k.a.window ? max(0, p0 - k.a.window + 1) & ~63 : 0, hi = s.m;
@@ -622,8 +705,8 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const float lag = kLag / k.c;
-    const int koff = E == 8 ? 8 * (col >> 2) + (col & 3) : col;               // this lane's key of a step (bf16: and the one 4 on)
-    const unsigned page_bytes = (unsigned)kv.Hkv * (D * IO::kBytes) << kv.page_log, head_bytes = (unsigned)h * (D * IO::kBytes) << kv.page_log;
+    const int koff = E == 8 ? PE * (col >> 2) + (col & 3) : col;              // this lane's key of a step (bf16: and the one 4 on, 8 bits: the three)
+    const unsigned page_bytes = (unsigned)kv.Hkv * (D * IO::kPageBytes) << kv.page_log, head_bytes = (unsigned)h * (D * IO::kPageBytes) << kv.page_log;
     const unsigned k_at = head_bytes + ((quarter * 16u) << kv.page_log), k_next = 64u << kv.page_log, v_at = head_bytes + col * 16u;
     const unsigned P = (unsigned)kv.P;
 
@@ -631,8 +714,14 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
         if constexpr (decltype(stream)::value) return __builtin_bit_cast(uint4, stream_load(reinterpret_cast<const float4 *>(p)));
         else return *reinterpret_cast<const uint4 *>(p);
     };
-    uint4 kr[KTILES * QG], vr[DT];
+    uint4 kr[KTILES * GROUPS], vr[DT];
+    float k_scale = 1.f, v_scale = 1.f;
     int vpage = -1;
+    // scale of the block of this lane's keys (which = 0) or values
+    auto scale_at = [&](int page, int key, int which) {
+        if constexpr (IO::kCoded) return kv.scales[2 * ((((long long)page * kv.Hkv + h) << (kv.page_log - kKvBlockLog)) + ((key & mask) >> kKvBlockLog)) + which];
+        else return 1.f;
+    };
     // sections of keys whose page numbers fit LDS
     const int keys_a_section = kSection << kv.page_log;
     for (int sec = begin; sec < end; sec += keys_a_section) {
@@ -642,13 +731,14 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
         __syncthreads();
         auto page_at = [&](int key) { return key < sec_end ? pages[(key >> kv.page_log) - first] : -1; };
         auto request_keys = [&](int base) {
-            const int key = base + koff, page = page_at(base + (E == 8 ? 8 * (col >> 2) : col));     // keys at and behind the end lie in its page, or in none
+            const int key = base + koff, page = page_at(base + (E == 8 ? PE * (col >> 2) : col));    // keys at and behind the end lie in its page, or in none
             const char *kb = reinterpret_cast<const char *>(kv.k) + (unsigned long long)(unsigned)page * page_bytes + k_at + (key & mask) * 16u;
             auto all = [&](auto stream) {
 #pragma unroll
-                for (int j = 0; j < QG; ++j)
+                for (int j = 0; j < GROUPS; ++j)
 #pragma unroll
-                    for (int t = 0; t < KTILES; ++t) kr[t * QG + j] = load(kb + j * k_next + 64 * t, stream);
+                    for (int t = 0; t < KTILES; ++t) kr[t * GROUPS + j] = load(kb + j * k_next + 64 * t, stream);
+                k_scale = scale_at(page, key, 0);
             };
             if (__ballot((unsigned)page < P) == ~0ull) {                          // nothing to choose, nothing to clear
                 if (k.few_stream) all(std::true_type());
@@ -656,16 +746,17 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
                 return;
             }
 #pragma unroll
-            for (int i = 0; i < KTILES * QG; ++i) kr[i] = make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < KTILES * GROUPS; ++i) kr[i] = make_uint4(0, 0, 0, 0);
             if ((unsigned)page < P) all(std::false_type());
         };
         auto request_values = [&](int base) {
-            const int key = base + E * quarter;
+            const int key = base + PE * quarter;
             vpage = page_at(key);
-            const char *vb = reinterpret_cast<const char *>(kv.v) + (unsigned long long)(unsigned)vpage * page_bytes + v_at + ((key & mask) / E) * (D * 16u);
+            const char *vb = reinterpret_cast<const char *>(kv.v) + (unsigned long long)(unsigned)vpage * page_bytes + v_at + ((key & mask) / PE) * (D * 16u);
             auto all = [&](auto stream) {
 #pragma unroll
                 for (int d = 0; d < DT; ++d) vr[d] = load(vb + 256 * d, stream);
+                v_scale = scale_at(vpage, key, 1);
             };
             if (__ballot((unsigned)vpage < P) == ~0ull) {
                 if (k.few_stream) all(std::true_type());
@@ -691,11 +782,11 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
             for (int t = 0; t < KTILES; ++t) {
                 sc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < QG; ++j) IO::mma16(sc[t], kr[t * QG + j], q[j]);
+                for (int j = 0; j < QG; ++j) IO::mma16(sc[t], operand<IO>(kr[t * GROUPS + j / HALVES], j % HALVES, k_scale), q[j]);
             }
             if (more) request_keys(base + WAVES * SK);
             if (edge) {
-                const unsigned at = (unsigned)(base + E * quarter - lowest);
+                const unsigned at = (unsigned)(base + PE * quarter - lowest);
 #pragma unroll
                 for (int t = 0; t < KTILES; ++t)
 #pragma unroll
@@ -725,8 +816,27 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
                 }
             // two terms of a probability may be of different signs, or one of them zero: infinite values go their own way in every step
             bool look = edge, odd = false;
-            if constexpr (E == 8) look = look || __ballot(!all_finite_bf16<DT>(vr)) != 0;
-            if (look) {
+            if constexpr (IO::kCoded) {
+                uint32_t nans = 0;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) nans |= IO::nan_bits(vr[d]);
+                look = look || __ballot(nans != 0) != 0;
+            } else if constexpr (E == 8) look = look || __ballot(!all_finite_bf16<DT>(vr)) != 0;
+            if constexpr (IO::kCoded) {
+                if (look) {
+                    const int have = s.m - (base + PE * quarter);
+                    bool fine = true;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        if (have < PE) vr[d] = IO::keep_codes(vr[d], have);
+                        if (IO::nan_bits(vr[d])) {
+                            fine = false;
+                            vr[d] = IO::finite_codes(vr[d]);
+                        }
+                    }
+                    odd = __ballot(!fine) != 0;
+                }
+            } else if (look) {
                 const int have = s.m - (base + E * quarter);
                 bool fine = true;
 #pragma unroll
@@ -739,13 +849,26 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
                 }
                 odd = __ballot(!fine) != 0;
             }
-            const uint4 pg = IO::pack(p);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) IO::mma16(o[d], vr[d], pg);
-            if constexpr (E == 8) {                        // the rest of the probabilities: four more products a step cost nothing here
-                const uint4 rest = IO::pack_rest(p, pg);
+            for (int x = 0; x < HALVES; ++x) {
+                const uint4 pg = IO::pack(p + 8 * x);
+                if constexpr (IO::kCoded) {
+                    const uint4 rest = IO::pack_rest(p + 8 * x, pg);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) IO::mma16(o[d], vr[d], rest);
+                    for (int d = 0; d < DT; ++d) {
+                        const uint4 v = operand<IO>(vr[d], x, v_scale);
+                        IO::mma16(o[d], v, pg);
+                        IO::mma16(o[d], v, rest);
+                    }
+                } else {
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) IO::mma16(o[d], vr[d], pg);
+                    if constexpr (E == 8) {                // the rest of the probabilities: four more products a step cost nothing here
+                        const uint4 rest = IO::pack_rest(p, pg);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) IO::mma16(o[d], vr[d], rest);
+                    }
+                }
             }
             if (more) request_values(base + WAVES * SK);
             if (odd)
@@ -1057,8 +1180,12 @@ hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const Atte
     const int pairs = a.B * kv.Hkv;
     k.few_blocks = pairs * p.few_splits;
     k.tile_blocks = pairs * p.tile_splits * p.tiles;
+    // rows' type and the pages'
+    const bool coded = kv.layer_scales != 0;
 #define SPECTRE_ATTEND_DISPATCH(CALL)                                 \
-    if (io == SPECTRE_BF16 && d == 64) { CALL(Bf16Mma, 64); }         \
+    if (coded && d == 64) { CALL(E4m3Mma, 64); }                      \
+    else if (coded) { CALL(E4m3Mma, 128); }                           \
+    else if (io == SPECTRE_BF16 && d == 64) { CALL(Bf16Mma, 64); }    \
     else if (io == SPECTRE_BF16) { CALL(Bf16Mma, 128); }              \
     else if (d == 64) { CALL(F32Mma, 64); }                           \
     else { CALL(F32Mma, 128); }
@@ -1085,7 +1212,10 @@ hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const Atte
 #define CALL(IO, D)                                                                                                             \
     if (rows <= kWideRows) k_attend_join<IO, D, 1024 / D><<<(int)rows, 256, 0, st>>>(k);                                        \
     else k_attend_join<IO, D, 1><<<(int)((rows + 1024 / D - 1) / (1024 / D)), 256, 0, st>>>(k)
-        SPECTRE_ATTEND_DISPATCH(CALL)
+        if (io == SPECTRE_BF16 && d == 64) { CALL(Bf16Mma, 64); }
+        else if (io == SPECTRE_BF16) { CALL(Bf16Mma, 128); }
+        else if (d == 64) { CALL(F32Mma, 64); }
+        else { CALL(F32Mma, 128); }
 #undef CALL
     }
     return hipGetLastError();

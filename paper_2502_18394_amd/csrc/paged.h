@@ -7,21 +7,27 @@
 namespace spectre {
 
 constexpr int kKvStatusWords = 8;
+constexpr int kKvBlock = SPECTRE_KV_BLOCK, kKvBlockLog = 4;
+static_assert(kKvBlock == 1 << kKvBlockLog && kKvBlock == 16, "a block of tokens is a 16-byte group of values");
+inline int kv_size_of(int dtype) { return dtype == SPECTRE_BF16 ? 2 : dtype == SPECTRE_E4M3 ? 1 : 4; }
 
 // One pool as the kernels see it.  A page of one key/value head is page * d elements of K, [d / E][page][E], and as many of V,
 // [page / E][d][E], E = 16 bytes of elements: the 16-byte groups that a lane of a matrix instruction holds as its operand (adjacent channels of
 // a key for Q K^T, adjacent keys of a channel for P V), so tiles go from memory to the matrix cores in wide loads without a transposition.
 struct KvView {
     void *k, *v;                     // of one layer
+    float *scales;                   // the same, pages of 8 bits: [page][head][block of kKvBlock tokens][keys, values]
     int *status, *lens, *refs, *table;
     int P, S, M, Hkv, page_log;      // pages, sequences, table row, key/value heads, log2(tokens a page)
     long long layer_bytes;           // of K, and of V
+    long long layer_scales;          // 0: pages of another type
 };
 
 inline KvView kv_view(const spectre_kv *kv, int layer) {
     KvView w;
-    const int size = kv->dtype == SPECTRE_BF16 ? 2 : 4;
-    w.layer_bytes = (long long)kv->pages * kv->Hkv * kv->page * kv->d * size;
+    w.layer_bytes = (long long)kv->pages * kv->Hkv * kv->page * kv->d * kv_size_of(kv->dtype);
+    w.layer_scales = kv->dtype == SPECTRE_E4M3 ? (long long)kv->pages * kv->Hkv * (kv->page / kKvBlock) * 2 : 0;
+    w.scales = w.layer_scales ? kv->scales + layer * w.layer_scales : nullptr;
     w.k = (char *)kv->k + (long long)layer * w.layer_bytes;
     w.v = (char *)kv->v + (long long)layer * w.layer_bytes;
     w.status = kv->book;
@@ -37,6 +43,7 @@ inline KvView kv_view(const spectre_kv *kv, int layer) {
 hipError_t load_kernels_heads();
 hipError_t load_kernels_pages();
 hipError_t load_kernels_attend();
+hipError_t load_kernels_append8();
 
 // heads.hip
 struct HeadRows {                    // token t, head h, channel c at base + (t * stride + h * d + c)
@@ -47,6 +54,8 @@ struct HeadRows {                    // token t, head h, channel c at base + (t 
 hipError_t launch_heads_forward(const spectre_heads &P, int io, const HeadRows &x, const int *positions, void *q_out, void *k_out, hipStream_t st);
 hipError_t launch_heads_append(const spectre_heads &P, int io, const HeadRows &x, const KvView &kv, const int *positions, const int *start, const int *seqs, int B, void *q_out,
                                hipStream_t st);
+hipError_t launch_heads_append8(const spectre_heads &P, const HeadRows &x, const KvView &kv, const int *positions, const int *start, const int *seqs, int B, void *q_out,
+                                hipStream_t st);   // append8.hip
 int heads_backward_blocks(int T);
 hipError_t launch_heads_backward(const spectre_heads &P, int io, const HeadRows &x, const HeadRows &dy, const int *positions, void *gq, void *gk, float *gwq, float *gwk,
                                  double *partial, hipStream_t st);

@@ -22,8 +22,10 @@ int check_dtype(spectre_dtype io, const char *who) {
 int check_sizes(const spectre_kv *kv, const char *who) {
     if (!kv) return fail(SPECTRE_EINVAL, "%s: null pool", who);
     if (kv->layers < 1 || kv->pages < 1 || kv->Hkv < 1 || kv->seqs < 1 || kv->max_pages < 1) return fail(SPECTRE_EINVAL, "%s: a size of the pool is below 1", who);
-    const int rc = check_dtype(kv->dtype, who);
-    if (rc) return rc;
+    if (kv->dtype != SPECTRE_E4M3) {
+        const int rc = check_dtype(kv->dtype, who);
+        if (rc) return rc;
+    }
     if (kv->d != 64 && kv->d != 128) return fail(SPECTRE_EUNSUPPORTED, "%s: d = %d (64 and 128 are supported)", who, kv->d);
     if (kv->page < 16 || kv->page > 256 || (kv->page & (kv->page - 1))) return fail(SPECTRE_EUNSUPPORTED, "%s: %d tokens a page (16, 32, 64, 128, 256 are supported)", who, kv->page);
     if (kv->seqs > SPECTRE_KV_MAX_SEQS || kv->max_pages > SPECTRE_KV_MAX_TABLE || kv->pages > (1 << 28) || kv->Hkv > 4096 || kv->layers > 65536)
@@ -36,6 +38,7 @@ int check_pool(const spectre_kv *kv, const char *who) {
     if (rc) return rc;
     if (!kv->k || !kv->v || !kv->book) return fail(SPECTRE_EINVAL, "%s: null array in the pool", who);
     if (!aligned(kv->k, 16) || !aligned(kv->v, 16) || !aligned(kv->book, 4)) return fail(SPECTRE_EINVAL, "%s: pool array not aligned", who);
+    if (kv->dtype == SPECTRE_E4M3 && (!kv->scales || !aligned(kv->scales, 8))) return fail(SPECTRE_EINVAL, "%s: scales of the pool null or not aligned", who);
     return SPECTRE_OK;
 }
 
@@ -44,6 +47,9 @@ int check_ws(const void *ws, size_t have, size_t need, const char *who) {
     if (!aligned(ws, 16)) return fail(SPECTRE_EINVAL, "%s: workspace not 16-byte aligned", who);
     return SPECTRE_OK;
 }
+
+// Type of the rows that calls on a pool take.
+spectre_dtype rows_of(const spectre_kv *kv) { return kv->dtype == SPECTRE_E4M3 ? SPECTRE_BF16 : kv->dtype; }
 
 struct Span {
     const void *at;
@@ -125,15 +131,16 @@ extern "C" {
 
 size_t spectre_kv_bytes(const spectre_kv *kv, int which) {
     if (check_sizes(kv, "kv_bytes")) return 0;
-    const size_t rows = (size_t)kv->layers * kv->pages * kv->Hkv * kv->page * kv->d * size_of(kv->dtype);
+    const size_t rows = (size_t)kv->layers * kv->pages * kv->Hkv * kv->page * kv->d * kv_size_of(kv->dtype);
     if (which == SPECTRE_KV_K || which == SPECTRE_KV_V) return rows;
     if (which == SPECTRE_KV_BOOK) return ((size_t)kKvStatusWords + kv->seqs + kv->pages + (size_t)kv->seqs * kv->max_pages) * sizeof(int);
+    if (which == SPECTRE_KV_SCALES && kv->dtype == SPECTRE_E4M3) return (size_t)kv->layers * kv->pages * kv->Hkv * (kv->page / kKvBlock) * 2 * sizeof(float);
     fail(SPECTRE_EINVAL, "kv_bytes: unknown array %d", which);
     return 0;
 }
 
 int spectre_kv_prepare(void) {
-    hipError_t (*const loaders[])() = {load_kernels_heads, load_kernels_pages, load_kernels_attend};
+    hipError_t (*const loaders[])() = {load_kernels_heads, load_kernels_pages, load_kernels_attend, load_kernels_append8};
     for (auto load : loaders) {
         const hipError_t e = load();
         if (e != hipSuccess) return fail_hip(e, "kv_prepare: loading kernels");
@@ -260,24 +267,26 @@ int spectre_kv_append_at(const spectre_kv *kv, int layer, const spectre_heads *P
     int rc = check_pool(kv, who);
     if (rc) return rc;
     if ((rc = check_layer(kv, layer, who))) return rc;
-    if ((rc = check_heads(P, positions, T, H, kv->Hkv, kv->dtype, who))) return rc;
+    const spectre_dtype io = rows_of(kv);
+    if ((rc = check_heads(P, positions, T, H, kv->Hkv, io, who))) return rc;
     if (P->d != kv->d) return fail(SPECTRE_EINVAL, "%s: d = %d, the pool has %d", who, P->d, kv->d);
     if ((rc = check_batch(kv, start, B, T, H, who))) return rc;
     if (T == 0) return SPECTRE_OK;
     const Span in[3] = {{q, q_stride, H, "q"}, {k, k_stride, kv->Hkv, "k"}, {v, v_stride, kv->Hkv, "v"}};
     for (const Span &x : in)
-        if ((rc = check_rows(x, kv->d, kv->dtype, who))) return rc;
-    if ((rc = check_rows({q_out, (long long)H * kv->d, H, "q_out"}, kv->d, kv->dtype, who))) return rc;
+        if ((rc = check_rows(x, kv->d, io, who))) return rc;
+    if ((rc = check_rows({q_out, (long long)H * kv->d, H, "q_out"}, kv->d, io, who))) return rc;
     for (const Span &x : in)
-        if (overlap(x, q_out, H, T, kv->d, kv->dtype)) return fail(SPECTRE_EINVAL, "%s: q_out overlaps %s", who, x.name);
+        if (overlap(x, q_out, H, T, kv->d, io)) return fail(SPECTRE_EINVAL, "%s: q_out overlaps %s", who, x.name);
     const HeadRows x = {q, k, v, q_stride, k_stride, v_stride, T, H, kv->Hkv};
-    return done(launch_heads_append(*P, (int)kv->dtype, x, kv_view(kv, layer), positions, start, seqs, B, q_out, static_cast<hipStream_t>(stream)), who);
+    if (kv->dtype == SPECTRE_E4M3) return done(launch_heads_append8(*P, x, kv_view(kv, layer), positions, start, seqs, B, q_out, static_cast<hipStream_t>(stream)), who);
+    return done(launch_heads_append(*P, (int)io, x, kv_view(kv, layer), positions, start, seqs, B, q_out, static_cast<hipStream_t>(stream)), who);
 }
 
 size_t spectre_kv_attend_workspace_bytes(const spectre_kv *kv, int B, int T, int H, int max_new, int max_len, int window) {
     if (check_sizes(kv, "kv_attend") || check_attend(kv, B, T, H, max_new, max_len, window, "kv_attend")) return 0;
     if (window >= kLongest) window = 0;
-    const AttendPlan p = attend_plan(kv->d, (int)kv->dtype, B, T, H, kv->Hkv, max_new, max_len, window);
+    const AttendPlan p = attend_plan(kv->d, (int)rows_of(kv), B, T, H, kv->Hkv, max_new, max_len, window);
     if (check_plan(p, B, H, max_new, "kv_attend")) return 0;
     return align256(p.partial_bytes + 1);
 }
@@ -295,14 +304,15 @@ int spectre_kv_attend(const spectre_kv *kv, int layer, const void *q, long long 
     if (window >= kLongest) window = 0;                 // sees everything there can be
     if (T == 0) return SPECTRE_OK;
     const Span x = {q, q_stride, H, "q"};
-    if ((rc = check_rows(x, kv->d, kv->dtype, who))) return rc;
-    if ((rc = check_rows({out, (long long)H * kv->d, H, "out"}, kv->d, kv->dtype, who))) return rc;
-    if (overlap(x, out, H, T, kv->d, kv->dtype)) return fail(SPECTRE_EINVAL, "%s: out overlaps q", who);
-    const AttendPlan p = attend_plan(kv->d, (int)kv->dtype, B, T, H, kv->Hkv, max_new, max_len, window);
+    const spectre_dtype io = rows_of(kv);
+    if ((rc = check_rows(x, kv->d, io, who))) return rc;
+    if ((rc = check_rows({out, (long long)H * kv->d, H, "out"}, kv->d, io, who))) return rc;
+    if (overlap(x, out, H, T, kv->d, io)) return fail(SPECTRE_EINVAL, "%s: out overlaps q", who);
+    const AttendPlan p = attend_plan(kv->d, (int)io, B, T, H, kv->Hkv, max_new, max_len, window);
     if ((rc = check_plan(p, B, H, max_new, who))) return rc;
     if (p.partial_bytes && (rc = check_ws(ws, ws_bytes, align256(p.partial_bytes + 1), who))) return rc;
     const AttendArgs a = {q, q_stride, start, seqs, B, T, H, window, scale, out, lse};
-    return done(launch_attend(kv_view(kv, layer), kv->layers, kv->d, (int)kv->dtype, a, p, ws, static_cast<hipStream_t>(stream)), who);
+    return done(launch_attend(kv_view(kv, layer), kv->layers, kv->d, (int)io, a, p, ws, static_cast<hipStream_t>(stream)), who);
 }
 
 }  // extern "C"

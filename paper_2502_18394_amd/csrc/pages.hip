@@ -197,6 +197,17 @@ __global__ __launch_bounds__(kScan) void k_kv_fork_plan(KvView kv, const int *sr
 
 // Child i's row of the table, and the tokens of its last page: block x = child, y = slices of the layers' K and V.  Parents' rows and lengths are only
 // read (no child is a parent), users are counted with integer atomics, whose order changes nothing.
+// Scales of `blocks` blocks of tokens, of keys and values, from page a to page b of every head of a layer (pages of 8 bits; a block of a page of one head after the other).
+__device__ __forceinline__ void copy_scales(const KvView &kv, int layer, int a, int b, int blocks) {
+    if (!kv.layer_scales) return;
+    const int of_page = 1 << (kv.page_log - kKvBlockLog);
+    float2 *base = reinterpret_cast<float2 *>(kv.scales + layer * kv.layer_scales);
+    for (int i = threadIdx.x; i < kv.Hkv * blocks; i += 256) {
+        const int h = i / blocks, x = i - h * blocks;
+        base[((long long)b * kv.Hkv + h) * of_page + x] = base[((long long)a * kv.Hkv + h) * of_page + x];
+    }
+}
+
 __global__ __launch_bounds__(256) void k_kv_fork(KvView kv, int layers, int d, int E, const int *src, const int *dst, int n, const int *ws) {
     if (!ws[0]) return;
     const int i = blockIdx.x, a = src[i], b = dst[i], len = kv.lens[a], page = 1 << kv.page_log;
@@ -224,6 +235,7 @@ __global__ __launch_bounds__(256) void k_kv_fork(KvView kv, int layers, int d, i
     const int part = some * lanes;                                             // groups a row
     for (long long u = blockIdx.y; u < rows; u += gridDim.y) {
         const int h = (int)(u % kv.Hkv), which = (int)(u / kv.Hkv) & 1, layer = (int)(u / (2 * kv.Hkv));
+        if (h == 0 && which == 0) copy_scales(kv, layer, old, fresh, (rest + kKvBlock - 1) >> kKvBlockLog);
         uint4 *base = reinterpret_cast<uint4 *>((which ? (char *)kv.v : (char *)kv.k) + layer * kv.layer_bytes);
         const long long at = (long long)h * lanes << kv.page_log;
         const uint4 *x = base + old * block + at;
@@ -320,6 +332,7 @@ __device__ __forceinline__ void copy_pages(const KvView &kv, int layers, long lo
             if (threadIdx.x == 0 && unit == 0) atomicOr(&kv.status[0], SPECTRE_KV_BAD_ARGUMENT);
             continue;
         }
+        if (which == 0 && unit == 0) copy_scales(kv, layer, a, b, 1 << (kv.page_log - kKvBlockLog));
         float4 *base = reinterpret_cast<float4 *>((which ? (char *)kv.v : (char *)kv.k) + layer * kv.layer_bytes);
         const float4 *p = base + a * groups;
         float4 *q = base + b * groups;
@@ -378,7 +391,7 @@ hipError_t launch_kv_fork(const KvView &kv, int layers, int d, int io, const int
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int rows = layers * 2 * kv.Hkv, most = (2048 + n - 1) / n;
-    k_kv_fork<<<dim3(n, rows < most ? rows : most), 256, 0, st>>>(kv, layers, d, io == SPECTRE_BF16 ? 8 : 4, src, dst, n, ws);
+    k_kv_fork<<<dim3(n, rows < most ? rows : most), 256, 0, st>>>(kv, layers, d, 16 / kv_size_of(io), src, dst, n, ws);
     return hipGetLastError();
 }
 
