@@ -41,6 +41,10 @@ __device__ __forceinline__ void to_lds(const void *from, uint4 *to) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, kNonTemporal);
 }
 
+__device__ __forceinline__ void to_lds4(const float *from, float *to) {     // the same of 4 bytes
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 4, 0, 0);
+}
+
 struct AttendK {
     KvView kv;
     AttendArgs a;
@@ -331,8 +335,15 @@ __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 
 // softmax within a wave (17 % slower, d = 128 1 % faster), two tiles a barrier (3 % slower), raised priority around the products (no difference), tiles through registers (4 % slower).
 template <typename IO, int D>
 constexpr int kTileGroups = IO::kTileKeys * D / IO::E;
+// Groups of a tile as they lie in pages of 8 bits, on their way.
+template <typename IO, int D>
+constexpr int kRawGroups = IO::kCoded && D == 64 ? 8 * D + 8 * D / 4 : 0;    // and their scales
+// Groups of queries that registers have no room for beside those tiles.
+template <typename IO, int D, int WAVES>
+constexpr int kQueryGroups = kRawGroups<IO, D> && WAVES == 8 ? 3 * 64 * WAVES : 0;
 struct TileLds {
     uint4 *sk0, *sv0, *sk1, *sv1;                   // kTileGroups each, arrays of their own: the compiler sees which loads a read need not wait for
+    uint4 *raw, *query;                             // kRawGroups, kQueryGroups
     int *odd;                                       // [2] the last tile whose values were not all finite; [2]: tokens x parts in front of the sequence's places
 };
 
@@ -375,11 +386,15 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
         t_hi = min(t_hi, t_lo + per);
     }
 
+    constexpr int QL = kQueryGroups<IO, D, WAVES> / THREADS;                   // of a row's groups, the last ones, in LDS
     uint4 q[QG];
     {
         const char *base = reinterpret_cast<const char *>(k.a.q) + ((s.from + token) * k.a.q_stride + head * D) * IO::kBytes;
 #pragma unroll
-        for (int i = 0; i < QG; ++i) q[i] = reinterpret_cast<const uint4 *>(base)[2 * i + half];
+        for (int i = 0; i < QG; ++i) {
+            q[i] = reinterpret_cast<const uint4 *>(base)[2 * i + half];
+            if (i >= QG - QL) lds.query[(i - (QG - QL)) * THREADS + threadIdx.x] = q[i];
+        }
     }
     f32x16_t o[DT];
 #pragma unroll
@@ -453,44 +468,72 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
             if (p < P) to_lds<false>(vb + threadIdx.x % D * 16u, to + 64 * wave_now + THREADS * i);
         }
     };
-    // Pages of 8 bits go through registers: requested a tile ahead of being written to LDS as bf16 numbers, which is a tile ahead of their use.  A wave's 64 threads
-    // have the same 16 channels of a tile's keys, or groups of one (d = 128: of half a) block of its values.
+    // Pages of 8 bits are requested a tile ahead of being written to the tiles' LDS as bf16 numbers, which is a tile ahead of their use.  On their way they lie in LDS that only
+    // the wave that asked for them reads (d = 128: in registers, of which it has enough, and LDS not).  A wave's 64 threads have the same 16 channels of a tile's
+    // keys, or groups of one (d = 128: of half a) block of its values.  What stands for keys that are absent is what was there before: nobody's scores, and cleared values.
     constexpr int CODED = IO::kCoded ? 8 * D / THREADS : 1;                  // groups a thread, keys' first
+    constexpr bool RAW = kRawGroups<IO, D> > 0;
     uint4 code[CODED];
-    float code_scale[CODED];
+    float code_scale[CODED] = {};
     auto request_codes = [&](int t, int page) {
         if constexpr (IO::kCoded) {
+            int lane = threadIdx.x;
+            asm volatile("" : "+v"(lane));                                   // opaque: what is formed of it is not kept in registers from tile to tile
+            lane &= 63;
 #pragma unroll
             for (int i = 0; i < CODED; ++i) {
                 const int u = 64 * wave + THREADS * i;
-                code_scale[i] = -1.f;
-                const int kg = (u - 4 * D) / D;                              // block of values
-                const int p = u < 4 * D ? page : __builtin_amdgcn_readlane(page, 16 * (kg > 0 ? kg : 0));
-                if ((unsigned)p >= P) continue;
-                const int slot = (t * KT + (u < 4 * D ? lane : 16 * kg)) & mask;
-                const unsigned at = u < 4 * D ? (((u / KT) * 16u) << kv.page_log) + slot * 16u : (slot >> kKvBlockLog) * (D * 16u) + ((u - 4 * D) % D + lane) * 16u;
-                const char *from = (u < 4 * D ? k_head : v_head) + (unsigned long long)(unsigned)p * page_bytes + at;
-                code[i] = *reinterpret_cast<const uint4 *>(from);
-                code_scale[i] = kv.scales[2 * ((((long long)p * kv.Hkv + h) << (kv.page_log - kKvBlockLog)) + (slot >> kKvBlockLog)) + (u < 4 * D ? 0 : 1)];
+                const bool keys = u < 4 * D;
+                const int kg = keys ? 0 : (u - 4 * D) / D;                   // block of values
+                auto request = [&](const char *from, const float *scale) {
+                    if constexpr (RAW) {
+                        to_lds<false>(from, lds.raw + u);
+                        to_lds4(scale, reinterpret_cast<float *>(lds.raw + 8 * D) + u);
+                    } else {
+                        code[i] = *reinterpret_cast<const uint4 *>(from);
+                        code_scale[i] = *scale;
+                    }
+                };
+                if (one_page || !keys) {                                     // scalar addresses
+                    const int p = one_page ? __builtin_amdgcn_readfirstlane(page) : __builtin_amdgcn_readlane(page, 16 * kg);
+                    if ((unsigned)p >= P) continue;
+                    const int slot = (t * KT + 16 * kg) & mask;
+                    const long long head = (long long)p * kv.Hkv + h;
+                    const char *base = reinterpret_cast<const char *>(keys ? kv.k : kv.v) + (head << kv.page_log) * D;
+                    const float *scale = kv.scales + 2 * ((head << (kv.page_log - kKvBlockLog)) + (slot >> kKvBlockLog));
+                    if (keys) request(base + ((((u / KT) << kv.page_log) + slot) * 16u) + lane * 16u, scale + (lane >> 4) * 2);
+                    else request(base + ((slot >> kKvBlockLog) * D + (u - 4 * D) % D) * 16u + lane * 16u, scale + 1);
+                } else {
+                    if ((unsigned)page >= P) continue;
+                    const int slot = (t * KT + lane) & mask;
+                    const long long head = (long long)page * kv.Hkv + h;
+                    request(reinterpret_cast<const char *>(kv.k) + (head << kv.page_log) * D + (((u / KT) << kv.page_log) + slot) * 16u,
+                            kv.scales + 2 * ((head << (kv.page_log - kKvBlockLog)) + (slot >> kKvBlockLog)));
+                }
             }
         }
     };
     auto write_codes = [&](uint4 *sk, uint4 *sv) {
         if constexpr (IO::kCoded) {
+            int at = threadIdx.x;
+            asm volatile("" : "+v"(at));
+            if constexpr (RAW) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < CODED; ++i) {
+                    code[i] = lds.raw[at + THREADS * i];
+                    code_scale[i] = reinterpret_cast<const float *>(lds.raw + 8 * D)[at + THREADS * i];
+                }
+            }
+            const int lane = at & 63;
 #pragma unroll
             for (int i = 0; i < CODED; ++i) {
                 const int u = 64 * wave + THREADS * i;
-                if (code_scale[i] < 0.f) continue;                           // absent: what lies there stays
-                const uint4 lo = operand<IO>(code[i], 0, code_scale[i]), hi = operand<IO>(code[i], 1, code_scale[i]);
-                if (u < 4 * D) {
-                    sk[2 * (u / KT) * KT + lane] = lo;
-                    sk[(2 * (u / KT) + 1) * KT + lane] = hi;
-                } else {
-                    const int x = u - 4 * D, kg = x / D, c = x % D + lane;
-                    sv[2 * kg * D + c] = lo;
-                    sv[(2 * kg + 1) * D + c] = hi;
-                }
+                uint4 *to = u < 4 * D ? sk + 2 * (u / KT) * KT + lane : sv + 2 * ((u - 4 * D) / D) * D + (u - 4 * D) % D + lane;
+                to[0] = operand<IO>(code[i], 0, code_scale[i]);
+                to[u < 4 * D ? KT : D] = operand<IO>(code[i], 1, code_scale[i]);
             }
+            if constexpr (RAW) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the next tile's come there
         }
     };
     auto arrived = [&]() {
@@ -545,7 +588,7 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
         return mx;
     };
     auto keep_up = [&](float mx) {                                      // with the maximum mx of a tile's scores, of both halves
-        if (!__ballot(lags(mx, top, lag))) return;
+        if (!__ballot(IO::kCoded ? (mx - top) * k.c > kLag : lags(mx, top, lag))) return;     // no register for the lag, either
         const float f = follow(mx, k.c, &top);
         sum *= f;
 #pragma unroll
@@ -559,6 +602,13 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
     };
     const int krow = IO::key_of_row(lane & 31);
     auto scores = [&](const uint4 *sk, f32x16_t(&sc)[NK]) {
+        uint4 ql[QL ? QL : 1];
+        if constexpr (QL > 0) {
+            int at = threadIdx.x;
+            asm volatile("" : "+v"(at));
+#pragma unroll
+            for (int i = 0; i < QL; ++i) ql[i] = lds.query[i * THREADS + at];
+        }
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
 #pragma unroll
@@ -568,39 +618,47 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
             for (int i = 0; i < QG; ++i) a[i] = sk[(2 * i + half) * KT + 32 * n + krow];
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < QG; ++i) IO::mma32(sc[n], a[i], q[i]);
+            for (int i = 0; i < QG; ++i) IO::mma32(sc[n], a[i], QL && i >= QG - QL ? ql[i - (QG - QL)] : q[i]);
         }
     };
     if (threadIdx.x < 2) odd[threadIdx.x] = -1;
-    int page = page_of(t_lo), next = page_of(t_lo + 1), later = IO::kCoded ? page_of(t_lo + 2) : -1;
+    int page = page_of(t_lo), next = page_of(t_lo + 1);
+    unsigned long long here = 0, soon = 0;               // which keys of this tile and the next are there (pages of 8 bits, whose page numbers are not kept so long)
     if (t_lo < t_hi) {
         if constexpr (IO::kCoded) {
+            here = __ballot((unsigned)page < P);
             request_codes(t_lo, page);
             write_codes(sk0, sv0);
+            soon = __ballot((unsigned)next < P);
             request_codes(t_lo + 1, next);
+            next = page_of(t_lo + 2);
         } else {
             request_keys(t_lo, page, sk0);
             request_values(t_lo, page, sv0);
         }
     }
     auto tile_step = [&](int t, uint4 *sk, uint4 *sv, uint4 *next_k, uint4 *next_v, int *flag) {
-        const unsigned long long there = __ballot((unsigned)page < P);      // bit = key of the tile (fp32: twice 32 keys)
+        const unsigned long long there = IO::kCoded ? here : __ballot((unsigned)page < P);      // bit = key of the tile (fp32: twice 32 keys)
         arrived();
-        page = next;
         if constexpr (IO::kCoded) {
             write_codes(next_k, next_v);
-            next = later;
-            request_codes(t + 2, next);
-            later = page_of(t + 3);
-        } else if (t + 1 < t_hi) {
+            here = soon;
+            soon = __ballot((unsigned)next < P);
+        } else page = next;
+        if (!IO::kCoded && t + 1 < t_hi) {
             request_keys(t + 1, page, next_k);
             request_values(t + 1, page, next_v);
             next = page_of(t + 2);
         }
         clean(t, there, sv, flag);
-        if (!busy || t * KT > wave_last) return;
+        const bool idle = !busy || t * KT > wave_last;
         f32x16_t sc[NK];
-        scores(sk, sc);
+        if (!idle) scores(sk, sc);
+        if constexpr (IO::kCoded) {        // behind the scores: queries that registers have no room for are read again for them, and whoever waits for those waits for all before
+            request_codes(t + 2, next);
+            next = page_of(t + 3);
+        }
+        if (idle) return;
         hide(t, there, sc);
         keep_up(max_halves(largest(sc)));
         const float shift = shift_of(top, k.c);
@@ -930,25 +988,31 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
 
 // ---------------------------------------------------------------- the launches: either kind, or both for a mixed batch
 template <typename IO, int D>
-__global__ __launch_bounds__(256, D == 64 ? 4 : 3) void k_attend_few(AttendK k) {
+__global__ __launch_bounds__(256, D == 64 ? 4 : IO::kCoded ? 2 : 3) void k_attend_few(AttendK k) {
     __shared__ int pages[kSection + 2];
     __shared__ float tops[4][16], sums[4][16];
     __shared__ f32x4_t outs[4][kFewGroups<IO, D>];
     few_rows<IO, D, 4>(k, blockIdx.x, FewLds{pages, tops, sums, outs[0], outs[1], outs[2], outs[3]});
 }
 
+// Waves a SIMD that registers (and, of workgroups of four waves with pages of 8 bits, LDS) leave room for.
 template <typename IO, int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k_attend_tile(AttendK k) {
+constexpr int tile_waves_a_simd() { return IO::E == 8 && D == 64 ? (IO::kCoded && WAVES == 4 ? 3 : 4) : 2; }
+
+template <typename IO, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (tile_waves_a_simd<IO, D, WAVES>())) void k_attend_tile(AttendK k) {
     __shared__ uint4 sk0[kTileGroups<IO, D>], sv0[kTileGroups<IO, D>], sk1[kTileGroups<IO, D>], sv1[kTileGroups<IO, D>];
+    __shared__ uint4 raw[kRawGroups<IO, D> ? kRawGroups<IO, D> : 1], query[kQueryGroups<IO, D, WAVES> ? kQueryGroups<IO, D, WAVES> : 1];
     __shared__ int odd[3];
-    tile_of_rows<IO, D, WAVES>(k, blockIdx.x, TileLds{sk0, sv0, sk1, sv1, odd});
+    tile_of_rows<IO, D, WAVES>(k, blockIdx.x, TileLds{sk0, sv0, sk1, sv1, raw, query, odd});
 }
 
 // The tiles of a batch's prompts, which arithmetic bounds, and behind them its single tokens, which memory bounds, where the tiles leave compute units free (before
 // them, or dealt out evenly: 32 ragged sequences 258 and 261 instead of 234 us; two launches 310).
 template <typename IO, int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k_attend_mixed(AttendK k) {
+__global__ __launch_bounds__(64 * WAVES, (tile_waves_a_simd<IO, D, WAVES>())) void k_attend_mixed(AttendK k) {
     __shared__ uint4 sk0[kTileGroups<IO, D>], sv0[kTileGroups<IO, D>], sk1[kTileGroups<IO, D>], sv1[kTileGroups<IO, D>];
+    __shared__ uint4 raw[kRawGroups<IO, D> ? kRawGroups<IO, D> : 1], query[kQueryGroups<IO, D, WAVES> ? kQueryGroups<IO, D, WAVES> : 1];
     __shared__ int odd[3], pages[kSection + 2];
     __shared__ float tops[WAVES][16], sums[WAVES][16];
     static_assert(kTileGroups<IO, D> >= (WAVES / 4) * kFewGroups<IO, D>, "outputs of few rows fit where tiles lie");
@@ -957,7 +1021,7 @@ __global__ __launch_bounds__(64 * WAVES, (IO::E == 8 && D == 64 ? 4 : 2)) void k
         few_rows<IO, D, WAVES>(k, block - tiles, FewLds{pages, tops, sums, reinterpret_cast<f32x4_t *>(sk0), reinterpret_cast<f32x4_t *>(sv0), reinterpret_cast<f32x4_t *>(sk1),
                                                         reinterpret_cast<f32x4_t *>(sv1)});
     } else if (block < k.tile_blocks) {
-        tile_of_rows<IO, D, WAVES>(k, block, TileLds{sk0, sv0, sk1, sv1, odd});
+        tile_of_rows<IO, D, WAVES>(k, block, TileLds{sk0, sv0, sk1, sv1, raw, query, odd});
     }
 }
 
@@ -1065,7 +1129,7 @@ constexpr long long kMostThreads = (1ll << 32) - 1;
 // 4000 over 60000, d = 128, 0.4 instead of 4.6 GB: 7102, before 6786).
 constexpr long long kPartBytes = 256ll << 20;
 
-AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new, int max_len, int window) {
+AttendPlan attend_plan(int d, int dtype, int B, int T, int H, int Hkv, int max_new, int max_len, int window) {
     AttendPlan p{};
     p.fits = true;
     if (T == 0 || B == 0) return p;                                // nothing to launch
@@ -1102,13 +1166,13 @@ AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new,
         // where many keys are left to split (2048 over 28672, d = 128: 494 instead of 518 us; a 1024-token prompt of its own would lose, 44 instead of 34).
         // A ragged fp32 batch has 128: its products take longer than the keys' way.
         // So have rows that fit 128 (256 sequences of 32 tokens 30 instead of 37 us, 90 of 16 over 1000, d = 128, 41 instead of 54).
-        const bool slow = io != SPECTRE_BF16 && !even && rows > 128;
+        const bool slow = dtype == SPECTRE_F32 && !even && rows > 128;
         p.tile_waves = groups(8) >= (even && len >= 8192 ? 128 : 256) && !slow && rows > 128 ? 8 : 4;
         p.tiles = (int)((rows + 32 * p.tile_waves - 1) / (32 * p.tile_waves));
         // workgroups that run at once, by their registers and LDS; keys are split where rows leave some of them free.  Of single tiles, which memory bounds, two a
         // compute unit are enough: the join costs more than a third and fourth gain (64 sequences of 8 tokens over 2000 48 instead of 55 us, 16 over 9000 53 instead
         // of 58; one a compute unit: 50 and 73).
-        const long long slots = p.tile_waves == 8 || d == 128 || rows <= 128 ? 512 : io == SPECTRE_BF16 ? 1024 : 768;
+        const long long slots = p.tile_waves == 8 || d == 128 || rows <= 128 ? 512 : dtype == SPECTRE_BF16 ? 1024 : 768;        // pages of 8 bits: LDS for three workgroups
         // Parts of the longest sequence; the others' parts are as long.  With several tiles a sequence of a ragged batch they take different times, and
         // twice the parts even them out (fp32 batch of up to 397 new tokens 135 instead of 142 us; single tiles, bound by memory, lose: 25.0 -> 28.8).
         const long long all = groups(p.tile_waves), keys = all > 4 * slots ? 2 * kRaggedKeys : kRaggedKeys;

@@ -88,7 +88,7 @@ struct AttendArgs {
     void *out;
     float *lse;
 };
-AttendPlan attend_plan(int d, int io, int B, int T, int H, int Hkv, int max_new, int max_len, int window);
+AttendPlan attend_plan(int d, int dtype, int B, int T, int H, int Hkv, int max_new, int max_len, int window);
 hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const AttendArgs &a, const AttendPlan &p, void *ws, hipStream_t st);
 
 }  // namespace spectre

@@ -286,7 +286,7 @@ int spectre_kv_append_at(const spectre_kv *kv, int layer, const spectre_heads *P
 size_t spectre_kv_attend_workspace_bytes(const spectre_kv *kv, int B, int T, int H, int max_new, int max_len, int window) {
     if (check_sizes(kv, "kv_attend") || check_attend(kv, B, T, H, max_new, max_len, window, "kv_attend")) return 0;
     if (window >= kLongest) window = 0;
-    const AttendPlan p = attend_plan(kv->d, (int)rows_of(kv), B, T, H, kv->Hkv, max_new, max_len, window);
+    const AttendPlan p = attend_plan(kv->d, (int)kv->dtype, B, T, H, kv->Hkv, max_new, max_len, window);
     if (check_plan(p, B, H, max_new, "kv_attend")) return 0;
     return align256(p.partial_bytes + 1);
 }
@@ -308,7 +308,7 @@ int spectre_kv_attend(const spectre_kv *kv, int layer, const void *q, long long 
     if ((rc = check_rows(x, kv->d, io, who))) return rc;
     if ((rc = check_rows({out, (long long)H * kv->d, H, "out"}, kv->d, io, who))) return rc;
     if (overlap(x, out, H, T, kv->d, io)) return fail(SPECTRE_EINVAL, "%s: out overlaps q", who);
-    const AttendPlan p = attend_plan(kv->d, (int)io, B, T, H, kv->Hkv, max_new, max_len, window);
+    const AttendPlan p = attend_plan(kv->d, (int)kv->dtype, B, T, H, kv->Hkv, max_new, max_len, window);
     if ((rc = check_plan(p, B, H, max_new, who))) return rc;
     if (p.partial_bytes && (rc = check_ws(ws, ws_bytes, align256(p.partial_bytes + 1), who))) return rc;
     const AttendArgs a = {q, q_stride, start, seqs, B, T, H, window, scale, out, lse};
