@@ -474,7 +474,7 @@ enum { SPECTRE_KV_NO_PAGES = 1, SPECTRE_KV_TOO_LONG = 2, SPECTRE_KV_BAD_ARGUMENT
 /* Bytes of the pool's arrays (which: SPECTRE_KV_K, _V, _BOOK, with pages of 8 bits _SCALES); 0 for a pool that is not supported.  Only sizes and dtype are read. */
 size_t spectre_kv_bytes(const spectre_kv *kv /*host*/, int which);
 
-/* Set-up, once per device before any call below is captured into a graph: loads their kernels. */
+/* Set-up, once per device before any call below is captured into a graph: loads their kernels (those of the norm, too). */
 int spectre_kv_prepare(void);
 
 /* Empty bookkeeping: no sequence has a token, no page a user.  Page contents are left as they are. */
@@ -542,6 +542,23 @@ int spectre_kv_append_at(const spectre_kv *kv /*host*/, int layer, const spectre
 int spectre_kv_append(const spectre_kv *kv /*host*/, int layer, const spectre_heads *P /*host*/, const void *q, long long q_stride, const void *k,
                       long long k_stride, const void *v, long long v_stride, const int *start, const int *seqs, int B, int T, int H,
                       void *q_out, void *stream);
+
+/*
+ * A residual's addition and the root-mean-square norm of the sum, in one pass: sum = x + delta (rounded to io, and normed as it is kept),
+ * y = w * sum / sqrt(mean sum^2 + eps).  Rows x, delta [T, D], row t `stride` elements from row t - 1 (a multiple of 16 bytes, at least D), 16-byte aligned;
+ * outputs are dense.  D * size of io: a multiple of 16 bytes, up to 32768.  delta and sum NULL: y is the norm of x.  w device fp32 [D], 16-byte aligned, NULL: ones.
+ *   y_type  io, or SPECTRE_E4M3: codes [T, D] with scales fp32 [T, D / SPECTRE_NORM_GROUP], D a multiple of that; a scale is the largest magnitude of its channels
+ *           / 448 (0, and with it codes of 0, where that is below 2^-126), what is meant is code * scale.  scales NULL otherwise.
+ * spectre_norm_backward: from dy (of y, in io whatever y's type was), sum as it was kept (without an addition: x) and dsum (of sum as a residual, NULL: none) the gradient
+ * gx [T, D], which is x's and delta's, and gw fp32 [D] (NULL: not wanted), whose sums over rows are of up to 128 rows in fp32, those sums in fp64, all in a fixed
+ * order.  Workspace for gw only.  spectre_kv_prepare loads the kernels.
+ */
+enum { SPECTRE_NORM_GROUP = 128 };
+int spectre_norm_forward(const void *x, long long x_stride, const void *delta, long long delta_stride, const float *w, int T, int D, float eps, spectre_dtype io,
+                         void *sum, void *y, spectre_dtype y_type, float *scales, void *stream);
+size_t spectre_norm_backward_workspace_bytes(int T, int D, spectre_dtype io);
+int spectre_norm_backward(const void *dy, long long dy_stride, const void *sum, long long sum_stride, const void *dsum, long long dsum_stride, const float *w,
+                          int T, int D, float eps, spectre_dtype io, void *gx, float *gw, void *ws, size_t ws_bytes, void *stream);
 
 /*
  * spectre_kv_attend - attention of new tokens over the pages: query i of a sequence's n stands at p = lens - n + i and sees the keys j <= p, with

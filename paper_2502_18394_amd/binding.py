@@ -75,7 +75,7 @@ def lib():
                      "spectre_prefix_update_workspace_bytes", "spectre_prefix_readout_workspace_bytes",
                      "spectre_prefix_step_workspace_bytes", "spectre_prefix_set_memory_workspace_bytes",
                      "spectre_mix_static_bytes", "spectre_layer_workspace_bytes", "spectre_kv_bytes", "spectre_kv_workspace_bytes",
-                     "spectre_kv_attend_workspace_bytes", "spectre_heads_backward_workspace_bytes"):
+                     "spectre_kv_attend_workspace_bytes", "spectre_heads_backward_workspace_bytes", "spectre_norm_backward_workspace_bytes"):
             getattr(L, name).restype = ctypes.c_size_t
         L.spectre_get_option.restype = ctypes.c_long
         # with the types declared, ctypes converts plain integers itself: a wrapper object per argument costs a few
@@ -103,6 +103,9 @@ def lib():
                 "spectre_heads_backward": (p, p, ll, p, ll, p, ll, p, ll, p, i, i, i, i, p, p, p, p, p, n, p),
                 "spectre_kv_append": (p, i, p, p, ll, p, ll, p, ll, p, p, i, i, i, p, p),
                 "spectre_kv_append_at": (p, i, p, p, ll, p, ll, p, ll, p, p, p, i, i, i, p, p),
+                "spectre_norm_forward": (p, ll, p, ll, p, i, i, ctypes.c_float, i, p, p, i, p, p),
+                "spectre_norm_backward_workspace_bytes": (i, i, i),
+                "spectre_norm_backward": (p, ll, p, ll, p, ll, p, i, i, ctypes.c_float, i, p, p, p, n, p),
                 "spectre_kv_attend_workspace_bytes": (p, i, i, i, i, i, i),
                 "spectre_kv_attend": (p, i, p, ll, p, p, i, i, i, i, i, ctypes.c_float, i, p, p, p, n, p)}.items():
             getattr(L, name).argtypes = types
@@ -666,6 +669,89 @@ def qk_norm_rotate_backward(dq, dk, q, k, positions=None, rope=None, wq=None, wk
                                         None if gw[0] is None else gw[0].data_ptr(), None if gw[1] is None else gw[1].data_ptr(), wsp, wsn,
                                         _now(stream)))
     return gq, gk, gw[0], gw[1]
+
+
+def _matrix(t, name, like=None):
+    """(address, elements from row to row) of rows [T, D] whose channels are adjacent."""
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{name} must be a device tensor [T, D]")
+    if like is not None:
+        _same(t, like, name)
+    st, sc = t.stride()
+    if sc != 1 and t.shape[1] > 1:
+        raise ValueError(f"{name} must have adjacent channels")
+    return t.data_ptr(), st if t.shape[0] > 1 else t.shape[1]
+
+
+def _norm_weight(weight, D):
+    if weight is None:
+        return None
+    if weight.dtype != torch.float32 or tuple(weight.shape) != (D,):
+        raise ValueError(f"weight must be float32 [{D}]")
+    return _ptr(weight, "weight")
+
+
+NORM_GROUP = 128
+
+
+def add_norm(x, weight=None, delta=None, eps=1e-6, dtype=None, sum_out=None, out=None, scales=None, stream=None):
+    """A residual's addition and the root-mean-square norm of the sum in one pass (spectre_norm_forward).  x, delta [T, D] f32/bf16, rows any 16-byte multiple
+    apart; weight float32 [D] (None: ones).  Returns (sum, y), the sum in x's dtype (x itself without delta), y in x's dtype, or with dtype=torch.float8_e4m3fn
+    (sum, codes, scales): a float32 scale for each 128 channels, scales [T, D / 128], and what is meant is code * scale."""
+    T, D = x.shape
+    io, coded = _dtype_code(x), dtype == torch.float8_e4m3fn
+    if dtype is not None and not coded and dtype != x.dtype:
+        raise TypeError(f"the norm of {x.dtype} rows is {x.dtype} or float8_e4m3fn, not {dtype}")
+    xa, xs = _matrix(x, "x")
+    da, ds = (None, 0) if delta is None else _matrix(delta, "delta", x)
+    if delta is None:
+        if sum_out is not None:
+            raise ValueError("without delta there is no sum")
+    elif sum_out is None:
+        sum_out = _like(x, stream)
+    else:
+        _same(sum_out, x, "sum_out")
+    if coded:
+        if D % NORM_GROUP:
+            raise ValueError(f"rows of 8 bits have a multiple of {NORM_GROUP} channels")
+        if out is None:
+            out = _new((T, D), dtype, x.device, stream)
+        if scales is None:
+            scales = _new((T, D // NORM_GROUP), torch.float32, x.device, stream)
+        elif scales.dtype != torch.float32 or tuple(scales.shape) != (T, D // NORM_GROUP):
+            raise ValueError(f"scales must be float32 [{T}, {D // NORM_GROUP}]")
+        if out.dtype != dtype or tuple(out.shape) != (T, D):
+            raise ValueError(f"out must be {dtype} [{T}, {D}]")
+    elif scales is not None:
+        raise ValueError("scales are of 8 bits' rows")
+    elif out is None:
+        out = _like(x, stream)
+    else:
+        _same(out, x, "out")
+    _check(lib().spectre_norm_forward(xa, xs, da, ds, _norm_weight(weight, D), T, D, eps, io, None if delta is None else _ptr(sum_out, "sum_out"), _ptr(out, "out"),
+                                      E4M3 if coded else io, _ptr(scales, "scales") if coded else None, _now(stream)))
+    total = x if delta is None else sum_out
+    return (total, out, scales) if coded else (total, out)
+
+
+def add_norm_backward(dy, total, weight=None, dsum=None, eps=1e-6, ws=None, stream=None):
+    """Gradients of add_norm (spectre_norm_backward): dy of its y (in the rows' dtype, of 8 bits' rows as if they had not been rounded), total: the sum it returned,
+    dsum: the gradient of that sum where it goes on as a residual (None: nothing comes from there).  Returns (gx, gw): gx is the gradient of x and of delta, gw float32
+    [D], None without a weight."""
+    T, D = total.shape
+    io = _dtype_code(total)
+    ta, ts = _matrix(total, "total")
+    ya, ys = _matrix(dy, "dy", total)
+    da, ds = (None, 0) if dsum is None else _matrix(dsum, "dsum", total)
+    w = _norm_weight(weight, D)
+    gx, gw, wsp, wsn = _like(total, stream), None, None, 0
+    if weight is not None:
+        gw = _new((D,), torch.float32, total.device, stream)
+        if ws is None:
+            ws = _new((lib().spectre_norm_backward_workspace_bytes(T, D, io) + 256,), torch.uint8, total.device, stream)
+        wsp, wsn = _given(ws)
+    _check(lib().spectre_norm_backward(ya, ys, ta, ts, da, ds, w, T, D, eps, io, _ptr(gx, "gx"), None if gw is None else _ptr(gw, "gw"), wsp, wsn, _now(stream)))
+    return gx, gw
 
 
 class KvPages:

@@ -41,18 +41,18 @@ __device__ __forceinline__ void cut(float (&x)[8], float scale) {
         if (fabsf(x[e]) > kCut && fabsf(x[e]) < INFINITY) x[e] = copysignf(kCut, x[e]);
 }
 
-template <int D>
+template <int D, bool AXES>
 __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, const int *positions, uint4 *q_out, KvView kv, const int *start, const int *seqs, int B) {
     constexpr int TOKENS = kKvBlock, LANES = D / 8, ROWS = kThreads / LANES, HEADS = ROWS / TOKENS, WAVES = LANES * TOKENS / 64;    // key heads at once; waves of each
     constexpr int VROW = D / 4 + D / 16;             // words of a token's coded values in LDS: four tokens on are a quarter or half of the banks on
     __shared__ float2 turns[TOKENS][kMostHalf];
-    __shared__ int pos[kMostAxes][TOKENS];
+    __shared__ int pos[kAxesOf<AXES>][TOKENS];
     __shared__ float weights[2][D];
     __shared__ float most[kThreads / 64][2];
     __shared__ __align__(16) uint32_t coded[HEADS][TOKENS][VROW];
     Run run;
     if (!find_run<TOKENS>(kv, start, seqs, B, X.T, blockIdx.x, &run)) return;
-    fill_positions<TOKENS>(P, positions, X.T, run.first, run.index, run.count, pos);
+    fill_positions<AXES, TOKENS>(P, AXES ? positions : nullptr, X.T, run.first, run.index, run.count, pos);
     for (int i = threadIdx.x; i < D; i += kThreads) {
         weights[0][i] = P.wq ? P.wq[i] : 1.f;
         weights[1][i] = P.wk ? P.wk[i] : 1.f;
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, 
     const int p = run.index >> kv.page_log, slot = run.index & ((1 << kv.page_log) - 1), had = slot & (TOKENS - 1);       // tokens that the block has already
     const int page = p < kv.M ? kv.table[(long long)run.seq * kv.M + p] : -1;
     __syncthreads();
-    fill_turns(P, pos, run.count, turns);
+    fill_turns<AXES>(P, pos, run.count, turns);
     __syncthreads();
     const bool in_pool = (unsigned)page < (unsigned)kv.P;
     const int users = in_pool ? kv.refs[page] : 0;   // a page with several users holds another sequence's tokens, too
@@ -187,14 +187,15 @@ __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, 
 
 hipError_t load_kernels_append8() {
     hipFuncAttributes a;
-    return hipFuncGetAttributes(&a, reinterpret_cast<const void *>(k_append8<64>));
+    return hipFuncGetAttributes(&a, reinterpret_cast<const void *>(k_append8<64, false>));
 }
 
 hipError_t launch_heads_append8(const spectre_heads &P, const HeadRows &x, const KvView &kv, const int *positions, const int *start, const int *seqs, int B, void *q_out,
                                 hipStream_t st) {
     const int blocks = x.T / kKvBlock + 2 * B, most = 2048 / blocks, parts = most < 1 ? 1 : most > 4 ? 4 : most;
-    if (P.d == 64) k_append8<64><<<dim3(blocks, parts), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, kv, start, seqs, B);
-    else k_append8<128><<<dim3(blocks, parts), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, kv, start, seqs, B);
+    auto launch = [&](auto kernel) { kernel<<<dim3(blocks, parts), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, kv, start, seqs, B); };
+    if (P.d == 64) positions ? launch(k_append8<64, true>) : launch(k_append8<64, false>);
+    else positions ? launch(k_append8<128, true>) : launch(k_append8<128, false>);
     return hipGetLastError();
 }
 

@@ -13,16 +13,16 @@ namespace {
 
 constexpr int kTokens = 8;                      // a workgroup: one 16-byte group of V pages, two in fp32
 
-template <typename IO, int D, bool SERVE>
+template <typename IO, int D, bool SERVE, bool AXES>
 __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, const int *positions, uint4 *q_out, uint4 *k_out, KvView kv, const int *start, const int *seqs,
                                                     int B, bool stream) {
     constexpr int E = IO::E, LANES = D / E, ROWS = kThreads / LANES;
     __shared__ float2 turns[kTokens][kMostHalf];
-    __shared__ int pos[kMostAxes][kTokens];
+    __shared__ int pos[kAxesOf<AXES>][kTokens];
     __shared__ float weights[2][D];
     Run run{(int)blockIdx.x * kTokens, min(kTokens, X.T - (int)blockIdx.x * kTokens), 0, 0};
     if (SERVE && !find_run<kTokens>(kv, start, seqs, B, X.T, blockIdx.x, &run)) return;
-    fill_positions<kTokens>(P, positions, X.T, run.first, SERVE ? run.index : run.first, run.count, pos);
+    fill_positions<AXES, kTokens>(P, SERVE && !AXES ? nullptr : positions, X.T, run.first, SERVE ? run.index : run.first, run.count, pos);
     for (int i = threadIdx.x; i < D; i += kThreads) {
         weights[0][i] = P.wq ? P.wq[i] : 1.f;
         weights[1][i] = P.wk ? P.wk[i] : 1.f;
@@ -34,7 +34,7 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
         slot = run.index & ((1 << kv.page_log) - 1);
     }
     __syncthreads();
-    fill_turns(P, pos, run.count, turns);
+    fill_turns<AXES>(P, pos, run.count, turns);
     __syncthreads();
 
     // A page with several users holds another sequence's tokens, too: a reserve would have given the new ones a page of their own.  (Looked at where keys are written.)
@@ -116,11 +116,11 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
 // costs registers (8000 fp32 tokens of 20 heads, d = 128, forward and backward: 92.2 us with LONG, 89.9 without).
 constexpr int kRunsEach = 4, kChain = 64;
 
-template <typename IO, int D, bool LONG>
+template <typename IO, int D, bool LONG, bool AXES>
 __global__ __launch_bounds__(kThreads) void k_heads_backward(HeadParams P, HeadRows X, HeadRows Y, const int *positions, uint4 *gq, uint4 *gk, double *partial, bool stream) {
     constexpr int E = IO::E, LANES = D / E, ROWS = kThreads / LANES;
     __shared__ float2 turns[kTokens][kMostHalf];
-    __shared__ int pos[kMostAxes][kTokens];
+    __shared__ int pos[kAxesOf<AXES>][kTokens];
     __shared__ float weights[2][D];
     __shared__ double sums[kThreads / 64][2][D];
     for (int i = threadIdx.x; i < D; i += kThreads) {
@@ -166,9 +166,9 @@ __global__ __launch_bounds__(kThreads) void k_heads_backward(HeadParams P, HeadR
         };
         request(first, rx, ry);                     // on their way while the angles are formed
         __syncthreads();                            // the run before has read `turns`
-        fill_positions<kTokens>(P, positions, X.T, t0, t0, count, pos);
+        fill_positions<AXES, kTokens>(P, positions, X.T, t0, t0, count, pos);
         __syncthreads();
-        fill_turns(P, pos, count, turns);
+        fill_turns<AXES>(P, pos, count, turns);
         __syncthreads();
         Lane<IO, D> L;
         L.set(P, turns[there ? token : 0], -1.f);
@@ -272,7 +272,12 @@ hipError_t load_kernels_heads() {
 
 hipError_t launch_heads_forward(const spectre_heads &P, int io, const HeadRows &x, const int *positions, void *q_out, void *k_out, hipStream_t st) {
     const int blocks = (x.T + kTokens - 1) / kTokens;
-#define CALL(IO, D) k_heads<IO, D, false><<<dim3(blocks, head_parts(blocks)), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, (uint4 *)k_out, KvView{}, nullptr, nullptr, 0, streams(x, P.d, io))
+    auto launch = [&](auto kernel) {
+        kernel<<<dim3(blocks, head_parts(blocks)), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, (uint4 *)k_out, KvView{}, nullptr, nullptr, 0, streams(x, P.d, io));
+    };
+#define CALL(IO, D)                                                  \
+    if (P.axes > 1 && positions) launch(k_heads<IO, D, false, true>);             \
+    else launch(k_heads<IO, D, false, false>)
     SPECTRE_HEADS_DISPATCH(CALL)
 #undef CALL
     return hipGetLastError();
@@ -281,7 +286,12 @@ hipError_t launch_heads_forward(const spectre_heads &P, int io, const HeadRows &
 hipError_t launch_heads_append(const spectre_heads &P, int io, const HeadRows &x, const KvView &kv, const int *positions, const int *start, const int *seqs, int B, void *q_out,
                                hipStream_t st) {
     const int blocks = x.T / kTokens + 2 * B;
-#define CALL(IO, D) k_heads<IO, D, true><<<dim3(blocks, head_parts(blocks)), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, nullptr, kv, start, seqs, B, false)
+    auto launch = [&](auto kernel) {
+        kernel<<<dim3(blocks, head_parts(blocks)), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, nullptr, kv, start, seqs, B, false);
+    };
+#define CALL(IO, D)                                                  \
+    if (positions) launch(k_heads<IO, D, true, true>);               \
+    else launch(k_heads<IO, D, true, false>)
     SPECTRE_HEADS_DISPATCH(CALL)
 #undef CALL
     return hipGetLastError();
@@ -298,9 +308,14 @@ hipError_t launch_heads_backward(const spectre_heads &P, int io, const HeadRows 
     const int blocks = heads_backward_blocks(x.T), lanes = P.d / (io == SPECTRE_BF16 ? 8 : 4), step = kThreads / lanes / kTokens;
     const long long runs = blocks ? ((x.T + kTokens - 1) / kTokens + blocks - 1) / blocks : 0;             // of a workgroup
     const bool many = P.wq && runs * ((x.H + x.Hkv + step - 1) / step) >= 2 * kChain;
-#define CALL(IO, D)                                                                                                              \
-    if (blocks && many) k_heads_backward<IO, D, true><<<blocks, kThreads, 0, st>>>(head_params(P), x, dy, positions, (uint4 *)gq, (uint4 *)gk, partial, streams(x, P.d, io)); \
-    else if (blocks) k_heads_backward<IO, D, false><<<blocks, kThreads, 0, st>>>(head_params(P), x, dy, positions, (uint4 *)gq, (uint4 *)gk, partial, streams(x, P.d, io)); \
+    auto launch = [&](auto kernel) {
+        if (blocks) kernel<<<blocks, kThreads, 0, st>>>(head_params(P), x, dy, positions, (uint4 *)gq, (uint4 *)gk, partial, streams(x, P.d, io));
+    };
+#define CALL(IO, D)                                                              \
+    if (P.axes > 1 && positions && many) launch(k_heads_backward<IO, D, true, true>);         \
+    else if (P.axes > 1 && positions) launch(k_heads_backward<IO, D, false, true>);           \
+    else if (many) launch(k_heads_backward<IO, D, true, false>);                 \
+    else launch(k_heads_backward<IO, D, false, false>);                          \
     if (P.wq) k_heads_weights<D><<<2 * D / 8, 256, 0, st>>>(partial, blocks, gwq, gwk)
     SPECTRE_HEADS_DISPATCH(CALL)
 #undef CALL

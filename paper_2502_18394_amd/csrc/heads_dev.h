@@ -57,22 +57,30 @@ inline HeadParams head_params(const spectre_heads &P) {
     return p;
 }
 
-// Positions of a workgroup's `count` tokens from `first` on, from the [axes][T] ones given, or from `from` on one after the other.
-template <int TOKENS>
+// Positions of a workgroup's `count` tokens from `first` on: given, [axes][T], or (null) from `from` on one after the other.  Kernels have AXES where there may be several
+// axes, as forms of their own: with one axis it would cost registers (backward, and with them waves) and 4 % of the time of 19 sequences' turns into pages.
+template <bool AXES, int TOKENS>
 __device__ __forceinline__ void fill_positions(const HeadParams &P, const int *positions, int T, int first, int from, int count, int (*pos)[TOKENS]) {
-    for (int i = threadIdx.x; i < TOKENS * P.axes; i += kThreads) {
-        const int a = i / TOKENS, t = i % TOKENS;
-        if (t < count) pos[a][t] = positions ? positions[(long long)a * T + first + t] : from + t;
+    if constexpr (AXES) {
+        for (int i = threadIdx.x; i < TOKENS * P.axes; i += kThreads) {
+            const int a = i / TOKENS, t = i % TOKENS;
+            if (t < count) pos[a][t] = positions[(long long)a * T + first + t];
+        }
+    } else if (threadIdx.x < count) {
+        pos[0][threadIdx.x] = positions ? positions[first + threadIdx.x] : from + (int)threadIdx.x;
     }
 }
+template <bool AXES>
+constexpr int kAxesOf = AXES ? kMostAxes : 1;
 
 // cos and sin of the angles of a workgroup's tokens, one pair a thread.  The turns pos * f / 2 pi are formed and reduced in 64 bits: a position of
 // 131072 leaves 32 bits with an angle that is wrong in the third digit.
-template <int TOKENS>
+template <bool AXES, int TOKENS>
 __device__ __forceinline__ void fill_turns(const HeadParams &P, const int (*pos)[TOKENS], int count, float2 (*turns)[kMostHalf]) {
     for (int i = threadIdx.x; i < count * P.half; i += kThreads) {
         const int t = i / P.half, f = i - t * P.half;
-        const int a = P.axis ? (int)min((unsigned)P.axis[f], (unsigned)P.axes - 1u) : 0;
+        int a = 0;
+        if constexpr (AXES) a = P.axis ? (int)min((unsigned)P.axis[f], (unsigned)P.axes - 1u) : 0;
         double rev = (double)pos[a][t] * P.freq[f] * 0.15915494309189533577;
         rev -= rint(rev);
         float s, c;

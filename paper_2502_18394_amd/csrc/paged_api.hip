@@ -5,6 +5,7 @@
 #include <cstdint>
 
 #include "internal.h"
+#include "norm.h"
 #include "paged.h"
 
 namespace spectre {
@@ -117,6 +118,24 @@ int check_attend(const spectre_kv *kv, int B, int T, int H, int max_new, int max
     return SPECTRE_OK;
 }
 
+int check_norm(const float *w, int T, int D, float eps, spectre_dtype io, const char *who) {
+    const int rc = check_dtype(io, who);
+    if (rc) return rc;
+    if (T < 0 || D < 1) return fail(SPECTRE_EINVAL, "%s: T below 0, or D below 1", who);
+    if ((long long)D * size_of(io) % 16 || (long long)D * size_of(io) > kNormMostBytes)
+        return fail(SPECTRE_EUNSUPPORTED, "%s: rows of %d channels (multiples of 16 bytes up to %d are supported)", who, D, kNormMostBytes);
+    if (!(eps >= 0.f && std::isfinite(eps))) return fail(SPECTRE_EINVAL, "%s: eps", who);
+    if (w && !aligned(w, 16)) return fail(SPECTRE_EINVAL, "%s: w not 16-byte aligned", who);
+    return SPECTRE_OK;
+}
+
+// `bytes` of an output against the rows of an input, or another output's bytes.
+bool meets(const void *out, size_t bytes, const void *at, size_t span) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(out), b = reinterpret_cast<uintptr_t>(at);
+    return a < b + span && b < a + bytes;
+}
+size_t span_of(const Span &x, int T, int D, spectre_dtype io) { return ((size_t)(T - 1) * x.stride + D) * size_of(io); }
+
 int check_plan(const AttendPlan &p, int B, int H, int max_new, const char *who) {
     return p.fits ? SPECTRE_OK : fail(SPECTRE_EUNSUPPORTED, "%s: %d sequences of %d new tokens, %d heads: more workgroups than a launch has", who, B, max_new, H);
 }
@@ -140,7 +159,7 @@ size_t spectre_kv_bytes(const spectre_kv *kv, int which) {
 }
 
 int spectre_kv_prepare(void) {
-    hipError_t (*const loaders[])() = {load_kernels_heads, load_kernels_pages, load_kernels_attend, load_kernels_append8};
+    hipError_t (*const loaders[])() = {load_kernels_heads, load_kernels_pages, load_kernels_attend, load_kernels_append8, load_kernels_norm};
     for (auto load : loaders) {
         const hipError_t e = load();
         if (e != hipSuccess) return fail_hip(e, "kv_prepare: loading kernels");
@@ -313,6 +332,61 @@ int spectre_kv_attend(const spectre_kv *kv, int layer, const void *q, long long 
     if (p.partial_bytes && (rc = check_ws(ws, ws_bytes, align256(p.partial_bytes + 1), who))) return rc;
     const AttendArgs a = {q, q_stride, start, seqs, B, T, H, window, scale, out, lse};
     return done(launch_attend(kv_view(kv, layer), kv->layers, kv->d, (int)io, a, p, ws, static_cast<hipStream_t>(stream)), who);
+}
+
+int spectre_norm_forward(const void *x, long long x_stride, const void *delta, long long delta_stride, const float *w, int T, int D, float eps, spectre_dtype io, void *sum,
+                         void *y, spectre_dtype y_type, float *scales, void *stream) {
+    const char *who = "norm_forward";
+    int rc = check_norm(w, T, D, eps, io, who);
+    if (rc) return rc;
+    if (y_type != io && y_type != SPECTRE_E4M3) return fail(SPECTRE_EINVAL, "%s: y is neither of the rows' type nor of 8 bits", who);
+    const bool coded = y_type == SPECTRE_E4M3;
+    if (coded && D % kNormGroup) return fail(SPECTRE_EUNSUPPORTED, "%s: %d channels in 8 bits (multiples of %d are supported)", who, D, kNormGroup);
+    if (T == 0) return SPECTRE_OK;
+    if (coded != (scales != nullptr)) return fail(SPECTRE_EINVAL, "%s: scales with y of the rows' type, or none with y of 8 bits", who);
+    if (!delta != !sum) return fail(SPECTRE_EINVAL, "%s: one of delta and sum is null", who);
+    const Span in[2] = {{x, x_stride, 1, "x"}, {delta, delta_stride, 1, "delta"}};
+    const size_t rows = (size_t)T * D;
+    const struct { const void *at; size_t bytes; const char *name; } out[3] = {
+        {y, rows * (coded ? 1 : size_of(io)), "y"}, {sum, rows * size_of(io), "sum"}, {scales, rows / kNormGroup * sizeof(float), "scales"}};
+    if (!y || !aligned(y, 16) || !aligned(sum, 16) || !aligned(scales, 4)) return fail(SPECTRE_EINVAL, "%s: an output is null or not aligned", who);
+    for (int i = 0; i < (delta ? 2 : 1); ++i) {
+        if ((rc = check_rows(in[i], D, io, who))) return rc;
+        for (const auto &o : out)
+            if (o.at && meets(o.at, o.bytes, in[i].at, span_of(in[i], T, D, io))) return fail(SPECTRE_EINVAL, "%s: %s overlaps %s", who, o.name, in[i].name);
+    }
+    for (int i = 0; i < 3; ++i)
+        for (int j = 0; j < i; ++j)
+            if (out[i].at && out[j].at && meets(out[i].at, out[i].bytes, out[j].at, out[j].bytes)) return fail(SPECTRE_EINVAL, "%s: outputs overlap", who);
+    const NormRows n = {x, delta, x_stride, delta_stride, w, eps, T, D};
+    return done(launch_norm(n, (int)io, sum, y, scales, static_cast<hipStream_t>(stream)), who);
+}
+
+size_t spectre_norm_backward_workspace_bytes(int T, int D, spectre_dtype io) {
+    if (check_norm(nullptr, T, D, 0.f, io, "norm_backward")) return 0;
+    return align256((size_t)norm_backward_rows(T, D * size_of(io) / 16) * D * sizeof(float) + 1);
+}
+
+int spectre_norm_backward(const void *dy, long long dy_stride, const void *sum, long long sum_stride, const void *dsum, long long dsum_stride, const float *w, int T, int D,
+                          float eps, spectre_dtype io, void *gx, float *gw, void *ws, size_t ws_bytes, void *stream) {
+    const char *who = "norm_backward";
+    int rc = check_norm(w, T, D, eps, io, who);
+    if (rc) return rc;
+    if (!aligned(gw, 4)) return fail(SPECTRE_EINVAL, "%s: gw not aligned", who);
+    const NormRows n = {sum, nullptr, sum_stride, 0, w, eps, T, D};
+    const NormGrads g = {dy, dsum, dy_stride, dsum_stride};
+    if (T == 0) return gw ? done(launch_norm_backward(n, g, (int)io, gx, gw, nullptr, static_cast<hipStream_t>(stream)), who) : SPECTRE_OK;
+    const Span in[3] = {{dy, dy_stride, 1, "dy"}, {sum, sum_stride, 1, "sum"}, {dsum, dsum_stride, 1, "dsum"}};
+    if (!gx || !aligned(gx, 16)) return fail(SPECTRE_EINVAL, "%s: gx is null or not aligned", who);
+    const size_t bytes = (size_t)T * D * size_of(io);
+    for (int i = 0; i < (dsum ? 3 : 2); ++i) {
+        if ((rc = check_rows(in[i], D, io, who))) return rc;
+        if (meets(gx, bytes, in[i].at, span_of(in[i], T, D, io)) || (gw && meets(gw, D * sizeof(float), in[i].at, span_of(in[i], T, D, io))))
+            return fail(SPECTRE_EINVAL, "%s: an output overlaps %s", who, in[i].name);
+    }
+    if (gw && meets(gx, bytes, gw, D * sizeof(float))) return fail(SPECTRE_EINVAL, "%s: outputs overlap", who);
+    if (gw && (rc = check_ws(ws, ws_bytes, spectre_norm_backward_workspace_bytes(T, D, io), who))) return rc;
+    return done(launch_norm_backward(n, g, (int)io, gx, gw, static_cast<float *>(ws), static_cast<hipStream_t>(stream)), who);
 }
 
 }  // extern "C"
