@@ -8,6 +8,8 @@
 // A workgroup has the new tokens of one block (they are one sequence's), all or some of the heads: queries as in the other types, then two key
 // heads (d = 128: one) at a time: 16 tokens' rows in the threads, their largest magnitudes through the wave and LDS, keys stored eight bytes a lane, values
 // turned in LDS into groups of 16 tokens a channel.
+#include <algorithm>
+
 #include "e4m3.h"
 #include "heads_dev.h"
 
@@ -42,7 +44,8 @@ __device__ __forceinline__ void cut(float (&x)[8], float scale) {
 }
 
 template <int D, bool AXES>
-__global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, const int *positions, uint4 *q_out, KvView kv, const int *start, const int *seqs, int B) {
+__global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, const int *positions, uint4 *q_out, KvView kv, const int *start, const int *seqs, int B,
+                                                       int q_parts) {
     constexpr int TOKENS = kKvBlock, LANES = D / 8, ROWS = kThreads / LANES, HEADS = ROWS / TOKENS, WAVES = LANES * TOKENS / 64;    // key heads at once; waves of each
     constexpr int VROW = D / 4 + D / 16;             // words of a token's coded values in LDS: four tokens on are a quarter or half of the banks on
     __shared__ float2 turns[TOKENS][kMostHalf];
@@ -52,6 +55,7 @@ __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, 
     __shared__ __align__(16) uint32_t coded[HEADS][TOKENS][VROW];
     Run run;
     if (!find_run<TOKENS>(kv, start, seqs, B, X.T, blockIdx.x, &run)) return;
+    const FirstTurn first_angle = first_turn<AXES>(P);
     fill_positions<AXES, TOKENS>(P, AXES ? positions : nullptr, X.T, run.first, run.index, run.count, pos);
     for (int i = threadIdx.x; i < D; i += kThreads) {
         weights[0][i] = P.wq ? P.wq[i] : 1.f;
@@ -60,12 +64,14 @@ __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, 
     const int p = run.index >> kv.page_log, slot = run.index & ((1 << kv.page_log) - 1), had = slot & (TOKENS - 1);       // tokens that the block has already
     const int page = p < kv.M ? kv.table[(long long)run.seq * kv.M + p] : -1;
     __syncthreads();
-    fill_turns<AXES>(P, pos, run.count, turns);
+    fill_turns<AXES, true>(P, first_angle, pos, run.count, turns);
     __syncthreads();
     const bool in_pool = (unsigned)page < (unsigned)kv.P;
     const int users = in_pool ? kv.refs[page] : 0;   // a page with several users holds another sequence's tokens, too
 
-    {   // queries, in the order (head, token), tokens padded to a power of two, so that a thread stays with one token and one group of channels
+    // parts of the heads: the first q_parts have queries, the others key heads; 0: each part has some of both
+    const int q_part = blockIdx.y, q_step = q_parts ? q_parts : gridDim.y, k_part = blockIdx.y - q_parts, k_step = gridDim.y - q_parts;
+    if (q_part < q_step) {   // queries, in the order (head, token), tokens padded to a power of two, so that a thread stays with one token and one group of channels
         int tl = 0;
         while ((1 << tl) < run.count) ++tl;
         const int token = (threadIdx.x / LANES) & ((1 << tl) - 1), first = (threadIdx.x / LANES) >> tl, step = ROWS >> tl;
@@ -75,7 +81,7 @@ __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, 
         const long long t = run.first + token;
         const uint4 *q = reinterpret_cast<const uint4 *>(X.q);
         constexpr int AHEAD = 4;
-        for (int h0 = first + (int)blockIdx.y * AHEAD * step; h0 - first < X.H; h0 += AHEAD * step * (int)gridDim.y) {
+        for (int h0 = first + q_part * AHEAD * step; h0 - first < X.H; h0 += AHEAD * step * q_step) {
             uint4 raw[AHEAD];
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
@@ -91,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, 
             }
         }
     }
-    if (!in_pool) return;
+    if (!in_pool || k_part < 0) return;
     if (users > 1) {
         if (threadIdx.x == 0) atomicOr(&kv.status[0], SPECTRE_KV_SHARED);
         return;
@@ -103,7 +109,7 @@ __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, 
     L.set(P, turns[there ? at - had : 0], 1.f);
     const long long t = run.first + at - had;
     const uint4 *k = reinterpret_cast<const uint4 *>(X.k), *v = reinterpret_cast<const uint4 *>(X.v);
-    for (int h0 = HEADS * blockIdx.y; h0 < X.Hkv; h0 += HEADS * gridDim.y) {
+    for (int h0 = HEADS * k_part; h0 < X.Hkv; h0 += HEADS * k_step) {
         const int h = h0 + sub;
         const bool mine = h < X.Hkv;
         const long long head = (long long)page * X.Hkv + (mine ? h : 0);
@@ -192,8 +198,10 @@ hipError_t load_kernels_append8() {
 
 hipError_t launch_heads_append8(const spectre_heads &P, const HeadRows &x, const KvView &kv, const int *positions, const int *start, const int *seqs, int B, void *q_out,
                                 hipStream_t st) {
-    const int blocks = x.T / kKvBlock + 2 * B, most = 2048 / blocks, parts = most < 1 ? 1 : most > 4 ? 4 : most;
-    auto launch = [&](auto kernel) { kernel<<<dim3(blocks, parts), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, kv, start, seqs, B); };
+    // few blocks: up to four workgroups for a block's queries and four for its key heads; many: one for both
+    const int blocks = x.T / kKvBlock + 2 * B, most = 2048 / blocks, heads = P.d == 64 ? 2 : 1;
+    const int q_parts = most < 2 ? 0 : most > 4 ? 4 : most, k_parts = most < 2 ? 1 : std::min(q_parts, (x.Hkv + heads - 1) / heads);
+    auto launch = [&](auto kernel) { kernel<<<dim3(blocks, q_parts + k_parts), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, kv, start, seqs, B, q_parts); };
     if (P.d == 64) positions ? launch(k_append8<64, true>) : launch(k_append8<64, false>);
     else positions ? launch(k_append8<128, true>) : launch(k_append8<128, false>);
     return hipGetLastError();

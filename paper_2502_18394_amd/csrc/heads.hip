@@ -22,6 +22,7 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
     __shared__ float weights[2][D];
     Run run{(int)blockIdx.x * kTokens, min(kTokens, X.T - (int)blockIdx.x * kTokens), 0, 0};
     if (SERVE && !find_run<kTokens>(kv, start, seqs, B, X.T, blockIdx.x, &run)) return;
+    const FirstTurn first_angle = first_turn<AXES>(P);
     fill_positions<AXES, kTokens>(P, SERVE && !AXES ? nullptr : positions, X.T, run.first, SERVE ? run.index : run.first, run.count, pos);
     for (int i = threadIdx.x; i < D; i += kThreads) {
         weights[0][i] = P.wq ? P.wq[i] : 1.f;
@@ -34,7 +35,7 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
         slot = run.index & ((1 << kv.page_log) - 1);
     }
     __syncthreads();
-    fill_turns<AXES>(P, pos, run.count, turns);
+    fill_turns<AXES, true>(P, first_angle, pos, run.count, turns);
     __syncthreads();
 
     // A page with several users holds another sequence's tokens, too: a reserve would have given the new ones a page of their own.  (Looked at where keys are written.)
@@ -168,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void k_heads_backward(HeadParams P, HeadR
         __syncthreads();                            // the run before has read `turns`
         fill_positions<AXES, kTokens>(P, positions, X.T, t0, t0, count, pos);
         __syncthreads();
-        fill_turns<AXES>(P, pos, count, turns);
+        fill_turns<AXES, false>(P, FirstTurn{}, pos, count, turns);
         __syncthreads();
         Lane<IO, D> L;
         L.set(P, turns[there ? token : 0], -1.f);
