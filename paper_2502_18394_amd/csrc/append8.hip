@@ -141,6 +141,7 @@ __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, 
             most[wave][0] = mk;
             most[wave][1] = mv;
         }
+        asm volatile("s_waitcnt vmcnt(0)" : "+v"(was.x), "+v"(was.y) : : "memory");        // everybody has the block's scales before one thread writes the new ones
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
