@@ -596,12 +596,19 @@ class Rope:
 
 def _heads(d, rope, wq, wk, eps):
     """The C parameters; rope None: no rotation, wq and wk None: no norm."""
-    for w, name in ((wq, "wq"), (wk, "wk")):
-        if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,)):
-            raise ValueError(f"{name} must be float32 [{d}]")
-    return HeadsC(d, rope.rot if rope else 0, int(rope.interleaved) if rope else 0, eps, rope.inv_freq.data_ptr() if rope else None,
-                  None if wq is None else _ptr(wq, "wq"), None if wk is None else _ptr(wk, "wk"), rope.axes if rope else 1,
-                  rope.axis.data_ptr() if rope and rope.axis is not None else None)
+    wq, wk = _vector(wq, "wq", d), _vector(wk, "wk", d)
+    if rope is None:
+        return HeadsC(d, 0, 0, eps, None, wq, wk, 1, None)
+    return HeadsC(d, rope.rot, rope.interleaved, eps, rope.inv_freq.data_ptr(), wq, wk, rope.axes, None if rope.axis is None else rope.axis.data_ptr())
+
+
+def _vector(w, name, d):
+    """Address of weights float32 [d], None of none."""
+    if w is None:
+        return None
+    if w.dtype != torch.float32 or w.shape != (d,):
+        raise ValueError(f"{name} must be float32 [{d}]")
+    return _ptr(w, name)
 
 
 def _positions(positions, rope, T):
@@ -633,10 +640,12 @@ def qk_norm_rotate(q, k, positions=None, rope=None, wq=None, wk=None, eps=1e-6, 
     P = _heads(d, rope, wq, wk, eps)
     if q_out is None:
         q_out = _like(q, stream)
+    else:
+        _same(q_out, q, "q_out")
     if k_out is None:
         k_out = _like(k, stream)
-    _same(q_out, q, "q_out")
-    _same(k_out, k, "k_out")
+    else:
+        _same(k_out, k, "k_out")
     _check(lib().spectre_heads_forward(ctypes.byref(P), qa, qs, ka, ks, _positions(positions, rope, T), T, H, Hkv, io,
                                        _ptr(q_out, "q_out"), _ptr(k_out, "k_out"), _now(stream)))
     return q_out, k_out
@@ -660,10 +669,13 @@ def qk_norm_rotate_backward(dq, dk, q, k, positions=None, rope=None, wq=None, wk
     gq, gk = _like(q, stream), _like(k, stream)
     gw, wsp, wsn = (None, None), None, 0
     if wq is not None:
-        gw = _new((2, d), torch.float32, q.device, stream).unbind(0)
+        gw = _like(wq, stream), _like(wk, stream)
         if ws is None:
-            ws = _new((lib().spectre_heads_backward_workspace_bytes(T, d) + 256,), torch.uint8, q.device, stream)
-        wsp, wsn = _given(ws)
+            wsn = lib().spectre_heads_backward_workspace_bytes(T, d)
+            ws = _new((wsn,), torch.uint8, q.device, stream)          # the allocator's memory is aligned
+            wsp = ws.data_ptr()
+        else:
+            wsp, wsn = _given(ws)
     _check(lib().spectre_heads_backward(ctypes.byref(P), *rows[0], *rows[1], *rows[2], *rows[3],
                                         _positions(positions, rope, T), T, H, Hkv, io, gq.data_ptr(), gk.data_ptr(),
                                         None if gw[0] is None else gw[0].data_ptr(), None if gw[1] is None else gw[1].data_ptr(), wsp, wsn,
@@ -671,24 +683,16 @@ def qk_norm_rotate_backward(dq, dk, q, k, positions=None, rope=None, wq=None, wk
     return gq, gk, gw[0], gw[1]
 
 
-def _matrix(t, name, like=None):
+def _matrix(t, name, T, D, dtype):
     """(address, elements from row to row) of rows [T, D] whose channels are adjacent."""
-    if not t.is_cuda or t.dim() != 2:
-        raise ValueError(f"{name} must be a device tensor [T, D]")
-    if like is not None:
-        _same(t, like, name)
+    if not t.is_cuda or t.shape != (T, D):
+        raise ValueError(f"{name} must be a device tensor [{T}, {D}]")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, not {dtype}")
     st, sc = t.stride()
-    if sc != 1 and t.shape[1] > 1:
+    if sc != 1 and D > 1:
         raise ValueError(f"{name} must have adjacent channels")
-    return t.data_ptr(), st if t.shape[0] > 1 else t.shape[1]
-
-
-def _norm_weight(weight, D):
-    if weight is None:
-        return None
-    if weight.dtype != torch.float32 or tuple(weight.shape) != (D,):
-        raise ValueError(f"weight must be float32 [{D}]")
-    return _ptr(weight, "weight")
+    return t.data_ptr(), st if T > 1 else D
 
 
 NORM_GROUP = 128
@@ -699,11 +703,11 @@ def add_norm(x, weight=None, delta=None, eps=1e-6, dtype=None, sum_out=None, out
     apart; weight float32 [D] (None: ones).  Returns (sum, y), the sum in x's dtype (x itself without delta), y in x's dtype, or with dtype=torch.float8_e4m3fn
     (sum, codes, scales): a float32 scale for each 128 channels, scales [T, D / 128], and what is meant is code * scale."""
     T, D = x.shape
-    io, coded = _dtype_code(x), dtype == torch.float8_e4m3fn
-    if dtype is not None and not coded and dtype != x.dtype:
-        raise TypeError(f"the norm of {x.dtype} rows is {x.dtype} or float8_e4m3fn, not {dtype}")
-    xa, xs = _matrix(x, "x")
-    da, ds = (None, 0) if delta is None else _matrix(delta, "delta", x)
+    io, kind, coded = _dtype_code(x), x.dtype, dtype == torch.float8_e4m3fn
+    if dtype is not None and not coded and dtype != kind:
+        raise TypeError(f"the norm of {kind} rows is {kind} or float8_e4m3fn, not {dtype}")
+    xa, xs = _matrix(x, "x", T, D, kind)
+    da, ds = (None, 0) if delta is None else _matrix(delta, "delta", T, D, kind)
     if delta is None:
         if sum_out is not None:
             raise ValueError("without delta there is no sum")
@@ -728,7 +732,7 @@ def add_norm(x, weight=None, delta=None, eps=1e-6, dtype=None, sum_out=None, out
         out = _like(x, stream)
     else:
         _same(out, x, "out")
-    _check(lib().spectre_norm_forward(xa, xs, da, ds, _norm_weight(weight, D), T, D, eps, io, None if delta is None else _ptr(sum_out, "sum_out"), _ptr(out, "out"),
+    _check(lib().spectre_norm_forward(xa, xs, da, ds, _vector(weight, "weight", D), T, D, eps, io, None if delta is None else _ptr(sum_out, "sum_out"), _ptr(out, "out"),
                                       E4M3 if coded else io, _ptr(scales, "scales") if coded else None, _now(stream)))
     total = x if delta is None else sum_out
     return (total, out, scales) if coded else (total, out)
@@ -739,17 +743,20 @@ def add_norm_backward(dy, total, weight=None, dsum=None, eps=1e-6, ws=None, stre
     dsum: the gradient of that sum where it goes on as a residual (None: nothing comes from there).  Returns (gx, gw): gx is the gradient of x and of delta, gw float32
     [D], None without a weight."""
     T, D = total.shape
-    io = _dtype_code(total)
-    ta, ts = _matrix(total, "total")
-    ya, ys = _matrix(dy, "dy", total)
-    da, ds = (None, 0) if dsum is None else _matrix(dsum, "dsum", total)
-    w = _norm_weight(weight, D)
+    io, kind = _dtype_code(total), total.dtype
+    ta, ts = _matrix(total, "total", T, D, kind)
+    ya, ys = _matrix(dy, "dy", T, D, kind)
+    da, ds = (None, 0) if dsum is None else _matrix(dsum, "dsum", T, D, kind)
+    w = _vector(weight, "weight", D)
     gx, gw, wsp, wsn = _like(total, stream), None, None, 0
     if weight is not None:
-        gw = _new((D,), torch.float32, total.device, stream)
+        gw = _like(weight, stream)
         if ws is None:
-            ws = _new((lib().spectre_norm_backward_workspace_bytes(T, D, io) + 256,), torch.uint8, total.device, stream)
-        wsp, wsn = _given(ws)
+            wsn = lib().spectre_norm_backward_workspace_bytes(T, D, io)
+            ws = _new((wsn,), torch.uint8, total.device, stream)      # the allocator's memory is aligned
+            wsp = ws.data_ptr()
+        else:
+            wsp, wsn = _given(ws)
     _check(lib().spectre_norm_backward(ya, ys, ta, ts, da, ds, w, T, D, eps, io, _ptr(gx, "gx"), None if gw is None else _ptr(gw, "gw"), wsp, wsn, _now(stream)))
     return gx, gw
 
