@@ -43,7 +43,7 @@ __device__ __forceinline__ void cut(float (&x)[8], float scale) {
         if (fabsf(x[e]) > kCut && fabsf(x[e]) < INFINITY) x[e] = copysignf(kCut, x[e]);
 }
 
-template <int D, bool AXES>
+template <int D, bool AXES, int TURN>
 __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, const int *positions, uint4 *q_out, KvView kv, const int *start, const int *seqs, int B,
                                                        int q_parts) {
     constexpr int TOKENS = kKvBlock, LANES = D / 8, ROWS = kThreads / LANES, HEADS = ROWS / TOKENS, WAVES = LANES * TOKENS / 64;    // key heads at once; waves of each
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, 
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) {
                 const int h = h0 + i * step;
-                const uint4 o = head_row<Bf16Group, D>(P, L, P.wq ? weights[0] : nullptr, raw[i]);
+                const uint4 o = head_row<Bf16Group, D, TURN>(P, L, P.wq ? weights[0] : nullptr, raw[i]);
                 if (there && h < X.H) q_out[(t * X.H + h) * LANES + L.lane] = o;
             }
         }
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, 
             if (at < had && mine) old = *keys;
         }
         float x[8], y[8];
-        head_channels<Bf16Group, D>(P, L, P.wq ? weights[1] : nullptr, kr, x);
+        head_channels<Bf16Group, D, TURN>(P, L, P.wq ? weights[1] : nullptr, kr, x);
         Bf16Group::unpack(vr, y);
         float mk = 0.f, mv = 0.f;
 #pragma unroll
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(kThreads) void k_append8(HeadParams P, HeadRows X, 
 
 hipError_t load_kernels_append8() {
     hipFuncAttributes a;
-    return hipFuncGetAttributes(&a, reinterpret_cast<const void *>(k_append8<64, false>));
+    return hipFuncGetAttributes(&a, reinterpret_cast<const void *>(k_append8<64, false, kHalves>));
 }
 
 hipError_t launch_heads_append8(const spectre_heads &P, const HeadRows &x, const KvView &kv, const int *positions, const int *start, const int *seqs, int B, void *q_out,
@@ -203,8 +203,11 @@ hipError_t launch_heads_append8(const spectre_heads &P, const HeadRows &x, const
     const int blocks = x.T / kKvBlock + 2 * B, most = 2048 / blocks, heads = P.d == 64 ? 2 : 1;
     const int q_parts = most < 2 ? 0 : most > 4 ? 4 : most, k_parts = most < 2 ? 1 : std::min(q_parts, (x.Hkv + heads - 1) / heads);
     auto launch = [&](auto kernel) { kernel<<<dim3(blocks, q_parts + k_parts), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, kv, start, seqs, B, q_parts); };
-    if (P.d == 64) positions ? launch(k_append8<64, true>) : launch(k_append8<64, false>);
-    else positions ? launch(k_append8<128, true>) : launch(k_append8<128, false>);
+    const int turn = turn_of(P);
+#define CALL(D, AXES) (turn == kHalves ? launch(k_append8<D, AXES, kHalves>) : turn == kPairs ? launch(k_append8<D, AXES, kPairs>) : launch(k_append8<D, AXES, kAnyTurn>))
+    if (P.d == 64) positions ? CALL(64, true) : CALL(64, false);
+    else positions ? CALL(128, true) : CALL(128, false);
+#undef CALL
     return hipGetLastError();
 }
 

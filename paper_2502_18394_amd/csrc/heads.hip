@@ -13,7 +13,7 @@ namespace {
 
 constexpr int kTokens = 8;                      // a workgroup: one 16-byte group of V pages, two in fp32
 
-template <typename IO, int D, bool SERVE, bool AXES>
+template <typename IO, int D, bool SERVE, bool AXES, int TURN>
 __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, const int *positions, uint4 *q_out, uint4 *k_out, KvView kv, const int *start, const int *seqs,
                                                     int B, bool stream) {
     constexpr int E = IO::E, LANES = D / E, ROWS = kThreads / LANES;
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
         for (int i = 0; i < AHEAD; ++i) {
             const int h = h0 + i * step;
             const bool key = h >= X.H;
-            const uint4 o = head_row<IO, D>(P, L, P.wq ? weights[key] : nullptr, raw[i]);
+            const uint4 o = head_row<IO, D, TURN>(P, L, P.wq ? weights[key] : nullptr, raw[i]);
             if (!there || h >= heads) continue;
             if (!key) put(&q_out[(t * X.H + h) * LANES + L.lane], o, stream);
             else if (!SERVE) put(&k_out[(t * X.Hkv + h - X.H) * LANES + L.lane], o, stream);
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(kThreads) void k_heads(HeadParams P, HeadRows X, co
 // costs registers (8000 fp32 tokens of 20 heads, d = 128, forward and backward: 92.2 us with LONG, 89.9 without).
 constexpr int kRunsEach = 4, kChain = 64;
 
-template <typename IO, int D, bool LONG, bool AXES>
+template <typename IO, int D, bool LONG, bool AXES, int TURN>
 __global__ __launch_bounds__(kThreads) void k_heads_backward(HeadParams P, HeadRows X, HeadRows Y, const int *positions, uint4 *gq, uint4 *gk, double *partial, bool stream) {
     constexpr int E = IO::E, LANES = D / E, ROWS = kThreads / LANES;
     __shared__ float2 turns[kTokens][kMostHalf];
@@ -180,10 +180,12 @@ __global__ __launch_bounds__(kThreads) void k_heads_backward(HeadParams P, HeadR
                 const bool key = h >= X.H;
                 float y[E], z[E], g[E], x[E];
                 IO::unpack(ry, y);
-                if (P.half) {
-                    const uint4 other = P.interleaved ? ry : shuffle(ry, L.partner);
-                    IO::unpack(other, z);
-                    L.turn(P, y, z, g);
+                if (TURN != kAnyTurn || P.half) {
+                    if constexpr (TURN != kPairs) {
+                        const uint4 other = TURN == kAnyTurn && P.interleaved ? ry : shuffle(ry, L.partner);
+                        IO::unpack(other, z);
+                    }
+                    L.template turn<TURN>(P, y, z, g);
                 } else {
 #pragma unroll
                     for (int e = 0; e < E; ++e) g[e] = y[e];
@@ -265,6 +267,10 @@ hipError_t load_kernels_heads() {
     return hipFuncGetAttributes(&a, reinterpret_cast<const void *>(k_heads_weights<64>));
 }
 
+#define BY_TURN(LAUNCH, KERNEL, ...)                                                   \
+    (turn_of(P) == kHalves  ? LAUNCH(KERNEL<__VA_ARGS__, kHalves>)                     \
+     : turn_of(P) == kPairs ? LAUNCH(KERNEL<__VA_ARGS__, kPairs>)                      \
+                            : LAUNCH(KERNEL<__VA_ARGS__, kAnyTurn>))
 #define SPECTRE_HEADS_DISPATCH(CALL)                                  \
     if (io == SPECTRE_BF16 && P.d == 64) { CALL(Bf16Group, 64); }     \
     else if (io == SPECTRE_BF16) { CALL(Bf16Group, 128); }            \
@@ -277,8 +283,8 @@ hipError_t launch_heads_forward(const spectre_heads &P, int io, const HeadRows &
         kernel<<<dim3(blocks, head_parts(blocks)), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, (uint4 *)k_out, KvView{}, nullptr, nullptr, 0, streams(x, P.d, io));
     };
 #define CALL(IO, D)                                                  \
-    if (P.axes > 1 && positions) launch(k_heads<IO, D, false, true>);             \
-    else launch(k_heads<IO, D, false, false>)
+    if (P.axes > 1 && positions) BY_TURN(launch, k_heads, IO, D, false, true); \
+    else BY_TURN(launch, k_heads, IO, D, false, false)
     SPECTRE_HEADS_DISPATCH(CALL)
 #undef CALL
     return hipGetLastError();
@@ -291,8 +297,8 @@ hipError_t launch_heads_append(const spectre_heads &P, int io, const HeadRows &x
         kernel<<<dim3(blocks, head_parts(blocks)), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, nullptr, kv, start, seqs, B, false);
     };
 #define CALL(IO, D)                                                  \
-    if (positions) launch(k_heads<IO, D, true, true>);               \
-    else launch(k_heads<IO, D, true, false>)
+    if (positions) BY_TURN(launch, k_heads, IO, D, true, true);      \
+    else BY_TURN(launch, k_heads, IO, D, true, false)
     SPECTRE_HEADS_DISPATCH(CALL)
 #undef CALL
     return hipGetLastError();
@@ -313,10 +319,10 @@ hipError_t launch_heads_backward(const spectre_heads &P, int io, const HeadRows 
         if (blocks) kernel<<<blocks, kThreads, 0, st>>>(head_params(P), x, dy, positions, (uint4 *)gq, (uint4 *)gk, partial, streams(x, P.d, io));
     };
 #define CALL(IO, D)                                                              \
-    if (P.axes > 1 && positions && many) launch(k_heads_backward<IO, D, true, true>);         \
-    else if (P.axes > 1 && positions) launch(k_heads_backward<IO, D, false, true>);           \
-    else if (many) launch(k_heads_backward<IO, D, true, false>);                 \
-    else launch(k_heads_backward<IO, D, false, false>);                          \
+    if (P.axes > 1 && positions && many) BY_TURN(launch, k_heads_backward, IO, D, true, true);  \
+    else if (P.axes > 1 && positions) BY_TURN(launch, k_heads_backward, IO, D, false, true);    \
+    else if (many) BY_TURN(launch, k_heads_backward, IO, D, true, false);        \
+    else BY_TURN(launch, k_heads_backward, IO, D, false, false);                 \
     if (P.wq) k_heads_weights<D><<<2 * D / 8, 256, 0, st>>>(partial, blocks, gwq, gwk)
     SPECTRE_HEADS_DISPATCH(CALL)
 #undef CALL

@@ -108,6 +108,18 @@ __device__ __forceinline__ void fill_turns(const HeadParams &P, FirstTurn first,
     }
 }
 
+// How rows are turned.  Whole rows have forms of their own, in which nothing is chosen element by element and adjacent pairs do without their partners' lane; the vector
+// unit works four fifths of these kernels' time.
+enum { kAnyTurn, kHalves, kPairs };
+inline int turn_of(const spectre_heads &P) { return P.rot != P.d ? kAnyTurn : P.interleaved ? kPairs : kHalves; }
+
+// a c + b s with one rounding of b s, whatever form it is compiled in: all give the same bits.
+__device__ __forceinline__ float turned_sum(float a, float c, float b, float s) {
+#pragma clang fp contract(off)
+    const float product = b * s;
+    return fmaf(a, c, product);
+}
+
 // What a lane needs of its E channels, the same for every row it visits: its pairs' cos and sin (sin negated in the first half of split pairs)
 // and the lane that holds the partners.
 template <typename IO, int D>
@@ -138,11 +150,13 @@ struct Lane {
         }
     }
     // y of this lane's channels, z of their partners'.  Channels that are not turned (whole lanes of them) pass through: a zero times an infinite neighbour is NaN.
+    template <int TURN>
     __device__ __forceinline__ void turn(const HeadParams &P, const float (&y)[E], const float (&z)[E], float (&o)[E]) const {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float t = y[e] * c[e] + (P.interleaved ? y[e ^ 1] : z[e]) * s[e];
-            o[e] = turned ? t : y[e];
+            const float other = TURN == kPairs ? y[e ^ 1] : TURN == kHalves ? z[e] : P.interleaved ? y[e ^ 1] : z[e];
+            const float t = turned_sum(y[e], c[e], other, s[e]);
+            o[e] = TURN != kAnyTurn || turned ? t : y[e];
         }
     }
 };
@@ -180,13 +194,16 @@ __device__ __forceinline__ uint4 shuffle(uint4 g, int lane) {
 }
 
 // One row's norm and rotation: this lane's channels.
-template <typename IO, int D>
+template <typename IO, int D, int TURN>
 __device__ __forceinline__ void head_channels(const HeadParams &P, const Lane<IO, D> &L, const float *w, uint4 raw, float (&o)[IO::E]) {
     constexpr int E = IO::E;
     float x[E], z[E];
     IO::unpack(raw, x);
-    const uint4 other = (P.half && !P.interleaved) ? shuffle(raw, L.partner) : raw;
-    IO::unpack(other, z);
+    constexpr bool MATE = TURN != kPairs;             // a partner's channels are looked at
+    if constexpr (MATE) {
+        const uint4 other = TURN == kHalves || (P.half && !P.interleaved) ? shuffle(raw, L.partner) : raw;
+        IO::unpack(other, z);
+    }
     if (w) {
         float sq = 0.f;
 #pragma unroll
@@ -196,18 +213,18 @@ __device__ __forceinline__ void head_channels(const HeadParams &P, const Lane<IO
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             x[e] = x[e] * r * w[base + e];
-            z[e] = z[e] * r * w[mate + e];
+            if (MATE) z[e] = z[e] * r * w[mate + e];
         }
     }
-    if (P.half) L.turn(P, x, z, o);
+    if (TURN != kAnyTurn || P.half) L.template turn<TURN>(P, x, z, o);
     else
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] = x[e];
 }
-template <typename IO, int D>
+template <typename IO, int D, int TURN>
 __device__ __forceinline__ uint4 head_row(const HeadParams &P, const Lane<IO, D> &L, const float *w, uint4 raw) {
     float o[IO::E];
-    head_channels<IO, D>(P, L, w, raw, o);
+    head_channels<IO, D, TURN>(P, L, w, raw, o);
     return IO::pack(o);
 }
 
