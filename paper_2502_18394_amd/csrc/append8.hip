@@ -199,9 +199,11 @@ hipError_t load_kernels_append8() {
 
 hipError_t launch_heads_append8(const spectre_heads &P, const HeadRows &x, const KvView &kv, const int *positions, const int *start, const int *seqs, int B, void *q_out,
                                 hipStream_t st) {
-    // few blocks: up to four workgroups for a block's queries and four for its key heads; many: one for both
-    const int blocks = x.T / kKvBlock + 2 * B, most = 2048 / blocks, heads = P.d == 64 ? 2 : 1;
-    const int q_parts = most < 2 ? 0 : most > 4 ? 4 : most, k_parts = most < 2 ? 1 : std::min(q_parts, (x.Hkv + heads - 1) / heads);
+    // As many workgroups as run at once, no more: each forms the angles of its tokens.  One or two for a block's queries and up to four for its key heads, or one for all.
+    // 19 sequences' turns (202 blocks), with 8 parts 13.3 us, 6 (two and four) 11.4, 5 (one and four) 12.5; a prompt of 4096 (258 blocks) 15.7, 15.1 and 13.2.
+    // Of the blocks of single tokens half are there.
+    const int blocks = x.T / kKvBlock + 2 * B, heads = P.d == 64 ? 2 : 1, parts = std::min(6, 1300 / std::min(blocks, x.T));
+    const int q_parts = parts < 2 ? 0 : parts < 6 ? 1 : 2, k_parts = std::max(1, std::min(parts - q_parts, (x.Hkv + heads - 1) / heads));
     auto launch = [&](auto kernel) { kernel<<<dim3(blocks, q_parts + k_parts), kThreads, 0, st>>>(head_params(P), x, positions, (uint4 *)q_out, kv, start, seqs, B, q_parts); };
     const int turn = turn_of(P);
 #define CALL(D, AXES) (turn == kHalves ? launch(k_append8<D, AXES, kHalves>) : turn == kPairs ? launch(k_append8<D, AXES, kPairs>) : launch(k_append8<D, AXES, kAnyTurn>))
