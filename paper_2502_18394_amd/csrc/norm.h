@@ -5,7 +5,7 @@
 namespace spectre {
 
 constexpr int kNormGroup = 128;                    // channels of a scale
-constexpr int kNormChain = 128;                    // rows whose gradients a thread adds in 32 bits, at most
+constexpr int kNormChain = 128;                    // rows whose gradients a workgroup adds in 32 bits, at most
 constexpr int kNormMostBytes = 32768;              // of a row
 
 struct NormRows {                                  // row t at x + t * x_stride (elements)
@@ -22,7 +22,7 @@ struct NormGrads {
 
 hipError_t load_kernels_norm();
 hipError_t launch_norm(const NormRows &n, int io, void *sum, void *y, float *scales, hipStream_t st);     // scales: y in 8 bits
-int norm_backward_rows(int T, int groups);
+int norm_backward_blocks(int T, int groups);             // as many rows of partial sums
 hipError_t launch_norm_backward(const NormRows &n, const NormGrads &g, int io, void *gx, float *gw, float *partial, hipStream_t st);
 
 }  // namespace spectre

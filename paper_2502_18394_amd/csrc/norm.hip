@@ -145,7 +145,7 @@ __global__ __launch_bounds__((kGroupThreads<LANES>)) void k_norm(NormRows N, uin
     }
 }
 
-// A thread's sums of the weights' gradient, of the rows that its row of threads went through, are in 32 bits (at most kNormChain rows); k_norm_weights adds the others in 64.
+// A workgroup's sums of the weights' gradient are in 32 bits (at most kNormChain rows); k_norm_weights adds the workgroups' in 64.
 template <typename IO, int LANES, int CHUNKS, bool WEIGHTS>
 __global__ __launch_bounds__((kGroupThreads<LANES>)) void k_norm_backward(NormRows N, NormGrads G, uint4 *gx, float *partial, bool stream) {
     constexpr int E = IO::E, ROWS = kGroupThreads<LANES> / LANES;
@@ -213,10 +213,27 @@ __global__ __launch_bounds__((kGroupThreads<LANES>)) void k_norm_backward(NormRo
         }
     }
     if constexpr (WEIGHTS) {
+        if constexpr (ROWS > 1) {                                              // the workgroup's waves, in their order
+            __shared__ float others[ROWS - 1][LANES * CHUNKS * E];
+            const int slot = threadIdx.x / LANES;
+            if (slot > 0)
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) others[slot - 1][(c * E + e) * LANES + lane] = gw[c][e];
+            __syncthreads();
+            if (slot > 0) return;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+#pragma unroll
+                    for (int o = 0; o < ROWS - 1; ++o) gw[c][e] += others[o][(c * E + e) * LANES + lane];
+        }
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
             if (lane + LANES * c < groups) {
-                float *to = partial + ((long long)blockIdx.x * ROWS + threadIdx.x / LANES) * N.D + (long long)(lane + LANES * c) * E;
+                float *to = partial + (long long)blockIdx.x * N.D + (long long)(lane + LANES * c) * E;
 #pragma unroll
                 for (int e = 0; e < E; e += 4) *reinterpret_cast<float4 *>(to + e) = make_float4(gw[c][e], gw[c][e + 1], gw[c][e + 2], gw[c][e + 3]);
             }
@@ -272,15 +289,16 @@ hipError_t launch_norm(const NormRows &n, int io, void *sum, void *y, float *sca
     return hipGetLastError();
 }
 
-// Rows of threads that go through the rows of a batch: 16 waves a compute unit, more where each would have more than kNormChain rows.
-int norm_backward_rows(int T, int groups) {
+// 16 waves a compute unit, more workgroups where each would have more than kNormChain rows.  (Half of them: 16384 rows of 2048 bf16 channels, forward and backward, 105.6
+// instead of 108.2 us, but 5000 of 8192 151 instead of 124.)
+int norm_backward_blocks(int T, int groups) {
     const int slots = row_slots(groups);
-    const long long most = std::max(1024ll * 256 / group_threads(groups), ((long long)T + (long long)kNormChain * slots - 1) / ((long long)kNormChain * slots));
-    return slots * (int)std::min<long long>(((long long)T + slots - 1) / slots, most);
+    const long long most = std::max(1024ll * 256 / group_threads(groups), ((long long)T + kNormChain - 1) / kNormChain);
+    return (int)std::min<long long>(((long long)T + slots - 1) / slots, most);
 }
 
 hipError_t launch_norm_backward(const NormRows &n, const NormGrads &g, int io, void *gx, float *gw, float *partial, hipStream_t st) {
-    const int size = io == SPECTRE_BF16 ? 2 : 4, groups = n.D * size / 16, rows = norm_backward_rows(n.T, groups), blocks = rows / row_slots(groups);
+    const int size = io == SPECTRE_BF16 ? 2 : 4, groups = n.D * size / 16, blocks = norm_backward_blocks(n.T, groups);
     const bool stream = (size_t)n.T * n.D * size > kL2Bytes;
     auto launch = [&](auto kernel) { kernel<<<blocks, group_threads(groups), 0, st>>>(n, g, (uint4 *)gx, partial, stream); };
 #define CALL(IO, LANES, CHUNKS) (gw ? launch(k_norm_backward<IO, LANES, CHUNKS, true>) : launch(k_norm_backward<IO, LANES, CHUNKS, false>))
@@ -289,7 +307,7 @@ hipError_t launch_norm_backward(const NormRows &n, const NormGrads &g, int io, v
         else { SPECTRE_NORM_CHUNKS(F32Group, CALL); }
     }
 #undef CALL
-    if (gw) k_norm_weights<<<(n.D + 15) / 16, 256, 0, st>>>(partial, n.T > 0 ? rows : 0, n.D, gw);
+    if (gw) k_norm_weights<<<(n.D + 15) / 16, 256, 0, st>>>(partial, n.T > 0 ? blocks : 0, n.D, gw);
     return hipGetLastError();
 }
 

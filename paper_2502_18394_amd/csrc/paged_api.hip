@@ -364,7 +364,7 @@ int spectre_norm_forward(const void *x, long long x_stride, const void *delta, l
 
 size_t spectre_norm_backward_workspace_bytes(int T, int D, spectre_dtype io) {
     if (check_norm(nullptr, T, D, 0.f, io, "norm_backward")) return 0;
-    return align256((size_t)norm_backward_rows(T, D * size_of(io) / 16) * D * sizeof(float) + 1);
+    return align256((size_t)norm_backward_blocks(T, D * size_of(io) / 16) * D * sizeof(float) + 1);
 }
 
 int spectre_norm_backward(const void *dy, long long dy_stride, const void *sum, long long sum_stride, const void *dsum, long long dsum_stride, const float *w, int T, int D,
