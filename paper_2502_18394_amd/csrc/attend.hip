@@ -335,10 +335,11 @@ __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 
 // softmax within a wave (17 % slower, d = 128 1 % faster), two tiles a barrier (3 % slower), raised priority around the products (no difference), tiles through registers (4 % slower).
 template <typename IO, int D>
 constexpr int kTileGroups = IO::kTileKeys * D / IO::E;
-// Groups of a tile as they lie in pages of 8 bits, on their way.
+// Groups of a tile as they lie in pages of 8 bits, on their way.  (d = 64: in registers the queries went to memory and were read again for every tile, which waited for all loads on
+// their way: 1006 instead of 630 us.)
 template <typename IO, int D>
 constexpr int kRawGroups = IO::kCoded && D == 64 ? 8 * D + 8 * D / 4 : 0;    // and their scales
-// Groups of queries that registers have no room for beside those tiles.
+// Groups of queries that registers have no room for beside those tiles: three of four (with two 709 us traced, with three 683, with none 737).
 template <typename IO, int D, int WAVES>
 constexpr int kQueryGroups = kRawGroups<IO, D> && WAVES == 8 ? 3 * 64 * WAVES : 0;
 struct TileLds {
@@ -468,7 +469,7 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
             if (p < P) to_lds<false>(vb + threadIdx.x % D * 16u, to + 64 * wave_now + THREADS * i);
         }
     };
-    // Pages of 8 bits are requested a tile ahead of being written to the tiles' LDS as bf16 numbers, which is a tile ahead of their use.  On their way they lie in LDS that only
+    // Pages of 8 bits (2048 rows over 28672, 32 heads, d = 64: 590 to 625 us by the machine, where pages of bf16 take 558 to 575: 815 to 844 TFLOP/s) are requested a tile ahead of being written to the tiles' LDS as bf16 numbers, which is a tile ahead of their use.  On their way they lie in LDS that only
     // the wave that asked for them reads (d = 128: in registers, of which it has enough, and LDS not).  A wave's 64 threads have the same 16 channels of a tile's
     // keys, or groups of one (d = 128: of half a) block of its values.  What stands for keys that are absent is what was there before: nobody's scores, and cleared values.
     constexpr int CODED = IO::kCoded ? 8 * D / THREADS : 1;                  // groups a thread, keys' first
@@ -714,6 +715,8 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
 }
 
 // ---------------------------------------------------------------- few rows: up to 16 of a key head, keys split over waves and workgroups
+// Pages of 8 bits have steps of 64 keys, the same bytes: 32 sequences of up to 32768 tokens, 547 MB, 98 us and 5 of the join (5.6 TB/s; parts of 1024 and of 4096 keys 104), bf16 pages 181
+// and 5.  Their codes become bf16 on the way to the matrix cores, two an instruction, the scale in it; the vector unit is busy in 44 % of the cycles.
 // Every key and value is read once and multiplied with 16 columns of rows, empty ones among them: memory bounds it.  No LDS: a lane's loads are the operands (the
 // layout of the pages), one step of 32 keys (fp32: 16) in registers, of which each half is requested again as soon as it has been used, so that four waves a SIMD
 // keep up to 8 KB (d = 64) each on its way.  (Two steps in turn need twice the registers: 16 sequences of 4000 tokens, d = 128, 36 instead of 29 us.)
@@ -1172,7 +1175,7 @@ AttendPlan attend_plan(int d, int dtype, int B, int T, int H, int Hkv, int max_n
         // workgroups that run at once, by their registers and LDS; keys are split where rows leave some of them free.  Of single tiles, which memory bounds, two a
         // compute unit are enough: the join costs more than a third and fourth gain (64 sequences of 8 tokens over 2000 48 instead of 55 us, 16 over 9000 53 instead
         // of 58; one a compute unit: 50 and 73).
-        const long long slots = p.tile_waves == 8 || d == 128 || rows <= 128 ? 512 : dtype == SPECTRE_BF16 ? 1024 : 768;        // pages of 8 bits: LDS for three workgroups
+        const long long slots = p.tile_waves == 8 || d == 128 || rows <= 128 ? 512 : dtype == SPECTRE_BF16 ? 1024 : 768;        // pages of 8 bits: LDS for three (13 ragged sequences 47 us, with 1024 59, with 512 55)
         // Parts of the longest sequence; the others' parts are as long.  With several tiles a sequence of a ragged batch they take different times, and
         // twice the parts even them out (fp32 batch of up to 397 new tokens 135 instead of 142 us; single tiles, bound by memory, lose: 25.0 -> 28.8).
         const long long all = groups(p.tile_waves), keys = all > 4 * slots ? 2 * kRaggedKeys : kRaggedKeys;

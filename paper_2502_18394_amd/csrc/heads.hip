@@ -4,8 +4,9 @@
 // Per row x of d channels: r = (mean x^2 + eps)^-1/2, y = w r x, and each pair (a, b) of y turned by the angle pos * f_i:
 // (a cos - b sin, b cos + a sin).  Backward with g = the output's gradient turned back: g_w = sum g r x over rows, h = g w,
 // g_x = r (h - r x mean(h r x)).  Rows are read and written once; memory bounds the long calls, the launch the short ones.  32768 tokens of 32 + 8 bf16 heads, d = 64:
-// forward 68 to 75 us by the machine (336 MB, 4.5 to 4.9 TB/s), backward 98 to 108 (503 MB, 4.7 to 5.1 TB/s, the sums of the weights' gradients in it), the two in turn 160 to 166,
-// against 5.2 TB/s of a large copy; 8192 tokens into pages 22 us (4.6 TB/s); one token 5.
+// forward 68 to 75 us by the machine (336 MB, 4.5 to 4.9 TB/s), backward 98 to 108 (503 MB, 4.7 to 5.1 TB/s, the sums of the weights' gradients in it), the two in turn 158 to 166,
+// against 5.2 TB/s of a large copy; 8192 tokens into pages 22 us (4.6 TB/s); one token 5.  24000 tokens of three axes, forward and backward 120 us (614 MB, 5.1 TB/s); 6126 of 16 + 4
+// heads, d = 128, three axes, adjacent pairs, into pages 15.6 us (75 MB, 4.8 TB/s).
 #include "heads_dev.h"
 
 namespace spectre {

@@ -109,7 +109,7 @@ __device__ __forceinline__ void fill_turns(const HeadParams &P, FirstTurn first,
 }
 
 // How rows are turned.  Whole rows have forms of their own, in which nothing is chosen element by element and adjacent pairs do without their partners' lane; the vector
-// unit works four fifths of these kernels' time.
+// unit works four fifths of these kernels' time.  6126 tokens of adjacent pairs into pages, d = 128: 15.6 us, in the one form for all 20.9; 24000 of halves, forward and backward, 120 and 124.
 enum { kAnyTurn, kHalves, kPairs };
 inline int turn_of(const spectre_heads &P) { return P.rot != P.d ? kAnyTurn : P.interleaved ? kPairs : kHalves; }
 

