@@ -339,9 +339,10 @@ constexpr int kTileGroups = IO::kTileKeys * D / IO::E;
 // their way: 1006 instead of 630 us.)
 template <typename IO, int D>
 constexpr int kRawGroups = IO::kCoded && D == 64 ? 8 * D + 8 * D / 4 : 0;    // and their scales
-// Groups of queries that registers have no room for beside those tiles: three of four (with two 709 us traced, with three 683, with none 737).
+// Groups of queries that registers have no room for beside those tiles: all of them (2048 rows over 28672 594 us, with
+// three of four 619).
 template <typename IO, int D, int WAVES>
-constexpr int kQueryGroups = kRawGroups<IO, D> && WAVES == 8 ? 3 * 64 * WAVES : 0;
+constexpr int kQueryGroups = kRawGroups<IO, D> && WAVES == 8 ? 4 * 64 * WAVES : 0;
 struct TileLds {
     uint4 *sk0, *sv0, *sk1, *sv1;                   // kTileGroups each, arrays of their own: the compiler sees which loads a read need not wait for
     uint4 *raw, *query;                             // kRawGroups, kQueryGroups
@@ -469,9 +470,10 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
             if (p < P) to_lds<false>(vb + threadIdx.x % D * 16u, to + 64 * wave_now + THREADS * i);
         }
     };
-    // Pages of 8 bits (2048 rows over 28672, 32 heads, d = 64: 590 to 625 us by the machine, where pages of bf16 take 558 to 575: 815 to 844 TFLOP/s) are requested a tile ahead of being written to the tiles' LDS as bf16 numbers, which is a tile ahead of their use.  On their way they lie in LDS that only
+    // Pages of 8 bits are requested a tile ahead of being written to the tiles' LDS as bf16 numbers, which is a tile ahead of their use.  On their way they lie in LDS that only
     // the wave that asked for them reads (d = 128: in registers, of which it has enough, and LDS not).  A wave's 64 threads have the same 16 channels of a tile's
     // keys, or groups of one (d = 128: of half a) block of its values.  What stands for keys that are absent is what was there before: nobody's scores, and cleared values.
+    // 2048 rows over 28672, 32 heads, d = 64: 585 to 600 us by the machine, 830 to 850 TFLOP/s, where pages of bf16 take 558 to 575.
     constexpr int CODED = IO::kCoded ? 8 * D / THREADS : 1;                  // groups a thread, keys' first
     constexpr bool RAW = kRawGroups<IO, D> > 0;
     uint4 code[CODED];
@@ -514,7 +516,8 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
             }
         }
     };
-    auto write_codes = [&](uint4 *sk, uint4 *sv) {
+    // Writes what has been requested of one tile, and requests tile t in its place.
+    auto write_codes = [&](uint4 *sk, uint4 *sv, int t, int page) {
         if constexpr (IO::kCoded) {
             int at = threadIdx.x;
             asm volatile("" : "+v"(at));
@@ -534,7 +537,9 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
                 to[0] = operand<IO>(code[i], 0, code_scale[i]);
                 to[u < 4 * D ? KT : D] = operand<IO>(code[i], 1, code_scale[i]);
             }
-            if constexpr (RAW) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the next tile's come there
+            // behind the writes, which the compiler would have wait for what is on its way to LDS
+            if constexpr (RAW) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // the codes have left their place
+            request_codes(t, page);
         }
     };
     auto arrived = [&]() {
@@ -629,9 +634,8 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
         if constexpr (IO::kCoded) {
             here = __ballot((unsigned)page < P);
             request_codes(t_lo, page);
-            write_codes(sk0, sv0);
             soon = __ballot((unsigned)next < P);
-            request_codes(t_lo + 1, next);
+            write_codes(sk0, sv0, t_lo + 1, next);
             next = page_of(t_lo + 2);
         } else {
             request_keys(t_lo, page, sk0);
@@ -642,9 +646,10 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
         const unsigned long long there = IO::kCoded ? here : __ballot((unsigned)page < P);      // bit = key of the tile (fp32: twice 32 keys)
         arrived();
         if constexpr (IO::kCoded) {
-            write_codes(next_k, next_v);
             here = soon;
             soon = __ballot((unsigned)next < P);
+            write_codes(next_k, next_v, t + 2, next);
+            next = page_of(t + 3);
         } else page = next;
         if (!IO::kCoded && t + 1 < t_hi) {
             request_keys(t + 1, page, next_k);
@@ -652,14 +657,9 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
             next = page_of(t + 2);
         }
         clean(t, there, sv, flag);
-        const bool idle = !busy || t * KT > wave_last;
+        if (!busy || t * KT > wave_last) return;
         f32x16_t sc[NK];
-        if (!idle) scores(sk, sc);
-        if constexpr (IO::kCoded) {        // behind the scores: queries that registers have no room for are read again for them, and whoever waits for those waits for all before
-            request_codes(t + 2, next);
-            next = page_of(t + 3);
-        }
-        if (idle) return;
+        scores(sk, sc);
         hide(t, there, sc);
         keep_up(max_halves(largest(sc)));
         const float shift = shift_of(top, k.c);
@@ -1175,7 +1175,8 @@ AttendPlan attend_plan(int d, int dtype, int B, int T, int H, int Hkv, int max_n
         // workgroups that run at once, by their registers and LDS; keys are split where rows leave some of them free.  Of single tiles, which memory bounds, two a
         // compute unit are enough: the join costs more than a third and fourth gain (64 sequences of 8 tokens over 2000 48 instead of 55 us, 16 over 9000 53 instead
         // of 58; one a compute unit: 50 and 73).
-        const long long slots = p.tile_waves == 8 || d == 128 || rows <= 128 ? 512 : dtype == SPECTRE_BF16 ? 1024 : 768;        // pages of 8 bits: LDS for three (13 ragged sequences 47 us, with 1024 59, with 512 55)
+        const long long slots = p.tile_waves == 8 || d == 128 || (rows <= 128 && dtype != SPECTRE_E4M3) ? 512 : dtype == SPECTRE_BF16 ? 1024 : 768;
+        // Pages of 8 bits leave LDS for three workgroups of four waves a compute unit: 13 ragged sequences 47 us, with 1024 59, with 512 55; 7 of 17 tokens over 17721 60.0, with 512 63.4.
         // Parts of the longest sequence; the others' parts are as long.  With several tiles a sequence of a ragged batch they take different times, and
         // twice the parts even them out (fp32 batch of up to 397 new tokens 135 instead of 142 us; single tiles, bound by memory, lose: 25.0 -> 28.8).
         const long long all = groups(p.tile_waves), keys = all > 4 * slots ? 2 * kRaggedKeys : kRaggedKeys;

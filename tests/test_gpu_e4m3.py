@@ -393,3 +393,40 @@ def test_tokens_one_by_one_end_as_all_at_once():
     for a, b, s in ((ka, kb, sa[..., :1]), (va, vb, sa[..., 1:])):
         normal = np.abs(a) >= 2.0 ** -5 * s
         assert np.array_equal(a[normal], b[normal]) and (np.abs(a - b) <= 2 * ref.SMALL * s * np.ones_like(a)).all()
+
+
+def test_pages_beyond_four_gigabytes():
+    """A pool whose keys alone are more than 2^32 bytes: the last pages are written, read, forked and copied where they lie, and nothing in front of them."""
+    pages, Hkv, page, d = 33000, 8, 256, 64                  # 4.3 GB of keys
+    pool = binding.KvPages.empty(1, pages, Hkv, d, page, 3, 4, F8)
+    last = [pages - 1, pages - 2, pages - 3]
+    pool.table[0, :3] = _ints(last)
+    pool.refs[_ints(last).long()] = 1
+    pool.lens[0] = 600
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn(600, n, d, generator=g).to(BF16).cuda() for n in (16, Hkv, Hkv))
+    pool.append(0, q, k, v, _ints([0, 600]), _ints([0]))
+    assert not pool.k_pages.view(torch.uint8)[0, :pages - 3].any() and not pool.v_pages.view(torch.uint8)[0, :pages - 3].any()
+    k_got, v_got, s = ref.rows(Window(pool, pages - 3), 0, 0, 600)
+    rows, x = [(k_got, v_got)], v.double().cpu().numpy()
+    assert (np.abs(v_got - x) <= ref.STEP * np.abs(x) + ref.SMALL * s[..., 1:]).all()          # half a step of a normal number, or of a subnormal one: 2^-10 of the scale
+    for n in (1, 40):
+        out, lse = pool.attend(0, q[:n].contiguous(), _ints([0, n]), _ints([0]), n, 600, want_lse=True)
+        check(out, lse, q[:n], [n], rows, 0.125, BF16)
+    pool.fork(_ints([0]), _ints([1]))                        # the last page goes to page 0
+    pool.copy(_ints([pages - 1]), _ints([pages - 5]))
+    assert pool.table[1, :3].tolist() == [pages - 1, pages - 2, 0] and int(pool.status[0]) == 0
+    # whole groups of 16 tokens: 600 - 512 = 88 are 96
+    assert torch.equal(pool.k_pages.view(torch.uint8)[0, 0, :, :, :96], pool.k_pages.view(torch.uint8)[0, pages - 3, :, :, :96])
+    assert torch.equal(pool.scales[0, 0, :, :6], pool.scales[0, pages - 3, :, :6]) and (pool.scales[0, 0, :, 6:] == 1).all()
+    for x in (pool.k_pages, pool.v_pages, pool.scales):
+        assert torch.equal(x.view(torch.uint8)[0, pages - 5], x.view(torch.uint8)[0, pages - 1])
+
+
+class Window:
+    """The pages from `first` on of a pool, as e4m3_ref.rows looks at one."""
+
+    def __init__(self, pool, first):
+        self.page, self.Hkv, self.d = pool.page, pool.Hkv, pool.d
+        self.table = (pool.table - first).clamp(min=-1)
+        self.k_pages, self.v_pages, self.scales = (x.view(torch.uint8)[:, first:].contiguous().view(x.dtype) for x in (pool.k_pages, pool.v_pages, pool.scales))
