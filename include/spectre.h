@@ -551,7 +551,7 @@ int spectre_kv_append(const spectre_kv *kv /*host*/, int layer, const spectre_he
  *           / 448 (0, and with it codes of 0, where that is below 2^-126), what is meant is code * scale.  scales NULL otherwise.
  * spectre_norm_backward: from dy (of y, in io whatever y's type was), sum as it was kept (without an addition: x) and dsum (of sum as a residual, NULL: none) the gradient
  * gx [T, D], which is x's and delta's, and gw fp32 [D] (NULL: not wanted), whose sums over rows are of up to 128 rows in fp32, those sums in fp64, all in a fixed
- * order.  Workspace for gw only.  spectre_kv_prepare loads the kernels.
+ * order.  gw 16-byte aligned; workspace for gw only, 0 bytes: none.  spectre_kv_prepare loads the kernels.
  */
 enum { SPECTRE_NORM_GROUP = 128 };
 int spectre_norm_forward(const void *x, long long x_stride, const void *delta, long long delta_stride, const float *w, int T, int D, float eps, spectre_dtype io,

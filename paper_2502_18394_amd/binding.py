@@ -753,8 +753,9 @@ def add_norm_backward(dy, total, weight=None, dsum=None, eps=1e-6, ws=None, stre
         gw = _like(weight, stream)
         if ws is None:
             wsn = lib().spectre_norm_backward_workspace_bytes(T, D, io)
-            ws = _new((wsn,), torch.uint8, total.device, stream)      # the allocator's memory is aligned
-            wsp = ws.data_ptr()
+            if wsn:
+                ws = _new((wsn,), torch.uint8, total.device, stream)  # the allocator's memory is aligned
+                wsp = ws.data_ptr()
         else:
             wsp, wsn = _given(ws)
     _check(lib().spectre_norm_backward(ya, ys, ta, ts, da, ds, w, T, D, eps, io, _ptr(gx, "gx"), None if gw is None else _ptr(gw, "gw"), wsp, wsn, _now(stream)))

@@ -364,7 +364,8 @@ int spectre_norm_forward(const void *x, long long x_stride, const void *delta, l
 
 size_t spectre_norm_backward_workspace_bytes(int T, int D, spectre_dtype io) {
     if (check_norm(nullptr, T, D, 0.f, io, "norm_backward")) return 0;
-    return align256((size_t)norm_backward_blocks(T, D * size_of(io) / 16) * D * sizeof(float) + 1);
+    const int blocks = norm_backward_blocks(T, D * size_of(io) / 16);
+    return blocks > 1 ? align256((size_t)blocks * D * sizeof(float)) : 0;
 }
 
 int spectre_norm_backward(const void *dy, long long dy_stride, const void *sum, long long sum_stride, const void *dsum, long long dsum_stride, const float *w, int T, int D,
@@ -372,7 +373,7 @@ int spectre_norm_backward(const void *dy, long long dy_stride, const void *sum, 
     const char *who = "norm_backward";
     int rc = check_norm(w, T, D, eps, io, who);
     if (rc) return rc;
-    if (!aligned(gw, 4)) return fail(SPECTRE_EINVAL, "%s: gw not aligned", who);
+    if (!aligned(gw, 16)) return fail(SPECTRE_EINVAL, "%s: gw not 16-byte aligned", who);
     const NormRows n = {sum, nullptr, sum_stride, 0, w, eps, T, D};
     const NormGrads g = {dy, dsum, dy_stride, dsum_stride};
     if (T == 0) return gw ? done(launch_norm_backward(n, g, (int)io, gx, gw, nullptr, static_cast<hipStream_t>(stream)), who) : SPECTRE_OK;
@@ -385,7 +386,8 @@ int spectre_norm_backward(const void *dy, long long dy_stride, const void *sum, 
             return fail(SPECTRE_EINVAL, "%s: an output overlaps %s", who, in[i].name);
     }
     if (gw && meets(gx, bytes, gw, D * sizeof(float))) return fail(SPECTRE_EINVAL, "%s: outputs overlap", who);
-    if (gw && (rc = check_ws(ws, ws_bytes, spectre_norm_backward_workspace_bytes(T, D, io), who))) return rc;
+    const size_t need = gw ? spectre_norm_backward_workspace_bytes(T, D, io) : 0;
+    if (need && (rc = check_ws(ws, ws_bytes, need, who))) return rc;
     return done(launch_norm_backward(n, g, (int)io, gx, gw, static_cast<float *>(ws), static_cast<hipStream_t>(stream)), who);
 }
 

@@ -80,7 +80,7 @@ def test_rows_in_8_bits(T, D, io):
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
-@pytest.mark.parametrize("T,D", [s for s in SHAPES if s != (1, 8)] + [(9000, 64), (1, 8)])
+@pytest.mark.parametrize("T,D", SHAPES + [(9000, 64), (8, 2048), (9, 2048), (32, 1024), (33, 1024), (8, 4096)])
 def test_backward(T, D, io):
     print(f"case T={T} D={D} {io}", flush=True)
     s, dy, w, g = _inputs(T, D, io, T + D + 1, strided=T == 33)

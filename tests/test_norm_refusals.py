@@ -36,18 +36,19 @@ def test_forward_refuses(lib):
 
 
 def test_backward_refuses(lib):
-    need = lib.spectre_norm_backward_workspace_bytes(3, 256, 1)
-    assert need >= 3 * 256 * 4 and lib.spectre_norm_backward_workspace_bytes(3, 250, 1) == 0 and lib.spectre_norm_backward_workspace_bytes(3, 256, 4) == 0
+    need = lib.spectre_norm_backward_workspace_bytes(3000, 256, 1)
+    assert need >= 3000 // 128 * 256 * 4 and lib.spectre_norm_backward_workspace_bytes(3, 256, 1) == 0       # one workgroup's sums are the gradient
+    assert lib.spectre_norm_backward_workspace_bytes(3000, 250, 1) == 0 and lib.spectre_norm_backward_workspace_bytes(3000, 256, 4) == 0
     assert lib.spectre_norm_backward_workspace_bytes(-1, 256, 1) == 0
     # the sums of 32 bits are of 128 rows at most: so many rows of partial sums
     assert lib.spectre_norm_backward_workspace_bytes(10 ** 7, 64, 1) >= 10 ** 7 // 128 * 64 * 4
 
-    def backward(dy=FAKE, ys=256, total=FAR, ts=256, dsum=FAR + BIG, ds=256, w=W, T=3, D=256, eps=1e-6, io=1, gx=OUT, gw=OUT + BIG, ws=W + BIG, size=need):
+    def backward(dy=FAKE, ys=256, total=FAR, ts=256, dsum=FAR + BIG, ds=256, w=W, T=3000, D=256, eps=1e-6, io=1, gx=OUT, gw=OUT + BIG, ws=W + BIG, size=need):
         return lib.spectre_norm_backward(dy, ys, total, ts, dsum, ds, w, T, D, eps, io, gx, gw, ws, size, None)
 
     for bad, code in ((dict(dy=None), 1), (dict(total=None), 1), (dict(dsum=FAR + BIG + 4), 1), (dict(ds=128), 1), (dict(gx=None), 1), (dict(gx=FAR), 1), (dict(gx=FAKE), 1),
                       (dict(gx=FAR + BIG), 1), (dict(gw=OUT + 16), 1), (dict(gw=FAKE), 1), (dict(ws=None), 3), (dict(size=need - 256), 3), (dict(ws=W + BIG + 4), 1),
-                      (dict(D=200), 1), (dict(D=4), 2), (dict(io=3), 1), (dict(eps=-0.5), 1), (dict(gw=OUT + BIG + 2), 1)):
+                      (dict(D=200), 1), (dict(D=4), 2), (dict(io=3), 1), (dict(eps=-0.5), 1), (dict(gw=OUT + BIG + 2), 1), (dict(gw=OUT + BIG + 4), 1)):
         a = dict(bad)
         if a.get("D") == 200:
             a["ys"] = 199
