@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import axes_ref
 import e4m3_ref as ref
 import paged_ref
 from paper_2502_18394_amd import binding
@@ -430,3 +431,42 @@ class Window:
         self.page, self.Hkv, self.d = pool.page, pool.Hkv, pool.d
         self.table = (pool.table - first).clamp(min=-1)
         self.k_pages, self.v_pages, self.scales = (x.view(torch.uint8)[:, first:].contiguous().view(x.dtype) for x in (pool.k_pages, pool.v_pages, pool.scales))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rot,interleaved,axes", [(32, False, 1), (32, True, 1), (0, False, 1), (None, True, 1), (None, False, 3), (None, True, 2), (48, False, 8)])
+def test_append_with_every_way_of_turning(d, rot, interleaved, axes):
+    """Part of a row, adjacent pairs, no rotation, several axes, positions given for one; rows of one projection, with something between the tokens; rows behind the last sequence stay."""
+    rot = d if rot is None else rot
+    print(f"case d={d} rot={rot} interleaved={interleaved} axes={axes}", flush=True)
+    H, Hkv, news, had, seqs, page = 5, 3 if d == 64 else 1, [21, 1, 40], [10, 5, 0], [1, 0, 2], 32
+    H *= Hkv
+    T, g = sum(news), torch.Generator().manual_seed(d + rot + axes)
+    pool = binding.KvPages.empty(1, 12, Hkv, d, page, 3, 4, F8)
+    pool.reserve(_ints(seqs), _ints(had))
+    pool.append(0, *(torch.zeros(sum(had), n, d, dtype=BF16, device="cuda") for n in (H, Hkv, Hkv)), _ints([0, 10, 15, 15]), _ints(seqs))     # blocks of zeros, the least scale
+    pool.reserve(_ints(seqs), _ints(news))
+    wide = torch.randn(T + 3, H + 2 * Hkv + 1, d, generator=g).to(BF16).cuda()
+    q, k, v = wide[:, :H], wide[:, H:H + Hkv], wide[:, H + Hkv:H + 2 * Hkv]
+    axis = torch.cat((torch.arange(axes), torch.randint(0, axes, (max(rot // 2 - axes, 0),), generator=g))) if rot else None
+    rope = binding.Rope.of(rot, 500000.0, interleaved, axes=axis if axes > 1 else None) if rot else None
+    places = torch.cat([torch.arange(a, a + n) for n, a in zip(news, had)] + [torch.zeros(3, dtype=torch.long)])
+    pos = torch.randint(0, 90000, (axes, T + 3), generator=g, dtype=torch.int32) if axes > 1 or rot == 32 else places[None].int()
+    w = [(1 + 0.2 * torch.randn(d, generator=g)).cuda() for _ in "qk"]
+    out = torch.full((T + 3, H, d), 7.0, dtype=BF16, device="cuda")
+    given = pos.cuda() if axes > 1 or rot == 32 else None
+    pool.append(0, q, k, v, torch.tensor([0] + news).cumsum(0).int().cuda(), _ints(seqs), rope, *w, 1e-6, out, positions=given)
+    assert (out[T:] == 7).all() and int(pool.status[0]) == 0
+    both = binding.qk_norm_rotate(q, k, pos.cuda() if axes > 1 else pos[0].cuda(), rope, *w)
+    assert torch.equal(out[:T], both[0][:T])
+    freq = paged_ref.f64(rope.inv_freq) if rot else np.zeros(0)
+    angle = axes_ref.angles(pos.numpy(), axis.numpy() if axes > 1 else np.zeros(rot // 2, int), freq) if rot else np.zeros((T + 3, 0))
+    plain = axes_ref.heads(k.double().cpu().numpy(), paged_ref.f64(w[1]), angle * 0, 1e-6, interleaved)
+    k64, size, v64 = axes_ref.heads(k.double().cpu().numpy(), paged_ref.f64(w[1]), angle, 1e-6, interleaved), _turn_size(plain, rot // 2, interleaved), v.double().cpu().numpy()
+    at = 0
+    for s, n, before in zip(seqs, news, had):
+        zeros = np.zeros((before, Hkv, d))
+        rows = [np.concatenate((zeros, x[at:at + n])) for x in (k64, size, v64)]
+        for first in range(0, before + n, 16):
+            _check_block(pool, 0, s, first, min(16, before + n - first), [before] if first < before < first + 16 else [], *rows, d)
+        at += n
