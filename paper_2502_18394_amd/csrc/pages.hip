@@ -195,8 +195,6 @@ __global__ __launch_bounds__(kScan) void k_kv_fork_plan(KvView kv, const int *sr
     }
 }
 
-// Child i's row of the table, and the tokens of its last page: block x = child, y = slices of the layers' K and V.  Parents' rows and lengths are only
-// read (no child is a parent), users are counted with integer atomics, whose order changes nothing.
 // Scales of `blocks` blocks of tokens, of keys and values, from page a to page b of every head of a layer (pages of 8 bits; a block of a page of one head after the other).
 __device__ __forceinline__ void copy_scales(const KvView &kv, int layer, int a, int b, int blocks) {
     if (!kv.layer_scales) return;
@@ -208,6 +206,8 @@ __device__ __forceinline__ void copy_scales(const KvView &kv, int layer, int a, 
     }
 }
 
+// Child i's row of the table, and the tokens of its last page: block x = child, y = slices of the layers' K and V.  Parents' rows and lengths are only
+// read (no child is a parent), users are counted with integer atomics, whose order changes nothing.
 __global__ __launch_bounds__(256) void k_kv_fork(KvView kv, int layers, int d, int E, const int *src, const int *dst, int n, const int *ws) {
     if (!ws[0]) return;
     const int i = blockIdx.x, a = src[i], b = dst[i], len = kv.lens[a], page = 1 << kv.page_log;

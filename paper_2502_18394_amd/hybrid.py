@@ -52,6 +52,10 @@ class HybridDecoder:
         """(x + more, its norm): `more` is what the layer before adds to the residual."""
         return binding.add_norm(x, None, more, torch.finfo(torch.float32).eps)
 
+    @staticmethod
+    def _sum(x, more):
+        return x if more is None else x + more
+
     def _attend(self, layer, x, more, start, seqs, max_new, positions=None):
         """Attention layer on new tokens x + more [T, width]: their keys and values go into the pages, then they attend over them.  Returns (x + more, what it adds)."""
         w, T = self.attention[layer], x.shape[0]
@@ -104,7 +108,7 @@ class HybridDecoder:
                 mixed = cache.readout(gate, binding.READ_WINDOW, self.dtype)[:, -T:]
                 more = mixed.reshape(T, self.width) @ w["out"]
             self.tokens += T
-        return x[-1:] + more[-1:]
+        return self._sum(x[-1:], None if more is None else more[-1:])
 
     def fork(self):
         """Samples 1 .. n take over the prompt: pages shared, the last one copied; the spectral state for each of them."""
@@ -158,11 +162,11 @@ class HybridDecoder:
                 rows = rows.view(self.samples, 1, self.H, self.d)
                 more = w["cache"].step(rows, rows, w["gate"]).view(self.samples, self.width) @ w["out"]
         self.tokens += 1
-        return x + more
+        return self._sum(x, more)
 
     def choose(self, x, noise):
         """A token for each row, drawn with the given uniform random numbers (Gumbel's trick)."""
-        logits = (self._norm(x)[1] @ self.head).float()
+        logits = (self._norm(x.contiguous())[1] @ self.head).float()
         return (logits - (-noise.clamp(1e-20, 1.0).log()).log()).argmax(-1)
 
     def release(self, keep):
@@ -176,7 +180,7 @@ def run(prompt, chunk, samples, new, noise, captured=True, **sizes):
     m = HybridDecoder(samples=samples, **sizes)
     x = m.prompt(prompt, chunk)
     m.fork()
-    x, got = x.expand(samples, -1).contiguous(), []
+    x, got = x.expand(samples, -1), []
     for i in range(new):
         got.append(m.choose(x, noise[i]))
         x = m.step(got[-1], captured)

@@ -61,3 +61,15 @@ def test_the_place_in_the_picture_matters():
     assert not torch.equal(keys[0], keys[1]) and not torch.equal(keys[1], keys[2])
     m = hybrid.HybridDecoder(samples=1, **dict(SIZES, layers=2), grid=5)
     assert m._positions(24, 3).tolist() == [[0, 1, 1], [4, 0, 0], [4, 0, 1]] and m._positions(7, 1, 2).tolist() == [[0, 0], [1, 1], [2, 2]]
+
+
+def test_rows_that_are_one_row_and_no_layers_at_all():
+    """Samples' rows that are one row's view, as a prompt's last row is before they part; a decoder without layers gives the tokens' own rows."""
+    prompt, noise = _inputs(20, 1, 3)
+    m = hybrid.HybridDecoder(samples=3, **SIZES)
+    x = m.prompt(prompt, 20).expand(3, -1)
+    assert torch.equal(m.choose(x, noise[0]), m.choose(x.clone(), noise[0]))
+    m = hybrid.HybridDecoder(samples=3, **dict(SIZES, layers=0))
+    assert torch.equal(m.prompt(prompt, 8), m.embed[prompt[-1:]])
+    m.fork()
+    assert torch.equal(m.step(prompt[:3]), m.embed[prompt[:3]])
