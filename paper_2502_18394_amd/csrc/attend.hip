@@ -258,7 +258,7 @@ __device__ __forceinline__ float shift_of(float top, float c) { return top == -I
 
 // Values that are not finite, of keys base .. base + count - 1 of head h, for a row at `pos` whose lane holds channels channel(r), r < N.  The rows' finite
 // parts have been added; a weight is above zero for every key a row sees, so what is added is the value itself.
-template <typename IO, int D, int N, typename Channel, typename Add>
+template <typename IO, int D, int N, bool ONE_BY_ONE, typename Channel, typename Add>
 __device__ __forceinline__ void add_not_finite(const KvView &kv, const Seq &s, int h, int base, int count, int pos, int from, Channel channel, Add add) {
     typedef typename IO::elem_t elem_t;
     const int *table = kv.table + (long long)s.row * kv.M;
@@ -276,7 +276,7 @@ __device__ __forceinline__ void add_not_finite(const KvView &kv, const Seq &s, i
             float x;
             if constexpr (IO::kCoded) x = e4m3_decode1(codes[channel(r) * IO::PE], scale);
             else x = IO::value(v[channel(r) * IO::E]);
-            if constexpr (N > 32) {
+            if constexpr (N > 32 || ONE_BY_ONE) {
                 // one condition at a time: 64 pairs of scalar registers are taken from the loop around otherwise (its addresses then live in lanes of a
                 // vector register: 540 instead of 499 us for 2048 rows over 28672, d = 128; with 32 channels a lane the plain form is the faster one)
                 add(r, isfinite(x) ? 0.f : x);
@@ -603,7 +603,7 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
             for (int i = 0; i < 16; ++i) o[d][i] *= f;
     };
     auto add_odd = [&](int t) {
-        add_not_finite<IO, D, 16 * DT>(kv, s, h, t * KT, KT, pos, lowest - 1, [half](int i) { return 32 * (i / 16) + 8 * ((i % 16) / 4) + 4 * half + i % 4; },
+        add_not_finite<IO, D, 16 * DT, false>(kv, s, h, t * KT, KT, pos, lowest - 1, [half](int i) { return 32 * (i / 16) + 8 * ((i % 16) / 4) + 4 * half + i % 4; },
                                        [&](int i, float x) { o[i / 16][i % 16] += x; });
     };
     const int krow = IO::key_of_row(lane & 31);
@@ -714,7 +714,7 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
     if (k.a.lse && half == 0) k.a.lse[at] = lse_of(top2, sum);
 }
 
-// ---------------------------------------------------------------- few rows: up to 16 of a key head, keys split over waves and workgroups
+// ---------------------------------------------------------------- few rows: up to 16 of a key head (pages of 8 bits: 64), keys split over waves and workgroups
 // Pages of 8 bits have steps of 64 keys, the same bytes: 32 sequences of up to 32768 tokens, 547 MB, 98 us and 5 of the join (5.6 TB/s; parts of 1024 and of 4096 keys 104), bf16 pages 181
 // and 5.  Their codes become bf16 on the way to the matrix cores, two an instruction, the scale in it; the vector unit is busy in 44 % of the cycles.
 // Every key and value is read once and multiplied with 16 columns of rows, empty ones among them: memory bounds it.  No LDS: a lane's loads are the operands (the
@@ -722,20 +722,33 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
 // keep up to 8 KB (d = 64) each on its way.  (Two steps in turn need twice the registers: 16 sequences of 4000 tokens, d = 128, 36 instead of 29 us.)
 // A large pool is read past the memory-side cache, its pages come round again only when every other layer's have.  8 sequences of 32700 tokens, 537 MB:
 // 89 us, 6.0 TB/s (cached 100); 32 of up to 32768, 1.09 GB, 185 us, 5.9 TB/s; a pool of 67 MB would lose (23.1 -> 24.2 us), one of 131 MB gains (33.2 -> 31.1).
+// COLS groups of 16 rows share what is read and, of pages of 8 bits, what is converted; their queries lie in LDS, and a probability goes as one term, as in tiles.  Without a
+// barrier between steps, and with every wave at work, a tile's way is the longer one up to 64 rows (d = 128: 48, whose registers leave one wave a SIMD): 64 sequences of
+// 8 tokens over 8000, 32 rows, 112 us, as tiles 179; 64 of 16 over 2000, 64 rows, 36 and 60; d = 128, 32 of 5 over 4000, 40 rows, 26 and 32.5, but 64 rows (registers
+// spilled) 48 and 34.5.  With so many rows a short part's time is that of its code's first execution, about 0.5 us a KB: outputs are joined in one loop for all groups (16 windows
+// of 5 tokens, 40 rows, d = 128: 21.3 us, group by group 23.1).
 constexpr int kSection = 256;                      // page numbers in LDS at a time
 
 template <typename IO, int D>
 constexpr int kFewGroups = 16 * D / 4;              // of a wave's 16 rows of outputs
+template <int ROWS>
 struct FewLds {
     int *pages;                                     // [kSection + 2]
-    float (*tops)[16], (*sums)[16];                 // [waves][16]
-    f32x4_t *out0, *out1, *out2, *out3;             // kFewGroups for every fourth wave each
+    float (*tops)[ROWS], (*sums)[ROWS];             // [waves][rows]
+    f32x4_t *out0, *out1, *out2, *out3;             // kFewGroups for 16 rows of every fourth wave each
+    uint4 *query;                                   // kFewQueries
 };
 
-template <typename IO, int D, int WAVES>
-__device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds) {
+// Operands of 16 rows' queries, of which there are COLS; more than one stay in LDS, where the waves share them.
+template <typename IO, int D>
+constexpr int kFewOperands = D / (4 * IO::PE) * (IO::PE == 16 ? 2 : 1);
+template <typename IO, int D, int COLS>
+constexpr int kFewQueries = COLS > 1 ? 64 * COLS * kFewOperands<IO, D> : 0;
+
+template <typename IO, int D, int WAVES, int COLS>
+__device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds<16 * COLS> lds) {
     constexpr int E = IO::E, PE = IO::PE, SK = IO::kStepKeys, KTILES = SK / 16, DT = D / 16, THREADS = 64 * WAVES;
-    constexpr int GROUPS = D / (4 * PE), HALVES = PE == 16 ? 2 : 1, QG = GROUPS * HALVES;    // groups of a key a lane, operands of each
+    constexpr int GROUPS = D / (4 * PE), HALVES = PE == 16 ? 2 : 1, QG = kFewOperands<IO, D>;    // groups of a key a lane, operands of each
     int *const pages = lds.pages;
     const KvView &kv = k.kv;
     const int pairs = kv.Hkv * k.a.B, split = block / pairs, pair = turned_pair(block, split, pairs), h = pair % kv.Hkv;
@@ -745,14 +758,22 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
     if (rows == 0 || rows > k.few_rows) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
     const int p0 = s.m - s.n, mask = (1 << kv.page_log) - 1;
-    const int token = min(col, rows - 1) / k.G, head = h * k.G + (min(col, rows - 1) - token * k.G);
-    const int pos = p0 + token, lowest = k.a.window ? pos - k.a.window + 1 : 0;              // the row sees the `span` keys from here on
-    const unsigned span = (unsigned)max(pos - lowest + 1, 0);
-    uint4 q[QG];
-    {
+    int pos[COLS], lowest[COLS];                                              // row 16 g + col sees the `span` keys from `lowest` on
+    unsigned span[COLS];
+    uint4 q[COLS > QG ? COLS : QG];
+#pragma unroll
+    for (int g = 0; g < COLS; ++g) {
+        const int r = min(16 * g + col, rows - 1), token = r / k.G, head = h * k.G + (r - token * k.G);
+        pos[g] = p0 + token;
+        lowest[g] = k.a.window ? pos[g] - k.a.window + 1 : 0;
+        span[g] = (unsigned)max(pos[g] - lowest[g] + 1, 0);
         const char *base = reinterpret_cast<const char *>(k.a.q) + ((s.from + token) * k.a.q_stride + head * D) * IO::kBytes;
 #pragma unroll
-        for (int j = 0; j < QG; ++j) q[j] = reinterpret_cast<const uint4 *>(base)[HALVES * (4 * (j / HALVES) + quarter) + j % HALVES];
+        for (int j = 0; j < QG; ++j) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(base) + HALVES * (4 * (j / HALVES) + quarter) + j % HALVES;
+            if constexpr (COLS == 1) q[j] = *from;
+            else if ((g * QG + j) % WAVES == wave) lds.query[64 * (g * QG + j) + lane] = *from;
+        }
     }
     // this workgroup's keys: whole steps of all waves
     const int lo = k.a.window ? max(0, p0 - k.a.window + 1) & ~63 : 0, hi = s.m;
@@ -761,10 +782,15 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
     const int all_from = k.a.window ? p0 + s.n - 1 - k.a.window : -1;         // every row sees the keys above it ...
     const int all_pos = p0;                                                   // ... up to this one
 
-    f32x4_t o[DT];
-    float top = -INFINITY, sum = 0.f;
+    f32x4_t o[COLS][DT];
+    float top[COLS], sum[COLS];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < COLS; ++g) {
+        top[g] = -INFINITY;
+        sum[g] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[g][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
     const float lag = kLag / k.c;
     const int koff = E == 8 ? PE * (col >> 2) + (col & 3) : col;              // this lane's key of a step (bf16: and the one 4 on, 8 bits: the three)
     const unsigned page_bytes = (unsigned)kv.Hkv * (D * IO::kPageBytes) << kv.page_log, head_bytes = (unsigned)h * (D * IO::kPageBytes) << kv.page_log;
@@ -838,43 +864,70 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
             const bool more = base + WAVES * SK < sec_end;
             const bool absent = (unsigned)vpage >= P;                             // this lane's run of E keys, whose scores and values it holds
             const bool edge = __ballot(absent) != 0 || base + SK - 1 > all_pos || base <= all_from;
-            f32x4_t sc[KTILES];
+            f32x4_t sc[COLS][KTILES];
 #pragma unroll
             for (int t = 0; t < KTILES; ++t) {
-                sc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < QG; ++j) IO::mma16(sc[t], operand<IO>(kr[t * GROUPS + j / HALVES], j % HALVES, k_scale), q[j]);
+                for (int g = 0; g < COLS; ++g) sc[g][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                if constexpr (COLS == 1) {
+#pragma unroll
+                    for (int j = 0; j < QG; ++j) IO::mma16(sc[0][t], operand<IO>(kr[t * GROUPS + j / HALVES], j % HALVES, k_scale), q[j]);
+                }
+            }
+            if constexpr (COLS > 1) {
+                int at = lane;
+                asm volatile("" : "+v"(at));                                  // opaque: not kept in registers from step to step
+#pragma unroll
+                for (int j = 0; j < QG; ++j) {
+#pragma unroll
+                    for (int g = 0; g < COLS; ++g) q[g] = lds.query[64 * (g * QG + j) + at];
+#pragma unroll
+                    for (int t = 0; t < KTILES; ++t) {
+                        const uint4 key = operand<IO>(kr[t * GROUPS + j / HALVES], j % HALVES, k_scale);
+#pragma unroll
+                        for (int g = 0; g < COLS; ++g) IO::mma16(sc[g][t], key, q[g]);
+                    }
+                }
             }
             if (more) request_keys(base + WAVES * SK);
-            if (edge) {
-                const unsigned at = (unsigned)(base + PE * quarter - lowest);
+            uint4 pg[COLS][HALVES], rest[HALVES];
+#pragma unroll
+            for (int g = 0; g < COLS; ++g) {
+                float p[4 * KTILES];
+                if (edge) {
+                    const unsigned at = (unsigned)(base + PE * quarter - lowest[g]);
+#pragma unroll
+                    for (int t = 0; t < KTILES; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (absent || at + (4 * t + e) >= span[g]) sc[g][t][e] = -INFINITY;
+                }
+                float mx = sc[g][0][0];
 #pragma unroll
                 for (int t = 0; t < KTILES; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (absent || at + (4 * t + e) >= span) sc[t][e] = -INFINITY;
-            }
-            float mx = sc[0][0];
+                    for (int e = 0; e < 4; ++e) mx = larger(mx, sc[g][t][e]);
+                mx = max_halves(max_quarters(mx));
+                if (__ballot(lags(mx, top[g], lag))) {
+                    const float f = follow(mx, k.c, &top[g]);
+                    sum[g] *= f;
 #pragma unroll
-            for (int t = 0; t < KTILES; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mx = larger(mx, sc[t][e]);
-            mx = max_halves(max_quarters(mx));
-            if (__ballot(lags(mx, top, lag))) {
-                const float f = follow(mx, k.c, &top);
-                sum *= f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] *= f;
-            }
-            const float shift = shift_of(top, k.c);
-            float p[4 * KTILES];
-#pragma unroll
-            for (int t = 0; t < KTILES; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[4 * t + e] = exp2_fast(fmaf(sc[t][e], k.c, shift));
-                    sum += p[4 * t + e];
+                    for (int d = 0; d < DT; ++d) o[g][d] *= f;
                 }
+                const float shift = shift_of(top[g], k.c);
+#pragma unroll
+                for (int t = 0; t < KTILES; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[4 * t + e] = exp2_fast(fmaf(sc[g][t][e], k.c, shift));
+                        sum[g] += p[4 * t + e];
+                    }
+#pragma unroll
+                for (int x = 0; x < HALVES; ++x) {
+                    pg[g][x] = IO::pack(p + 8 * x);
+                    if constexpr (E == 8 && COLS == 1) rest[x] = IO::pack_rest(p + 8 * x, pg[g][x]);
+                }
+            }
             // two terms of a probability may be of different signs, or one of them zero: infinite values go their own way in every step
             bool look = edge, odd = false;
             if constexpr (IO::kCoded) {
@@ -912,49 +965,59 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
             }
 #pragma unroll
             for (int x = 0; x < HALVES; ++x) {
-                const uint4 pg = IO::pack(p + 8 * x);
                 if constexpr (IO::kCoded) {
-                    const uint4 rest = IO::pack_rest(p + 8 * x, pg);
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
                         const uint4 v = operand<IO>(vr[d], x, v_scale);
-                        IO::mma16(o[d], v, pg);
-                        IO::mma16(o[d], v, rest);
+#pragma unroll
+                        for (int g = 0; g < COLS; ++g) {
+                            IO::mma16(o[g][d], v, pg[g][x]);
+                            if constexpr (COLS == 1) IO::mma16(o[g][d], v, rest[x]);
+                        }
                     }
                 } else {
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) IO::mma16(o[d], vr[d], pg);
-                    if constexpr (E == 8) {                // the rest of the probabilities: four more products a step cost nothing here
-                        const uint4 rest = IO::pack_rest(p, pg);
+                    for (int d = 0; d < DT; ++d) IO::mma16(o[0][d], vr[d], pg[0][0]);
+                    if constexpr (E == 8) {
 #pragma unroll
-                        for (int d = 0; d < DT; ++d) IO::mma16(o[d], vr[d], rest);
+                        for (int d = 0; d < DT; ++d) IO::mma16(o[0][d], vr[d], rest[0]);
                     }
                 }
             }
             if (more) request_values(base + WAVES * SK);
             if (odd)
-                add_not_finite<IO, D, 4 * DT>(kv, s, h, base, SK, pos, lowest - 1, [quarter](int n) { return 16 * (n / 4) + 4 * quarter + n % 4; },
-                                              [&](int n, float y) { o[n / 4][n % 4] += y; });
+#pragma unroll
+                for (int g = 0; g < COLS; ++g)
+                    add_not_finite<IO, D, 4 * DT, (COLS > 1)>(kv, s, h, base, SK, pos[g], lowest[g] - 1, [quarter](int n) { return 16 * (n / 4) + 4 * quarter + n % 4; },
+                                                  [&](int n, float y) { o[g][n / 4][n % 4] += y; });
         }
     }
 
     // the waves' results, joined in a fixed order
-    sum += __shfl_xor(sum, 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
-    if (quarter == 0) {
-        lds.tops[wave][col] = top;
-        lds.sums[wave][col] = sum;
-    }
     // rows turned, no two in one bank; every pointer by its name, so that accesses stay LDS accesses
-    auto place = [&](int w, int r, int c) { return (w >> 2) * kFewGroups<IO, D> + r * (D / 4) + (c ^ r); };
+    auto place = [&](int w, int r, int c) { return ((w >> 2) + (r >> 4) * (WAVES / 4)) * kFewGroups<IO, D> + (r & 15) * (D / 4) + (c ^ (r & 15)); };
+    constexpr int of_wave = COLS * kFewGroups<IO, D>;                         // several: one array, four waves
+    static_assert(COLS == 1 || WAVES == 4, "outputs' places");
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-        const int at = place(wave, col, 4 * d + quarter), which = wave & 3;
-        if (which == 0) lds.out0[at] = o[d];
-        else if (which == 1) lds.out1[at] = o[d];
-        else if (which == 2) lds.out2[at] = o[d];
-        else lds.out3[at] = o[d];
+    for (int g = 0; g < COLS; ++g) {
+        sum[g] += __shfl_xor(sum[g], 16, 64);
+        sum[g] += __shfl_xor(sum[g], 32, 64);
+        if (quarter == 0) {
+            lds.tops[wave][16 * g + col] = top[g];
+            lds.sums[wave][16 * g + col] = sum[g];
+        }
     }
+#pragma unroll
+    for (int g = 0; g < COLS; ++g)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const int at = place(wave, 16 * g + col, 4 * d + quarter), which = wave & 3;
+            if constexpr (COLS > 1) lds.out0[of_wave * wave + at] = o[g][d];
+            else if (which == 0) lds.out0[at] = o[g][d];
+            else if (which == 1) lds.out1[at] = o[g][d];
+            else if (which == 2) lds.out2[at] = o[g][d];
+            else lds.out3[at] = o[g][d];
+        }
     __syncthreads();
     for (int x = threadIdx.x; x < rows * (D / 4); x += THREADS) {
         const int r = x / (D / 4), c = 4 * (x % (D / 4));
@@ -967,7 +1030,8 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
             const float f = lds.tops[w][r] == best ? 1.f : exp2_fast((lds.tops[w][r] - best) * k.c);
             const int at = place(w, r, c / 4);
             total += f * lds.sums[w][r];
-            y += f * ((w & 3) == 0 ? lds.out0[at] : (w & 3) == 1 ? lds.out1[at] : (w & 3) == 2 ? lds.out2[at] : lds.out3[at]);
+            if constexpr (COLS > 1) y += f * lds.out0[of_wave * w + at];
+            else y += f * ((w & 3) == 0 ? lds.out0[at] : (w & 3) == 1 ? lds.out1[at] : (w & 3) == 2 ? lds.out2[at] : lds.out3[at]);
         }
         const int token = r / k.G, head = h * k.G + (r - token * k.G);
         const long long at = (long long)(s.from + token) * k.a.H + head;
@@ -990,12 +1054,13 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds lds
 }
 
 // ---------------------------------------------------------------- the launches: either kind, or both for a mixed batch
-template <typename IO, int D>
-__global__ __launch_bounds__(256, D == 64 ? 4 : IO::kCoded ? 2 : 3) void k_attend_few(AttendK k) {
+template <typename IO, int D, int COLS>
+__global__ __launch_bounds__(256, COLS > 2 && D == 128 ? 1 : COLS > 1 ? 2 : D == 64 ? 4 : IO::kCoded ? 2 : 3) void k_attend_few(AttendK k) {
     __shared__ int pages[kSection + 2];
-    __shared__ float tops[4][16], sums[4][16];
-    __shared__ f32x4_t outs[4][kFewGroups<IO, D>];
-    few_rows<IO, D, 4>(k, blockIdx.x, FewLds{pages, tops, sums, outs[0], outs[1], outs[2], outs[3]});
+    __shared__ float tops[4][16 * COLS], sums[4][16 * COLS];
+    __shared__ f32x4_t outs[4][kFewGroups<IO, D> * COLS];
+    __shared__ uint4 query[kFewQueries<IO, D, COLS> ? kFewQueries<IO, D, COLS> : 1];
+    few_rows<IO, D, 4, COLS>(k, blockIdx.x, FewLds<16 * COLS>{pages, tops, sums, outs[0], outs[1], outs[2], outs[3], query});
 }
 
 // Waves a SIMD that registers (and, of workgroups of four waves with pages of 8 bits, LDS) leave room for.
@@ -1021,8 +1086,8 @@ __global__ __launch_bounds__(64 * WAVES, (tile_waves_a_simd<IO, D, WAVES>())) vo
     static_assert(kTileGroups<IO, D> >= (WAVES / 4) * kFewGroups<IO, D>, "outputs of few rows fit where tiles lie");
     const int tiles = (k.tile_blocks + 7) & ~7, block = blockIdx.x;              // eights again, for the XCDs
     if (block >= tiles) {
-        few_rows<IO, D, WAVES>(k, block - tiles, FewLds{pages, tops, sums, reinterpret_cast<f32x4_t *>(sk0), reinterpret_cast<f32x4_t *>(sv0), reinterpret_cast<f32x4_t *>(sk1),
-                                                        reinterpret_cast<f32x4_t *>(sv1)});
+        few_rows<IO, D, WAVES, 1>(k, block - tiles, FewLds<16>{pages, tops, sums, reinterpret_cast<f32x4_t *>(sk0), reinterpret_cast<f32x4_t *>(sv0), reinterpret_cast<f32x4_t *>(sk1),
+                                                        reinterpret_cast<f32x4_t *>(sv1), nullptr});
     } else if (block < k.tile_blocks) {
         tile_of_rows<IO, D, WAVES>(k, block, TileLds{sk0, sv0, sk1, sv1, raw, query, odd});
     }
@@ -1141,10 +1206,11 @@ AttendPlan attend_plan(int d, int dtype, int B, int T, int H, int Hkv, int max_n
     const long long rows = (long long)max_new * G;
     const bool even = T == (long long)B * max_new;                 // every sequence has max_new tokens
     const long long len = window ? std::min<long long>(max_len, (long long)window + max_new) : max_len;
-    // Up to 16 rows need no tile.  Beyond, one tile does for the few rows of a mixed batch too (23 sequences of up to 5 tokens, 8 heads a key head: 39 instead of 73 us) until
+    // Up to 16 rows (pages of 8 bits: 64 or 48) need no tile.  Beyond, one tile does for the few rows of a mixed batch too (23 sequences of up to 5 tokens, 8 heads a key head: 39 instead of 73 us) until
     // the tiles of the others make it long.
-    p.few = rows <= 16 || (!even && G <= 16 && rows > 128);
-    p.tile = rows > 16;
+    const int few_most = dtype == SPECTRE_E4M3 ? (d == 64 ? 64 : 48) : 16;
+    p.few = rows <= few_most || (!even && G <= 16 && rows > 128);
+    p.tile = rows > few_most;
     p.few_rows = !p.few ? 0 : p.tile ? 16 : (int)rows;
     p.few_splits = p.tile_splits = 1;
     const long long pairs = (long long)B * Hkv, place = 4 * d + 8;         // bytes of a part's results
@@ -1154,7 +1220,8 @@ AttendPlan attend_plan(int d, int dtype, int B, int T, int H, int Hkv, int max_n
         // two workgroups a compute unit of at least 256 keys each: four of 128 cost the join what they gain (one sequence of 32700 tokens 21.9 instead of
         // 19.8 us, 64 of 2000, which need no join then, 48 instead of 43), one leaves the memory waiting (16 fp32 sequences of 4000: 52.7 instead of 47.5).
         // No part longer than 2048 keys, for sequences of different lengths (32 of up to 32768: 202 us, with 4096 205).
-        long long s = std::max((512 + pairs - 1) / pairs, (len + 2047) / 2048);
+        long long s = std::max(rows > 16 ? 256 / pairs : (512 + pairs - 1) / pairs, (len + 2047) / 2048);
+        // More than 16 rows: one workgroup a compute unit (48 sequences of 60 rows over 560 keys 15.6 us, with two 18.7; 4 of 24 over 8000, d = 128, 18.6 and 20.0).
         s = std::min(s, (len + 255) / 256);
         s = std::min(s, std::max((512 + pairs - 1) / pairs, kPartBytes / (few_rows * (place + 4))));
         p.few_splits = (int)std::max(1ll, std::min(s, 256ll));
@@ -1221,6 +1288,19 @@ void launch_mixed(int waves, int blocks, const AttendK &k, hipStream_t st) {
     k_attend_mixed<IO, D, 4><<<blocks, 256, 0, st>>>(k);
 }
 
+template <typename IO, int D>
+void launch_few(const AttendK &k, hipStream_t st) {
+    if constexpr (IO::kCoded) {
+        if (k.few_rows > 16) {
+            if (k.few_rows <= 32) k_attend_few<IO, D, 2><<<k.few_blocks, 256, 0, st>>>(k);
+            else if (k.few_rows <= 48) k_attend_few<IO, D, 3><<<k.few_blocks, 256, 0, st>>>(k);
+            else if constexpr (D == 64) k_attend_few<IO, D, 4><<<k.few_blocks, 256, 0, st>>>(k);
+            return;
+        }
+    }
+    k_attend_few<IO, D, 1><<<k.few_blocks, 256, 0, st>>>(k);
+}
+
 hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const AttendArgs &a, const AttendPlan &p, void *ws, hipStream_t st) {
     AttendK k;
     k.kv = kv;
@@ -1263,7 +1343,7 @@ hipError_t launch_attend(const KvView &kv, int layers, int d, int io, const Atte
         SPECTRE_ATTEND_DISPATCH(CALL)
 #undef CALL
     } else if (p.few) {
-#define CALL(IO, D) k_attend_few<IO, D><<<k.few_blocks, 256, 0, st>>>(k)
+#define CALL(IO, D) launch_few<IO, D>(k, st)
         SPECTRE_ATTEND_DISPATCH(CALL)
 #undef CALL
     } else {

@@ -234,6 +234,59 @@ def test_keys_split_over_workgroups(d, n):
     check(out, lse, q, [n], rows, d ** -0.5, BF16)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [1, 4, 7, 8])
+@pytest.mark.parametrize("rows", [17, 32, 33, 48, 49, 64, 65])
+def test_some_rows_of_a_key_head(d, G, rows):
+    """Several new tokens of a few sequences, from one group of 16 rows of a key head to the first tile: sequences with fewer, one and no tokens, more new tokens than
+    there are tokens, with a window and without."""
+    print(f"case d={d} G={G} rows={rows}", flush=True)
+    n = rows // G
+    news, lens = [n, 1, 0, n, n // 2 + 1, n], [n + 700, 90, 5, n, 64, max(1, n - 2)]
+    page = (16, 256)[rows % 2]
+    pool, kv = make(d, 2, page, lens, d + G + rows)
+    q, start = queries(news, 2 * G, d, "bf16", rows)
+    for window in (0, 50):
+        out, lse = pool.attend(0, q, start, max_new=n, max_len=max(lens), window=window, want_lse=True)
+        check(out, lse, q, news, kv, d ** -0.5, BF16, window)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [5, 11, 16])
+def test_some_rows_with_absent_pages_and_nan(d, n):
+    """As above, four rows a token: absent pages hide their tokens, a NaN value reaches the rows that see it and no other."""
+    print(f"case d={d} n={n}", flush=True)
+    m, H = 700, 4
+    pool, kv = make(d, 1, 16, [m, m], n)
+    there = np.ones(m, bool)
+    for j, value in ((0, -1), (3, pool.pages), (20, -7), (43, 1 << 30)):
+        pool.table[0, j] = value
+        there[16 * j:16 * j + 16] = False
+    q, start = queries([n, n], H, d, "bf16", 5)
+    out, lse = pool.attend(0, q, start, max_new=n, max_len=m, want_lse=True)
+    check(out, lse, q, [n, n], kv, d ** -0.5, BF16, there=[there, np.ones(m, bool)])
+    at, channel = m - n + 2, 5                                # all tokens but the first two see it
+    pool.v_pages.view(torch.uint8)[0, int(pool.table[1, at // 16]), 0, 0, channel, at % 16] = NAN
+    got = pool.attend(0, q, start, max_new=n, max_len=m).float().cpu()
+    bad = torch.zeros(2 * n, H, d, dtype=torch.bool)
+    bad[n + 2:, :, channel] = True
+    assert torch.equal(got.isnan(), bad) and torch.equal(got[~bad], out.float().cpu()[~bad])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_some_rows_that_the_call_is_not_sized_for(d):
+    """A sequence with more new tokens than max_new says, and rows behind the last sequence, stay as they are; the others are the same without them."""
+    news, lens, H = [8, 9, 3], [300, 1200, 70], 4
+    pool, kv = make(d, 1, 64, lens, d)
+    q, start = queries(news + [4], H, d, "bf16", 1)
+    out = torch.full_like(q, 7)
+    lse = torch.full((q.shape[0], H), 7.0, device="cuda")
+    pool.attend(0, q, start[:4].contiguous(), max_new=8, max_len=1200, out=out, lse=lse)
+    for t in (out, lse):
+        assert (t[8:17] == 7).all() and (t[20:] == 7).all()
+    check(torch.cat((out[:8], out[17:20])), torch.cat((lse[:8], lse[17:20])), torch.cat((q[:8], q[17:20])), [8, 3], [kv[0], kv[2]], d ** -0.5, BF16)
+
+
 @pytest.mark.parametrize("page", [16, 64])
 @pytest.mark.parametrize("n", [1, 40])
 def test_pages_that_are_absent_and_values_that_are_nan(page, n):
