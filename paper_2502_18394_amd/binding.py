@@ -599,6 +599,8 @@ def _heads(d, rope, wq, wk, eps):
     wq, wk = _vector(wq, "wq", d), _vector(wk, "wk", d)
     if rope is None:
         return HeadsC(d, 0, 0, eps, None, wq, wk, 1, None)
+    if not rope.inv_freq.is_cuda:
+        raise ValueError("rope must be on the device")
     return HeadsC(d, rope.rot, rope.interleaved, eps, rope.inv_freq.data_ptr(), wq, wk, rope.axes, None if rope.axis is None else rope.axis.data_ptr())
 
 

@@ -77,3 +77,9 @@ def test_each_pair_goes_by_its_own_axis():
     angle = ref.angles([[np.pi / 2], [np.pi], [0.0]], [0, 1, 2], [1.0, 1.0, 1.0])
     assert np.allclose(ref.rotate(x, angle, True), [[[-1, 0, -2, -3, 4, 5, 6, 7]]])           # a quarter, a half, nothing, and what is not turned
     assert np.allclose(ref.rotate(x, angle, False), [[[-3, -1, 2, 0, -4, 5, 6, 7]]])
+
+
+def test_angles_in_host_memory_are_refused():
+    for axes in (None, [0, 1, 2, 0]):
+        with pytest.raises(ValueError, match="rope must be on the device"):
+            binding._heads(64, binding.Rope([1.0, 0.5, 0.25, 0.1], device="cpu", axes=axes), None, None, 1e-6)
