@@ -450,7 +450,8 @@ int spectre_prefix_step(spectre_prefix_cache *cache /*host*/, const void *v_t, c
  * spectre_kv_append takes the smallest power of two with which the largest finite magnitude of a block is no more than 448 (values of less than 2^-110 may
  * become zero; magnitudes are cut at 1.875 * 2^127, non-finite values become NaN).  Tokens that join others in a block keep the larger of its scale and
  * their own; where that grows, the others' codes are rounded to it, which leaves them as they are but for codes below the smallest normal one.
- * fork, compact and copy move scales with their pages.  Contents that a caller writes itself have to be finite as bf16 numbers, or NaN codes.
+ * fork, compact and copy move scales with their pages.  Contents that a caller writes itself have to be finite as bf16 numbers, or NaN codes; blocks that no token has
+ * reached, their scales among them, may hold anything: append writes a block's scales with its first token, and nothing else is looked at.
  */
 typedef struct {
     int layers, pages;         /* pages: of each layer                                       */

@@ -838,7 +838,7 @@ __device__ __forceinline__ void few_rows(const AttendK &k, int block, FewLds<16 
         };
         auto request_values = [&](int base) {
             const int key = base + PE * quarter;
-            vpage = page_at(key);
+            vpage = page_at(key);                                                 // a block of 16 that begins behind the end has no page here: its scale, which nobody has written, is not asked for
             const char *vb = reinterpret_cast<const char *>(kv.v) + (unsigned long long)(unsigned)vpage * page_bytes + v_at + ((key & mask) / PE) * (D * 16u);
             auto all = [&](auto stream) {
 #pragma unroll
