@@ -1220,8 +1220,10 @@ AttendPlan attend_plan(int d, int dtype, int B, int T, int H, int Hkv, int max_n
         // two workgroups a compute unit of at least 256 keys each: four of 128 cost the join what they gain (one sequence of 32700 tokens 21.9 instead of
         // 19.8 us, 64 of 2000, which need no join then, 48 instead of 43), one leaves the memory waiting (16 fp32 sequences of 4000: 52.7 instead of 47.5).
         // No part longer than 2048 keys, for sequences of different lengths (32 of up to 32768: 202 us, with 4096 205).
-        long long s = std::max(rows > 16 ? 256 / pairs : (512 + pairs - 1) / pairs, (len + 2047) / 2048);
-        // More than 16 rows: one workgroup a compute unit (48 sequences of 60 rows over 560 keys 15.6 us, with two 18.7; 4 of 24 over 8000, d = 128, 18.6 and 20.0).
+        long long s = std::max(p.few_rows > 16 ? 256 / pairs : (512 + pairs - 1) / pairs, (len + 2047) / 2048);
+        // More than 16 rows without a tile: one workgroup a compute unit (48 sequences of 60 rows over 560 keys 15.6 us, with two 18.7; 4 of 24 over 8000, d = 128, 18.6 and
+        // 20.0).  Few rows beside tiles have their two: they are a launch's last workgroups, and longer parts its tail (a chunk of 300 and 31 tokens over 2000 70.0 us, with
+        // half the parts 80.6, fp32 119 and 143, pages of 8 bits 50.8 and 54.7; one of 2048 and three over 8192 191 and 187).
         s = std::min(s, (len + 255) / 256);
         s = std::min(s, std::max((512 + pairs - 1) / pairs, kPartBytes / (few_rows * (place + 4))));
         p.few_splits = (int)std::max(1ll, std::min(s, 256ll));
