@@ -670,7 +670,7 @@ def qk_norm_rotate_backward(dq, dk, q, k, positions=None, rope=None, wq=None, wk
     rows = [_rows(t, name, q.dtype) for t, name in ((dq, "dq"), (dk, "dk"), (q, "q"), (k, "k"))]
     gq, gk = _like(q, stream), _like(k, stream)
     gw, wsp, wsn = (None, None), None, 0
-    if wq is not None:
+    if wq is not None and wk is not None:                                 # one of them alone is refused by the library
         gw = _like(wq, stream), _like(wk, stream)
         if ws is None:
             wsn = lib().spectre_heads_backward_workspace_bytes(T, d)
