@@ -153,7 +153,7 @@ def _stream(stream):
 
 def _given(ws):
     """(address, bytes) of the caller's workspace from its first 256-byte boundary on."""
-    at = ws.data_ptr()
+    at = _ptr(ws, "ws")
     off = -at % 256
     return at + off, max(0, ws.numel() * ws.element_size() - off)
 
@@ -164,7 +164,7 @@ def _workspace(nbytes, device, ws):
     if size < nbytes:
         size = nbytes + 256
         ws = torch.empty(size, dtype=torch.uint8, device=device)
-    at = ws.data_ptr()
+    at = _ptr(ws, "ws")
     off = -at % 256
     return ws, ctypes.c_void_p(at + off), ctypes.c_size_t(size - off)
 
