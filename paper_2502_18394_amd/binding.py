@@ -570,7 +570,7 @@ def _kv_prepare():
 class Rope:
     """Angles by which a head's channels are turned: position * inv_freq[i] for pair i.  inv_freq: float64 [rot / 2] (any rule a model has for
     it), or use Rope.of for theta^(-2 i / rot).  axes: for tokens with several positions (time, height, width), the axis of each pair, integers
-    [rot / 2] from 0 on; positions are then int32 [number of axes, T]."""
+    [rot / 2] from 0 on; positions are then int32 [axes, T], with a row for each axis up to the largest that a pair has; rows behind it have no part."""
 
     MAX_AXES = 8
 
@@ -624,7 +624,8 @@ def _positions(positions, rope, T):
         return _ints(positions, "positions", T)
     if positions.dtype != torch.int32:
         raise TypeError("positions must be int32")
-    if tuple(positions.shape) != (axes, T):
+    # rows of axes that no pair goes by lie behind those that are read
+    if positions.dim() != 2 or positions.shape[1] != T or not axes <= positions.shape[0] <= Rope.MAX_AXES:
         raise ValueError(f"positions must have shape [{axes}, {T}]")
     return _ptr(positions, "positions")
 
