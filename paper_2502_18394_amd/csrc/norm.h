@@ -22,7 +22,7 @@ struct NormGrads {
 
 hipError_t load_kernels_norm();
 hipError_t launch_norm(const NormRows &n, int io, void *sum, void *y, float *scales, hipStream_t st);     // scales: y in 8 bits
-int norm_backward_blocks(int T, int groups);             // as many rows of partial sums
+int norm_backward_blocks(int T, int groups, bool weights);   // with the weights' gradient: as many rows of partial sums
 hipError_t launch_norm_backward(const NormRows &n, const NormGrads &g, int io, void *gx, float *gw, float *partial, hipStream_t st);
 
 }  // namespace spectre

@@ -294,15 +294,18 @@ hipError_t launch_norm(const NormRows &n, int io, void *sum, void *y, float *sca
 
 // 16 waves a compute unit, more workgroups where each would have more than kNormChain rows.  (Half of them: 16384 rows of 2048 bf16 channels, forward and backward, 105.6
 // instead of 108.2 us, but 5000 of 8192 151 instead of 124.)
-int norm_backward_blocks(int T, int groups) {
+int norm_backward_blocks(int T, int groups, bool weights) {
     const int slots = row_slots(groups);
-    if (T <= 8 * slots) return T > 0;            // one workgroup, whose sums are the gradient: no other launch (8 rows of 2048, forward and backward, 19.4 us; 9 rows, with it, 24.1)
+    if (T == 0) return 0;
+    // one workgroup, whose sums are the weights' gradient: no other launch (8 rows of 2048, forward and backward, 19.4 us; 9 rows, with it, 24.1).  Without
+    // that gradient there is none to save: 8 rows of 16384 7.9 us, by one workgroup 17.2
+    if (weights && T <= 8 * slots) return 1;
     const long long most = std::max(1024ll * 256 / group_threads(groups), ((long long)T + kNormChain - 1) / kNormChain);
     return (int)std::min<long long>(((long long)T + slots - 1) / slots, most);
 }
 
 hipError_t launch_norm_backward(const NormRows &n, const NormGrads &g, int io, void *gx, float *gw, float *partial, hipStream_t st) {
-    const int size = io == SPECTRE_BF16 ? 2 : 4, groups = n.D * size / 16, blocks = norm_backward_blocks(n.T, groups);
+    const int size = io == SPECTRE_BF16 ? 2 : 4, groups = n.D * size / 16, blocks = norm_backward_blocks(n.T, groups, gw != nullptr);
     const bool stream = (size_t)n.T * n.D * size > kL2Bytes;
     auto launch = [&](auto kernel) { kernel<<<blocks, group_threads(groups), 0, st>>>(n, g, (uint4 *)gx, blocks == 1 ? gw : partial, stream); };
 #define CALL(IO, LANES, CHUNKS) (gw ? launch(k_norm_backward<IO, LANES, CHUNKS, true>) : launch(k_norm_backward<IO, LANES, CHUNKS, false>))

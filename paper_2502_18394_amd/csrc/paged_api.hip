@@ -364,7 +364,7 @@ int spectre_norm_forward(const void *x, long long x_stride, const void *delta, l
 
 size_t spectre_norm_backward_workspace_bytes(int T, int D, spectre_dtype io) {
     if (check_norm(nullptr, T, D, 0.f, io, "norm_backward")) return 0;
-    const int blocks = norm_backward_blocks(T, D * size_of(io) / 16);
+    const int blocks = norm_backward_blocks(T, D * size_of(io) / 16, true);
     return blocks > 1 ? align256((size_t)blocks * D * sizeof(float)) : 0;
 }
 
