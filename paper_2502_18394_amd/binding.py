@@ -698,7 +698,7 @@ def _matrix(t, name, T, D, dtype):
     return t.data_ptr(), st if T > 1 else D
 
 
-NORM_GROUP = 128
+NORM_GROUP, NORM_MOST_BYTES = 128, 32768          # channels of a scale; the widest row
 
 
 def add_norm(x, weight=None, delta=None, eps=1e-6, dtype=None, sum_out=None, out=None, scales=None, stream=None):

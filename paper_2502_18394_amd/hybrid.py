@@ -50,6 +50,9 @@ class HybridDecoder:
 
     def _norm(self, x, more=None):
         """(x + more, its norm): `more` is what the layer before adds to the residual."""
+        if self.width * x.element_size() > binding.NORM_MOST_BYTES:
+            x = self._sum(x, more)
+            return x, torch.nn.functional.rms_norm(x.float(), (self.width,)).to(self.dtype)
         return binding.add_norm(x, None, more, torch.finfo(torch.float32).eps)
 
     @staticmethod
