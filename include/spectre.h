@@ -452,6 +452,9 @@ int spectre_prefix_step(spectre_prefix_cache *cache /*host*/, const void *v_t, c
  * their own; where that grows, the others' codes are rounded to it, which leaves them as they are but for codes below the smallest normal one.
  * fork, compact and copy move scales with their pages.  Contents that a caller writes itself have to be finite as bf16 numbers, or NaN codes; blocks that no token has
  * reached, their scales among them, may hold anything: append writes a block's scales with its first token, and nothing else is looked at.
+ *
+ * Clear a spectre_kv or spectre_heads (= {0}) before filling it: fields behind those that a caller knows (version 140 added `scales`, `axes` and `axis`) have to be
+ * zero where they are not used.
  */
 typedef struct {
     int layers, pages;         /* pages: of each layer                                       */
@@ -547,7 +550,8 @@ int spectre_kv_append(const spectre_kv *kv /*host*/, int layer, const spectre_he
 /*
  * A residual's addition and the root-mean-square norm of the sum, in one pass: sum = x + delta (rounded to io, and normed as it is kept),
  * y = w * sum / sqrt(mean sum^2 + eps).  Rows x, delta [T, D], row t `stride` elements from row t - 1 (a multiple of 16 bytes, at least D), 16-byte aligned;
- * outputs are dense.  D * size of io: a multiple of 16 bytes, up to 32768.  delta and sum NULL: y is the norm of x.  w device fp32 [D], 16-byte aligned, NULL: ones.
+ * outputs are dense and overlap neither inputs nor each other (sum has memory of its own, too).  D * size of io: a multiple of 16 bytes, up to 32768.  delta and sum
+ * NULL: y is the norm of x.  w device fp32 [D], 16-byte aligned, NULL: ones.
  *   y_type  io, or SPECTRE_E4M3: codes [T, D] with scales fp32 [T, D / SPECTRE_NORM_GROUP], D a multiple of that; a scale is the largest magnitude of its channels
  *           / 448 (0, and with it codes of 0, where that is below 2^-126), what is meant is code * scale.  scales NULL otherwise.
  * spectre_norm_backward: from dy (of y, in io whatever y's type was), sum as it was kept (without an addition: x) and dsum (of sum as a residual, NULL: none) the gradient

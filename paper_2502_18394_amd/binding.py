@@ -703,7 +703,7 @@ NORM_GROUP, NORM_MOST_BYTES = 128, 32768          # channels of a scale; the wid
 
 def add_norm(x, weight=None, delta=None, eps=1e-6, dtype=None, sum_out=None, out=None, scales=None, stream=None):
     """A residual's addition and the root-mean-square norm of the sum in one pass (spectre_norm_forward).  x, delta [T, D] f32/bf16, rows any 16-byte multiple
-    apart; weight float32 [D] (None: ones).  Returns (sum, y), the sum in x's dtype (x itself without delta), y in x's dtype, or with dtype=torch.float8_e4m3fn
+    apart; weight float32 [D] (None: ones); given outputs overlap no input.  Returns (sum, y), the sum in x's dtype (x itself without delta), y in x's dtype, or with dtype=torch.float8_e4m3fn
     (sum, codes, scales): a float32 scale for each 128 channels, scales [T, D / 128], and what is meant is code * scale."""
     T, D = x.shape
     io, kind, coded = _dtype_code(x), x.dtype, dtype == torch.float8_e4m3fn
