@@ -726,7 +726,7 @@ __device__ __forceinline__ void tile_of_rows(const AttendK &k, int block, TileLd
 // barrier between steps, and with every wave at work, a tile's way is the longer one up to 64 rows (d = 128: 48, whose registers leave one wave a SIMD): 64 sequences of
 // 8 tokens over 8000, 32 rows, 112 us, as tiles 179; 64 of 16 over 2000, 64 rows, 36 and 60; d = 128, 32 of 5 over 4000, 40 rows, 26 and 32.5, but 64 rows (registers
 // spilled) 48 and 34.5.  A second term (see above) costs more here, where the first one's registers are all there are: 32 rows over 8000 122 us instead of 111, 64 rows over 2000 55
-// instead of 37 (it spills), 40 rows of d = 128 over 4000 27.3 instead of 25.3, for outputs that are off by 1.65e-3 instead of 1.9e-3.
+// instead of 37 (it spills), 40 rows of d = 128 over 4000 27.3 instead of 25.3, for outputs that would be off by 1.65e-3, as those of up to 16 rows are, instead of 1.9e-3.
 // Short parts take the longer the more code they go through once (kernels of 12.5, 14.8 and 17.2 KB, one step each: 7.6, 9.6 and 11.5 us): outputs are joined in one loop
 // for all groups (16 windows of 5 tokens, 40 rows, d = 128: 21.3 us, group by group 23.1).
 constexpr int kSection = 256;                      // page numbers in LDS at a time
